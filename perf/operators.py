@@ -30,7 +30,7 @@ import torch
 
 own = False          # whether run() calls the package or computes the plain form
 
-SCRATCH = 128 << 20  # device scratch that a program keeps for these calls
+SCRATCH = 128 << 20  # device scratch that a program keeps for the calls that take some
 PAD = -1             # "no token here"
 _TYPE = {"bf16": torch.bfloat16, "f32": torch.float32}
 _BYTES = {"bf16": 2, "f32": 4}
@@ -310,7 +310,7 @@ def _own_score(st):
     case = st["case"]
     top_token, top_logprob = (st["top_token"], st["top_logprob"]) if case["top"] else (None, None)
     sv.sv_token_logprobs(st["z"], st["tokens"], st["logprob"], st["lse"], st["entropy"], st["rank"], top_token,
-                         top_logprob, temperature=case["T"], t_offsets=st["offsets"], ws=st["scratch"])
+                         top_logprob, temperature=case["T"], t_offsets=st["offsets"])
     names = ["logprob", "lse", "entropy", "rank"] + (["top_token", "top_logprob"] if case["top"] else [])
     return {n: st[n] for n in names}
 
@@ -318,8 +318,7 @@ def _own_score(st):
 def _own_score_grad(st):
     import paper_2509_24328_amd as sv
     sv.sv_token_logprobs_grad(st["z"], st["tokens"], st["g_logprob"], st["dz"], g_entropy=st["g_entropy"],
-                              logprob=st["logprob"], entropy=st["entropy"], temperature=st["case"]["T"],
-                              ws=st["scratch"])
+                              logprob=st["logprob"], entropy=st["entropy"], temperature=st["case"]["T"])
     return {n: st[n] for n in ("logprob", "entropy", "dz") if st[n] is not None}
 
 
