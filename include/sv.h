@@ -14,7 +14,9 @@
  * normalisers over from sv_row_stats through the workspace and sweeps the
  * target rows only).  Further down: the profile-construction pass that
  * produces the table, the sampling warps (temperature, top-k, top-p,
- * repetition penalty) with dense and compacted forms of the step, and helpers.
+ * repetition penalty) with dense and compacted forms of the step, what is done
+ * with the emitted tokens and with the models that drafted them (log-probabilities
+ * of tokens and their gradient, embedding rows and theirs, gradient norm), and helpers.
  *
  * Conventions common to all calls
  *   - Every data pointer is a DEVICE pointer owned by the caller.  The library
@@ -81,10 +83,11 @@ enum {
   SV_FLAG_BAD_TOKEN = 16,         /* drafted token id outside [0, V)                          */
   SV_FLAG_NOT_COMPACT = 32,       /* a needed row has no compact support (count < 0): the
                                      result is not valid, use the dense warped entry points   */
-  SV_FLAG_NO_CHAIN = 64           /* sv_verify_sample_chained: the workspace does not hold the
+  SV_FLAG_NO_CHAIN = 64,          /* sv_verify_sample_chained: the workspace does not hold the
                                      draft normalisers of these arguments (no sv_row_stats call
                                      on it, or one with another z_d, x, shape, dtype, draft
                                      temperature or draft cutoffs): the draft rows count as bad   */
+  SV_FLAG_NONFINITE = 128         /* sv_grad_norm, sv_clip_grad_norm: the norm is not finite      */
 };
 
 /* Largest B*k accepted by sv_select_length (keys are sorted in one workgroup). */
@@ -97,6 +100,11 @@ enum {
 #define SV_PENALTY_MAX_TOKENS 4096
 /* Largest per-row capacity of a compacted support (sv_warp_compact). */
 #define SV_SUPPORT_MAX_CAP 1024
+
+/* Largest number of alternatives sv_token_logprobs lists per position. */
+#define SV_TOP_MAX 32
+/* Largest number of tokens one sv_embedding_grad call takes. */
+#define SV_EMBEDDING_MAX_TOKENS (1 << 24)
 
 /* Device scratch that sv_verify_sample_static holds on every GPU it runs on. */
 #define SV_STATIC_SCRATCH_BYTES (1 << 20)
@@ -573,6 +581,121 @@ int sv_accept_ratio_sparse(const int32_t* count_t, const int32_t* token_t, const
                            int t_rows_per_seq, const int32_t* count_d, const int32_t* token_d,
                            const double* prob_d, int cap, const int32_t* x, int B, int k, int V,
                            float* ratio, uint32_t* flags_or_null, sv_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The tokens that a step has emitted, and the models that drafted them: what is
+ * computed over the vocabulary next to the step itself.  A server returns the
+ * log-probabilities of the emitted tokens; S is as high as the companion is like
+ * the target, and one way to acquire a companion is to fit it to the target's
+ * answers: embedding rows, the model's body, log-probabilities with their
+ * gradient, the embedding's gradient, the norm of all gradients.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * Log-probabilities of given tokens under p = soft-max(z / temperature), row by row:
+ *   logprob = log p(token)
+ *   lse     = log sum_v exp(z_v / temperature)
+ *   entropy = - sum_v p(v) log p(v)                    (nats)
+ *   rank    = 1 + the number of entries before the token's in the order by descending
+ *             logit, equal ones by ascending token id   (1: the most probable token)
+ *   top_token, top_logprob   the first n_top entries of that order
+ *   z       dense [B, P, V], or packed [n_rows, V] with t_offsets_or_null [B+1]: position
+ *           (b, i) is row t_offsets[b] + i for i < t_offsets[b+1] - t_offsets[b] and not
+ *           there otherwise; rows addressed outside [0, n_rows) are bad rows, never read.
+ *           Consecutive rows lie z_stride >= V elements apart (rows padded to a multiple)
+ *   tokens_or_null [B, P] int32   -1: no token at this position.  NULL: no token is asked
+ *           for, all rows are swept; logprob and rank must be NULL then
+ *   logprob_or_null, lse_or_null, entropy_or_null  [B, P] float,  rank_or_null [B, P] int32
+ *   top_token_or_null [B, P, n_top] int32, top_logprob_or_null [B, P, n_top] float
+ *           0 <= n_top <= SV_TOP_MAX; both needed when n_top > 0
+ *   flags_or_null [B, P] uint32   SV_FLAG_BAD_ROW / SV_FLAG_BAD_TOKEN
+ * Positions without a token, or not there, are not read: logprob, lse, entropy and rank
+ * are 0, top_token -1, top_logprob -inf.  An entry without mass (-inf, or below the range
+ * of the logits) has log-probability -inf and is no alternative: past the last one
+ * top_token is -1 and top_logprob -inf.  Bad rows: NaN, rank 0, top_token -1.  Bad token:
+ * logprob NaN and rank 0, the rest as ever.
+ * V <= 16777216, temperature in [1e-3, 1e3].
+ */
+int sv_token_logprobs(const void* z, int64_t z_stride, const int32_t* t_offsets_or_null, int n_rows,
+                      const int32_t* tokens_or_null, int B, int P, int V, int dtype, float temperature, int n_top,
+                      float* logprob_or_null, float* lse_or_null, float* entropy_or_null, int32_t* rank_or_null,
+                      int32_t* top_token_or_null, float* top_logprob_or_null, uint32_t* flags_or_null,
+                      sv_stream_t stream);
+
+/*
+ * Gradient of  sum_r ( g_logprob[r] * logprob[r] + g_entropy[r] * entropy[r] )  with respect to
+ * the logits, together with logprob and entropy (as in sv_token_logprobs):
+ *   dz[r, v] = ( g_logprob (1[v = token] - p(v)) - g_entropy p(v) (log p(v) + entropy) ) / temperature
+ * A loss that weighs log-probabilities by known numbers (negative log-likelihood:
+ * g_logprob = -1/n; policy gradients: advantages; an entropy bonus) takes this one call.
+ *   z, dz   [rows, V] dtype, rows z_stride and dz_stride >= V elements apart; dz may be z
+ *           itself (same address and stride), and must not overlap it otherwise
+ *   tokens  [rows] int32          -1: no token, dz[r, :] = 0, logprob = entropy = 0; z is not read
+ *   g_logprob [rows] float, g_entropy_or_null [rows] float           in
+ *   logprob_or_null, entropy_or_null [rows] float                    out
+ *   flags_or_null [rows] uint32   SV_FLAG_BAD_ROW / SV_FLAG_BAD_TOKEN: dz[r, :] is NaN then
+ * bfloat16 gradients are rounded once, to nearest-even.  Columns of dz past V are left as they are.
+ * V <= 16777216, temperature in [1e-3, 1e3].
+ */
+int sv_token_logprobs_grad(const void* z, int64_t z_stride, const int32_t* tokens, int rows, int V, int dtype,
+                           float temperature, const float* g_logprob, const float* g_entropy_or_null,
+                           float* logprob_or_null, float* entropy_or_null, void* dz, int64_t dz_stride,
+                           uint32_t* flags_or_null, sv_stream_t stream);
+
+/*
+ * Embedding rows of tokens: out[i, :] = scale * table[ids[i], :], formed in float32 and rounded once.
+ *   table [V, D] dtype, ids [n] int32   in;   out [n, D] dtype   out (must not overlap table)
+ *   flags_or_null [n] uint32            out  SV_FLAG_BAD_TOKEN for ids outside [0, V) other than -1
+ * Rows of id -1 (padding) and of bad tokens are zeros.  n >= 0.
+ */
+int sv_embedding(const void* table, const int32_t* ids, int n, int V, int D, int dtype, float scale,
+                 void* out, uint32_t* flags_or_null, sv_stream_t stream);
+
+/* Bytes of device scratch sv_embedding_grad needs (0 if the shape is invalid). */
+size_t sv_embedding_grad_workspace_bytes(int n, int V, int D);
+
+/*
+ * Gradient of the table of sv_embedding:
+ *   grad_table[v, :] = scale * sum over {i : ids[i] = v} of grad_out[i, :]   (+ grad_table[v, :] if accumulate)
+ * in float32, rounded once.  The tokens are sorted first and the rows of one token are
+ * summed in the order of their positions, so the result does not depend on timing.
+ *   grad_out [n, D] dtype, ids [n] int32 (ids outside [0, V) contribute nothing)   in
+ *   grad_table [V, D] table_dtype    out  every row is written; with accumulate != 0 (a table
+ *            tied to the output projection) only rows of tokens that occur are touched
+ *   ws: at least sv_embedding_grad_workspace_bytes(n, V, D) bytes, 256-byte aligned
+ * Limits: n <= SV_EMBEDDING_MAX_TOKENS, V <= 16777216.
+ */
+int sv_embedding_grad(const void* grad_out, int dtype, const int32_t* ids, int n, int V, int D, float scale,
+                      void* grad_table, int table_dtype, int accumulate,
+                      void* ws, size_t ws_bytes, sv_stream_t stream);
+
+/* Bytes of device scratch sv_grad_norm / sv_clip_grad_norm need for n tensors (0 if n < 0). */
+size_t sv_grad_norm_workspace_bytes(int n);
+
+/*
+ * 2-norm over all elements of n tensors: norm[0] = sqrt( sum_t sum_j grads[t][j]^2 ), squares and
+ * sums in float64 and in an order that depends on the sizes alone.
+ *   grads, numel, dtype   HOST arrays of length n: device pointer, number of elements (>= 0) and
+ *            SV_F32 / SV_BF16 of each tensor (tensors of no elements may be NULL)
+ *   norm [1] float        out
+ *   flag_or_null [1] uint32  out  SV_FLAG_NONFINITE or 0
+ *   ws: at least sv_grad_norm_workspace_bytes(n) bytes, 256-byte aligned
+ */
+int sv_grad_norm(int n, const void* const* grads, const int64_t* numel, const int* dtype,
+                 float* norm, uint32_t* flag_or_null, void* ws, size_t ws_bytes, sv_stream_t stream);
+
+/*
+ * sv_grad_norm, and the gradients scaled to a norm of at most max_norm:
+ *   out[t][j] = grads[t][j] * min(1, max_norm / (norm + 1e-6))
+ * in float32, rounded once to out_dtype[t].
+ *   out, out_dtype   HOST arrays of length n.  out[t] may be grads[t] itself (same type): such
+ *            tensors are not written when nothing is to be scaled.  Tensors must not overlap otherwise
+ * If the norm is not finite the factor is 1 (the gradients stay as they are) and SV_FLAG_NONFINITE
+ * is set.  max_norm > 0.
+ */
+int sv_clip_grad_norm(int n, const void* const* grads, const int64_t* numel, const int* dtype, float max_norm,
+                      void* const* out, const int* out_dtype, float* norm, uint32_t* flag_or_null,
+                      void* ws, size_t ws_bytes, sv_stream_t stream);
 
 /*
  * The uniforms sv_verify_sample draws (for tests and for callers that want to

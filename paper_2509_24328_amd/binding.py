@@ -22,6 +22,7 @@ SV_ERR_WORKSPACE, SV_ERR_LAUNCH, SV_ERR_TOO_LARGE = -5, -6, -7
 FLAG_BAD_ROW, FLAG_NEAR_TIE, FLAG_RESIDUAL_FALLBACK, FLAG_NEAR_CDF_EDGE, FLAG_BAD_TOKEN = 1, 2, 4, 8, 16
 FLAG_NOT_COMPACT = 32
 FLAG_NO_CHAIN = 64
+FLAG_NONFINITE = 128
 SV_SUPPORT_MAX_CAP = 1024
 SV_SELECT_MAX_KEYS = 8192
 SV_MAX_K = 64
@@ -34,9 +35,13 @@ EXPORTS = ("sv_strerror", "sv_workspace_bytes", "sv_row_stats", "sv_accept_estim
            "sv_accept_ratio_sparse", "sv_verify_sample_static", "sv_accept_ratio_warped",
            "sv_warp_cutoffs_multi", "sv_warp_compact_multi", "sv_verify_sample_chained",
            "sv_verify_sample_warped_chained", "sv_estimate_select", "sv_repetition_penalty",
-           "sv_repetition_penalty_multi")
+           "sv_repetition_penalty_multi", "sv_token_logprobs", "sv_token_logprobs_grad", "sv_embedding",
+           "sv_embedding_grad_workspace_bytes", "sv_embedding_grad", "sv_grad_norm_workspace_bytes", "sv_grad_norm",
+           "sv_clip_grad_norm")
 SV_WARP_MAX_TENSORS = 8
 SV_STATIC_SCRATCH_BYTES = 1 << 20
+SV_TOP_MAX = 32
+SV_EMBEDDING_MAX_TOKENS = 1 << 24
 (SV_KERNEL_ROW_STATS, SV_KERNEL_ACCEPT_ESTIMATE, SV_KERNEL_SELECT_LENGTH, SV_KERNEL_VERIFY_ROWS,
  SV_KERNEL_VERIFY_MASS, SV_KERNEL_VERIFY_PICK, SV_KERNEL_COUNT) = range(7)
 
@@ -109,6 +114,23 @@ lib.sv_accept_ratio_sparse.restype = _i
 lib.sv_accept_ratio_sparse.argtypes = [_vp, _vp, _vp, _i, _vp, _vp, _vp, _i, _vp, _i, _i, _i, _vp, _vp, _vp]
 lib.sv_uniforms.restype = _i
 lib.sv_uniforms.argtypes = [ctypes.c_uint64, ctypes.c_uint32, _i, _i, _vp, _vp, _vp]
+_ll = ctypes.c_longlong
+lib.sv_token_logprobs.restype = _i
+lib.sv_token_logprobs.argtypes = [_vp, _ll, _vp, _i, _vp, _i, _i, _i, _i, _f, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+lib.sv_token_logprobs_grad.restype = _i
+lib.sv_token_logprobs_grad.argtypes = [_vp, _ll, _vp, _i, _i, _i, _f, _vp, _vp, _vp, _vp, _vp, _ll, _vp, _vp]
+lib.sv_embedding.restype = _i
+lib.sv_embedding.argtypes = [_vp, _vp, _i, _i, _i, _i, _f, _vp, _vp, _vp]
+lib.sv_embedding_grad_workspace_bytes.restype = _sz
+lib.sv_embedding_grad_workspace_bytes.argtypes = [_i, _i, _i]
+lib.sv_embedding_grad.restype = _i
+lib.sv_embedding_grad.argtypes = [_vp, _i, _vp, _i, _i, _i, _f, _vp, _i, _i, _vp, _sz, _vp]
+lib.sv_grad_norm_workspace_bytes.restype = _sz
+lib.sv_grad_norm_workspace_bytes.argtypes = [_i]
+lib.sv_grad_norm.restype = _i
+lib.sv_grad_norm.argtypes = [_i, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+lib.sv_clip_grad_norm.restype = _i
+lib.sv_clip_grad_norm.argtypes = [_i, _vp, _vp, _vp, _f, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 lib.sv_set_timing_events.restype = _i
 lib.sv_set_timing_events.argtypes = [_i, _vp, _vp]
 
@@ -439,3 +461,142 @@ def sv_accept_ratio_sparse(sup_t, sup_d, x, V, ratio, flags=None, stream=None):
     _check(lib.sv_accept_ratio_sparse(_ptr(sup_t.count), _ptr(sup_t.token), _ptr(sup_t.prob), sup_t.rows // B,
                                       _ptr(sup_d.count), _ptr(sup_d.token), _ptr(sup_d.prob), sup_t.cap, _ptr(x),
                                       B, k, V, _ptr(ratio), _ptr(flags), _stream(stream)))
+
+
+def _strided(z):
+    """(address, elements from row to row) of logits [..., V] whose rows lie at one distance from each other, as
+    columns [:V] of a contiguous tensor with wider rows do; other layouts are refused."""
+    if z.is_cuda and z.is_contiguous():
+        return z.data_ptr(), z.shape[-1]
+    stride = z.stride(-2) if z.dim() >= 2 else 0
+    ok = z.is_cuda and z.dim() >= 2 and (z.stride(-1) == 1 or z.shape[-1] == 1) and stride >= z.shape[-1]
+    for d in range(z.dim() - 2):
+        ok = ok and (z.shape[d] == 1 or z.stride(d) == z.stride(d + 1) * z.shape[d + 1])
+    if not ok:
+        raise ValueError("sv: logits must be device tensors whose rows are contiguous and equally far apart "
+                         f"(got device={z.device}, shape={tuple(z.shape)}, strides={z.stride()})")
+    return z.data_ptr(), stride
+
+
+def _outputs(shape, *tensors):
+    """Refuses outputs that are smaller than what a call writes."""
+    n = 1
+    for s in shape:
+        n *= s
+    for t in tensors:
+        if t is not None and t.numel() != n:
+            raise SvError(SV_ERR_INVALID_ARG)
+
+
+def _i32(*tensors):                 # (unsigned ones hold flags)
+    for t in tensors:
+        if t is not None and t.dtype not in (torch.int32, torch.uint32):
+            raise SvError(SV_ERR_DTYPE)
+
+
+def _f32(*tensors):
+    for t in tensors:
+        if t is not None and t.dtype != torch.float32:
+            raise SvError(SV_ERR_DTYPE)
+
+
+def sv_token_logprobs(z, tokens, logprob, lse=None, entropy=None, rank=None, top_token=None, top_logprob=None,
+                      flags=None, temperature=1.0, t_offsets=None, stream=None):
+    """z: [B, P, V] (or [N, V]) with tokens [B, P] ([N]); or packed [n_rows, V] with t_offsets [B+1] and tokens
+    [B, P].  tokens None: every row of z is swept, logprob and rank are None."""
+    V = z.shape[-1]
+    if t_offsets is not None:
+        if tokens is None or tokens.dim() != 2 or z.dim() != 2 or t_offsets.numel() != tokens.shape[0] + 1:
+            raise SvError(SV_ERR_INVALID_ARG)
+        B, P = tokens.shape
+        n_rows = z.shape[0]
+    else:
+        n_rows, B, P = 0, z.numel() // V if V else 0, 1
+        if tokens is not None and tokens.numel() != B:
+            raise SvError(SV_ERR_INVALID_ARG)
+    n_top = 0 if top_token is None else top_token.shape[-1]
+    _i32(tokens, rank, top_token, t_offsets, flags)
+    _f32(logprob, lse, entropy, top_logprob)
+    _outputs((B, P), logprob, lse, entropy, rank, flags)
+    _outputs((B, P, n_top), top_token, top_logprob)
+    addr, stride = _strided(z)
+    _check(lib.sv_token_logprobs(addr, stride, _ptr(t_offsets), n_rows, _ptr(tokens), B, P, V, _dtype_tag(z),
+                                 temperature, n_top, _ptr(logprob), _ptr(lse), _ptr(entropy), _ptr(rank),
+                                 _ptr(top_token), _ptr(top_logprob), _ptr(flags), _stream(stream)))
+
+
+def sv_token_logprobs_grad(z, tokens, g_logprob, dz, g_entropy=None, logprob=None, entropy=None, flags=None,
+                           temperature=1.0, stream=None):
+    """z, dz: [..., V], dz may be z; tokens, g_logprob, g_entropy, logprob, entropy: one entry per row."""
+    V = z.shape[-1]
+    rows = z.numel() // V if V else 0
+    if dz.shape != z.shape or dz.dtype != z.dtype:
+        raise SvError(SV_ERR_INVALID_ARG)
+    _i32(tokens, flags)
+    _f32(g_logprob, g_entropy, logprob, entropy)
+    _outputs((rows,), tokens, g_logprob, g_entropy, logprob, entropy, flags)
+    addr, stride = _strided(z)
+    d_addr, d_stride = _strided(dz)
+    _check(lib.sv_token_logprobs_grad(addr, stride, _ptr(tokens), rows, V, _dtype_tag(z), temperature,
+                                      _ptr(g_logprob), _ptr(g_entropy), _ptr(logprob), _ptr(entropy), d_addr,
+                                      d_stride, _ptr(flags), _stream(stream)))
+
+
+def sv_embedding(table, ids, out, scale=1.0, flags=None, stream=None):
+    V, D = table.shape
+    n = ids.numel()
+    if out.dtype != table.dtype:
+        raise SvError(SV_ERR_INVALID_ARG)
+    _i32(ids, flags)
+    _outputs((n, D), out)
+    _outputs((n,), flags)
+    _check(lib.sv_embedding(_ptr(table), _ptr(ids), n, V, D, _dtype_tag(table), scale, _ptr(out), _ptr(flags),
+                            _stream(stream)))
+
+
+def sv_embedding_grad_workspace_bytes(n, V, D):
+    return int(lib.sv_embedding_grad_workspace_bytes(n, V, D))
+
+
+def sv_embedding_grad(grad_out, ids, grad_table, scale=1.0, accumulate=False, ws=None, stream=None):
+    V, D = grad_table.shape
+    n = ids.numel()
+    _i32(ids)
+    _outputs((n, D), grad_out)
+    _check(lib.sv_embedding_grad(_ptr(grad_out), _dtype_tag(grad_out), _ptr(ids), n, V, D, scale, _ptr(grad_table),
+                                 _dtype_tag(grad_table), int(accumulate), _ptr(ws), 0 if ws is None else ws.numel(),
+                                 _stream(stream)))
+
+
+def sv_grad_norm_workspace_bytes(n):
+    return int(lib.sv_grad_norm_workspace_bytes(n))
+
+
+def _tensor_lists(tensors):
+    """HOST arrays of the addresses, sizes and types of a list of contiguous device tensors."""
+    n = len(tensors)
+    return (n, _host_ptrs(tensors), (ctypes.c_longlong * n)(*[t.numel() for t in tensors]),
+            (ctypes.c_int * n)(*[_dtype_tag(t) for t in tensors]))
+
+
+def sv_grad_norm(grads, norm, flag=None, ws=None, stream=None):
+    """grads: a list of tensors; norm: [1] float32."""
+    n, ptrs, numel, tags = _tensor_lists(grads)
+    _f32(norm)
+    _i32(flag)
+    _check(lib.sv_grad_norm(n, ptrs, numel, tags, _ptr(norm), _ptr(flag), _ptr(ws), 0 if ws is None else ws.numel(),
+                            _stream(stream)))
+
+
+def sv_clip_grad_norm(grads, max_norm, norm, out=None, flag=None, ws=None, stream=None):
+    """out: a list of tensors of the same numbers of elements (None: in place)."""
+    n, ptrs, numel, tags = _tensor_lists(grads)
+    o_ptrs, o_tags = ptrs, tags
+    if out is not None:
+        if len(out) != n or any(o.numel() != g.numel() for o, g in zip(out, grads)):
+            raise SvError(SV_ERR_INVALID_ARG)
+        _, o_ptrs, _, o_tags = _tensor_lists(out)
+    _f32(norm)
+    _i32(flag)
+    _check(lib.sv_clip_grad_norm(n, ptrs, numel, tags, max_norm, o_ptrs, o_tags, _ptr(norm), _ptr(flag), _ptr(ws),
+                                 0 if ws is None else ws.numel(), _stream(stream)))

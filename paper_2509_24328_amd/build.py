@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsv.so")
 SOURCES = ["row_stats.hip", "warp.hip", "verify_sample.hip", "select_length.hip", "profile.hip", "sparse.hip",
-           "accept_estimate.hip", "penalty.hip", "api.hip"]
+           "accept_estimate.hip", "penalty.hip", "token_logprobs.hip", "embedding.hip", "grad_norm.hip", "api.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-shared",
          # products are fused only where the code says fmaf: the online
          # accumulator relies on c(m) being the same rounded fp32 number

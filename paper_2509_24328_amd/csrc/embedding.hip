@@ -1,0 +1,324 @@
+// sv_embedding: scaled rows of a table.  sv_embedding_grad: the gradient of that table.
+//
+// The gradient sorts the tokens (least significant digit first, kDigitBits bits a pass, stable) and then
+// sums, for every row of the table, the rows of the token's positions in their order: no atomics
+// on the result, the same bits from every call.  Positions whose id is no row sort behind all others.
+#include "sv_device.hpp"
+#include "sv_host.hpp"
+
+namespace sv {
+
+constexpr int kChunkCols = 8;           // columns of one lane: 16 bytes of bfloat16, 32 of float32
+constexpr int kEmbThreads = 256;
+
+// Columns 8c .. 8c + 7 of a row of D; columns past D are 0 and are not written.
+template <int DT>
+__device__ __forceinline__ void load_chunk(const void* row, int D, int c, float (&f)[kChunkCols]) {
+  if ((c + 1) * kChunkCols <= D) {
+    if constexpr (DT == DT_F32) {
+      const u32x4 a = load_vec(row, 2 * c), b = load_vec(row, 2 * c + 1);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { f[j] = __uint_as_float(a[j]); f[4 + j] = __uint_as_float(b[j]); }
+    } else {
+      unpack<DT_BF16>(load_vec(row, c), f);
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < kChunkCols; ++j) f[j] = c * kChunkCols + j < D ? load_elem<DT>(row, c * kChunkCols + j) : 0.f;
+}
+template <int DT>
+__device__ __forceinline__ void store_chunk(void* row, int D, int c, const float (&f)[kChunkCols]) {
+  if constexpr (DT == DT_F32) {
+    if ((c + 1) * kChunkCols <= D) {
+      u32x4_row* p = reinterpret_cast<u32x4_row*>(row) + 2 * c;
+      p[0] = u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+      p[1] = u32x4{__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])};
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < kChunkCols; ++j)
+      if (c * kChunkCols + j < D) reinterpret_cast<float*>(row)[c * kChunkCols + j] = f[j];
+  } else {
+    const u32x4 q = {pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
+    if ((c + 1) * kChunkCols <= D) {
+      reinterpret_cast<u32x4_row*>(row)[c] = q;
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < kChunkCols; ++j)
+      if (c * kChunkCols + j < D)
+        reinterpret_cast<uint16_t*>(row)[c * kChunkCols + j] = (uint16_t)(q[j >> 1] >> (16 * (j & 1)));
+  }
+}
+
+// Lanes that share a row: a power of two, so that a workgroup holds a whole number of rows.
+inline int lanes_per_row(int D) {
+  const int chunks = (D + kChunkCols - 1) / kChunkCols;
+  int lanes = 1;
+  while (lanes < chunks && lanes < kEmbThreads) lanes *= 2;
+  return lanes;
+}
+
+template <int DT>
+__global__ __launch_bounds__(kEmbThreads) void embedding_kernel(const void* table, const int32_t* ids, int n, int V,
+                                                                int D, float scale, void* out, uint32_t* flags,
+                                                                int lanes) {
+  const long long i = (long long)blockIdx.x * (kEmbThreads / lanes) + threadIdx.x / lanes;
+  if (i >= n) return;
+  const int id = ids[i], l = threadIdx.x % lanes;
+  const bool given = id >= 0 && id < V;
+  const char* from = static_cast<const char*>(table) + (given ? (size_t)id * D * Elem<DT>::bytes : 0);
+  char* to = static_cast<char*>(out) + (size_t)i * D * Elem<DT>::bytes;
+  if (flags && l == 0) flags[i] = given || id == -1 ? 0 : SV_FLAG_BAD_TOKEN;
+  for (int c = l; c * kChunkCols < D; c += lanes) {
+    float f[kChunkCols] = {};
+    if (given) load_chunk<DT>(from, D, c, f);
+#pragma unroll
+    for (int j = 0; j < kChunkCols; ++j) f[j] = given ? f[j] * scale : 0.f;
+    store_chunk<DT>(to, D, c, f);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// stable sort of (token, position) by token
+// ---------------------------------------------------------------------------
+constexpr int kSortThreads = 1024, kSortPerLane = 4, kSortTile = kSortThreads * kSortPerLane;
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
+constexpr int kSortWaves = kSortThreads / kWave;
+
+struct SortPass {
+  const int32_t* ids;          // first pass: the tokens as given
+  const uint32_t* key_in;      // later ones
+  const int32_t* pos_in;
+  uint32_t* key_out;
+  int32_t* pos_out;
+  int32_t* hist;               // [tiles, kDigits]
+  int n, V, shift;
+};
+
+__device__ __forceinline__ uint32_t sort_key(const SortPass& p, int i) {
+  if (!p.ids) return p.key_in[i];
+  const int id = p.ids[i];
+  return id >= 0 && id < p.V ? (uint32_t)id : (uint32_t)p.V;
+}
+
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortPass p) {
+  __shared__ int count[kDigits];
+  const int tid = threadIdx.x;
+  if (tid < kDigits) count[tid] = 0;
+  __syncthreads();
+  const int base = blockIdx.x * kSortTile;
+#pragma unroll
+  for (int j = 0; j < kSortPerLane; ++j) {
+    const int i = base + j * kSortThreads + tid;
+    if (i < p.n) atomicAdd(&count[(sort_key(p, i) >> p.shift) & (kDigits - 1)], 1);
+  }
+  __syncthreads();
+  if (tid < kDigits) p.hist[(size_t)blockIdx.x * kDigits + tid] = count[tid];
+}
+
+// A wavefront owns kSortPerLane * 64 consecutive entries of the tile.
+__global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortPass p, int tiles) {
+  __shared__ int count[kSortWaves][kDigits];
+  __shared__ int wave_sum[kSortWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int i = tid; i < kSortWaves * kDigits; i += kSortThreads) (&count[0][0])[i] = 0;
+  __syncthreads();
+  const int base = blockIdx.x * kSortTile + wave * kSortPerLane * kWave;
+  uint32_t key[kSortPerLane];
+  int pos[kSortPerLane], rank[kSortPerLane];
+#pragma unroll
+  for (int j = 0; j < kSortPerLane; ++j) {
+    const int i = base + j * kWave + lane;
+    key[j] = i < p.n ? sort_key(p, i) : 0;
+    pos[j] = i < p.n ? (p.ids ? i : p.pos_in[i]) : 0;
+  }
+  volatile int* mine = count[wave];
+#pragma unroll
+  for (int j = 0; j < kSortPerLane; ++j) {
+    const bool on = base + j * kWave + lane < p.n;
+    const int d = (key[j] >> p.shift) & (kDigits - 1);
+    uint64_t same = __ballot(on);
+#pragma unroll
+    for (int b = 0; b < kDigitBits; ++b) {
+      const uint64_t set = __ballot((d >> b) & 1);
+      same &= (d >> b) & 1 ? set : ~set;
+    }
+    const int below = __popcll(same & ((1ull << lane) - 1));
+    const int before = mine[d];
+    rank[j] = before + below;
+    __builtin_amdgcn_wave_barrier();                   // (every lane has read before one of them writes)
+    if (on && below == 0) mine[d] = before + __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+  }
+  __syncthreads();
+  // where a digit's entries of this tile start, and each wavefront's within them
+  int before = 0, total = 0, own = 0;
+  if (tid < kDigits) {
+    for (int t = 0; t < tiles; ++t) {
+      const int c = p.hist[(size_t)t * kDigits + tid];
+      before += t < (int)blockIdx.x ? c : 0;
+      total += c;
+    }
+  }
+  const int scan = wave_scan_i32(total);
+  if (lane == kWave - 1) wave_sum[wave] = scan;
+  __syncthreads();
+  int start = scan - total;
+  for (int w = 0; w < wave; ++w) start += wave_sum[w];
+  if (tid < kDigits) {
+    own = start + before;
+    for (int w = 0; w < kSortWaves; ++w) {
+      const int c = count[w][tid];
+      count[w][tid] = own;
+      own += c;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kSortPerLane; ++j) {
+    if (base + j * kWave + lane >= p.n) continue;
+    const int to = count[wave][(key[j] >> p.shift) & (kDigits - 1)] + rank[j];
+    p.key_out[to] = key[j];
+    p.pos_out[to] = pos[j];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// sums
+// ---------------------------------------------------------------------------
+constexpr int kRowsPerGroup = 16;       // rows of the table of one workgroup
+
+struct GradRows {
+  const void* g;
+  void* table;
+  const uint32_t* key;                  // sorted tokens
+  const int32_t* pos;                   // their positions
+  int n, V, D, lanes, accumulate;
+  float scale;
+};
+
+template <int DTG, int DTW>
+__global__ __launch_bounds__(kEmbThreads) void embedding_grad_kernel(const GradRows a) {
+  __shared__ int start[kRowsPerGroup + 1];
+  const int v0 = blockIdx.x * kRowsPerGroup;
+  if (threadIdx.x <= kRowsPerGroup) {                  // first sorted position of a token at least v0 + lane
+    const uint32_t v = (uint32_t)min(v0 + (int)threadIdx.x, a.V);
+    int lo = 0, hi = a.n;
+    while (lo < hi) {
+      const int mid = lo + (hi - lo) / 2;
+      if (a.key[mid] < v) lo = mid + 1; else hi = mid;
+    }
+    start[threadIdx.x] = lo;
+  }
+  __syncthreads();
+  const int groups = kEmbThreads / a.lanes, l = threadIdx.x % a.lanes;
+  for (int r = threadIdx.x / a.lanes; r < kRowsPerGroup && v0 + r < a.V; r += groups) {
+    const int lo = start[r], hi = start[r + 1];
+    if (lo == hi && a.accumulate) continue;
+    char* to = static_cast<char*>(a.table) + (size_t)(v0 + r) * a.D * Elem<DTW>::bytes;
+    for (int c = l; c * kChunkCols < a.D; c += a.lanes) {
+      float sum[kChunkCols] = {};
+      for (int i = lo; i < hi; ++i) {
+        float f[kChunkCols];
+        load_chunk<DTG>(static_cast<const char*>(a.g) + (size_t)a.pos[i] * a.D * Elem<DTG>::bytes, a.D, c, f);
+#pragma unroll
+        for (int j = 0; j < kChunkCols; ++j) sum[j] += f[j];
+      }
+      float old[kChunkCols] = {};
+      if (a.accumulate) load_chunk<DTW>(to, a.D, c, old);
+#pragma unroll
+      for (int j = 0; j < kChunkCols; ++j) sum[j] = __builtin_fmaf(sum[j], a.scale, old[j]);
+      store_chunk<DTW>(to, a.D, c, sum);
+    }
+  }
+}
+
+struct EmbeddingWs {
+  uint32_t* key[2];
+  int32_t* pos[2];
+  int32_t* hist;
+  size_t bytes;
+};
+inline int sort_tiles(int n) { return (n + kSortTile - 1) / kSortTile; }
+inline EmbeddingWs carve_embedding_ws(void* base, int n) {
+  EmbeddingWs w;
+  char* p = static_cast<char*>(base);
+  size_t off = 0;
+  auto take = [&](size_t bytes) { char* q = p ? p + off : nullptr; off += ws_round(bytes); return q; };
+  for (int i = 0; i < 2; ++i) {
+    w.key[i] = reinterpret_cast<uint32_t*>(take((size_t)n * 4));
+    w.pos[i] = reinterpret_cast<int32_t*>(take((size_t)n * 4));
+  }
+  w.hist = reinterpret_cast<int32_t*>(take((size_t)sort_tiles(n) * kDigits * 4));
+  w.bytes = off;
+  return w;
+}
+
+template <int DTG>
+void launch_grad_rows(const GradRows& a, int table_dtype, hipStream_t st) {
+  const dim3 grid((unsigned)((a.V + kRowsPerGroup - 1) / kRowsPerGroup)), block(kEmbThreads);
+  if (table_dtype == SV_F32) hipLaunchKernelGGL((embedding_grad_kernel<DTG, DT_F32>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((embedding_grad_kernel<DTG, DT_BF16>), grid, block, 0, st, a);
+}
+
+}  // namespace sv
+
+extern "C" int sv_embedding(const void* table, const int32_t* ids, int n, int V, int D, int dtype, float scale,
+                            void* out, uint32_t* flags_or_null, sv_stream_t stream) {
+  using namespace sv;
+  SV_REQUIRE(dtype == SV_F32 || dtype == SV_BF16, SV_ERR_DTYPE);
+  SV_REQUIRE(n >= 0 && V >= 1 && D >= 1, SV_ERR_INVALID_ARG);
+  SV_REQUIRE(V <= (1 << 24) && D <= (1 << 24), SV_ERR_TOO_LARGE);
+  if (n == 0) return SV_OK;
+  SV_REQUIRE(table && ids && out, SV_ERR_NULL);
+  SV_REQUIRE(is_aligned(table, elem_bytes(dtype)) && is_aligned(out, elem_bytes(dtype)) && is_aligned(ids, 4) &&
+                 is_aligned(flags_or_null, 4),
+             SV_ERR_ALIGN);
+  const int lanes = lanes_per_row(D), rows = kEmbThreads / lanes;
+  const dim3 grid((unsigned)(((long long)n + rows - 1) / rows)), block(kEmbThreads);
+  hipStream_t st = as_stream(stream);
+  if (dtype == SV_F32)
+    hipLaunchKernelGGL(embedding_kernel<DT_F32>, grid, block, 0, st, table, ids, n, V, D, scale, out, flags_or_null, lanes);
+  else
+    hipLaunchKernelGGL(embedding_kernel<DT_BF16>, grid, block, 0, st, table, ids, n, V, D, scale, out, flags_or_null, lanes);
+  return launch_status();
+}
+
+extern "C" size_t sv_embedding_grad_workspace_bytes(int n, int V, int D) {
+  if (n < 0 || n > SV_EMBEDDING_MAX_TOKENS || V < 1 || V > (1 << 24) || D < 1 || D > (1 << 24)) return 0;
+  const size_t need = sv::carve_embedding_ws(nullptr, n).bytes;
+  return need < sv::kWsAlign ? sv::kWsAlign : need;
+}
+
+extern "C" int sv_embedding_grad(const void* grad_out, int dtype, const int32_t* ids, int n, int V, int D, float scale,
+                                 void* grad_table, int table_dtype, int accumulate, void* ws, size_t ws_bytes,
+                                 sv_stream_t stream) {
+  using namespace sv;
+  SV_REQUIRE((dtype == SV_F32 || dtype == SV_BF16) && (table_dtype == SV_F32 || table_dtype == SV_BF16), SV_ERR_DTYPE);
+  SV_REQUIRE(n >= 0 && V >= 1 && D >= 1, SV_ERR_INVALID_ARG);
+  SV_REQUIRE(n <= SV_EMBEDDING_MAX_TOKENS && V <= (1 << 24) && D <= (1 << 24), SV_ERR_TOO_LARGE);
+  if (n == 0 && accumulate) return SV_OK;
+  SV_REQUIRE(grad_table && (n == 0 || (grad_out && ids)), SV_ERR_NULL);
+  SV_REQUIRE(is_aligned(grad_out, elem_bytes(dtype)) && is_aligned(grad_table, elem_bytes(table_dtype)) &&
+                 is_aligned(ids, 4),
+             SV_ERR_ALIGN);
+  SV_REQUIRE(ws && is_aligned(ws, kWsAlign) && ws_bytes >= sv_embedding_grad_workspace_bytes(n, V, D), SV_ERR_WORKSPACE);
+  hipStream_t st = as_stream(stream);
+  const EmbeddingWs w = carve_embedding_ws(ws, n);
+  int bits = 1;
+  while ((V >> bits) != 0) ++bits;                       // keys 0 .. V
+  int at = 0;
+  for (int shift = 0; n > 0 && shift < bits; shift += kDigitBits) {
+    SortPass p = {shift == 0 ? ids : nullptr, w.key[at], w.pos[at], w.key[1 - at], w.pos[1 - at], w.hist, n, V, shift};
+    const dim3 grid((unsigned)sort_tiles(n)), block(kSortThreads);
+    hipLaunchKernelGGL(sort_count_kernel, grid, block, 0, st, p);
+    hipLaunchKernelGGL(sort_scatter_kernel, grid, block, 0, st, p, sort_tiles(n));
+    at = 1 - at;
+  }
+  const GradRows a = {grad_out, grad_table, w.key[at], w.pos[at], n, V, D, lanes_per_row(D), accumulate != 0, scale};
+  if (dtype == SV_F32) launch_grad_rows<DT_F32>(a, table_dtype, st);
+  else launch_grad_rows<DT_BF16>(a, table_dtype, st);
+  return launch_status();
+}

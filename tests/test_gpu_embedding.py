@@ -1,0 +1,202 @@
+"""sv_embedding and sv_embedding_grad against the fp64 definitions.
+
+The lookup is one float32 product, rounded once: compared bit for bit.  The gradient's sum of c rows has at most
+c + 1 roundings of 2^-24 against the sum of absolute values (times the scale's), then the result's own, to float32 or to bfloat16."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2509_24328_amd as P
+from oracle import operators_oracle as O
+from paper_2509_24328_amd import binding as Bd
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def bits(t):
+    t = t.detach().cpu().contiguous()
+    return t.view(torch.int16).numpy().view(np.uint16) if t.dtype == BF16 else t.numpy()
+
+
+def tokens(n, V, seed, kind="zipf"):
+    g = torch.Generator().manual_seed(seed)
+    if kind == "one":
+        t = torch.full((n,), V - 1)
+    elif kind == "uniform":
+        t = torch.randint(0, V, (n,), generator=g)
+    elif kind == "runs":                                # tokens whose counts lie about powers of two
+        t = torch.repeat_interleave(torch.arange(V), torch.randint(1, 140, (V,), generator=g))[:n]
+        t = torch.cat([t, torch.zeros(n - len(t), dtype=t.dtype)])[torch.randperm(n, generator=g)]
+    else:
+        t = (torch.exp(torch.rand(n, generator=g, dtype=torch.float64) * np.log(V + 1)) - 1).long().clamp(0, V - 1)
+    t = t.to(torch.int32)
+    if n > 4:
+        t[n // 2], t[n // 3], t[n // 4] = -1, V, -5
+    return t
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D", [1, 7, 8, 64, 100, 257, 896, 2048, 4099])
+@pytest.mark.parametrize("n", [1, 9, 300])
+def test_lookup(dtype, D, n):
+    V = 501
+    w = torch.randn((V, D), generator=torch.Generator().manual_seed(D)).to(dtype)
+    w[3, 0], w[4, D - 1] = float("inf"), float("nan")
+    ids = tokens(n, V, n)
+    ids[0] = 4
+    scale = float(np.float32(np.sqrt(D)))
+    out = torch.full((n, D), 9.0, dtype=dtype, device="cuda")
+    flags = torch.full((n,), 9, dtype=torch.int32, device="cuda")
+    P.sv_embedding(w.cuda(), ids.cuda(), out, scale, flags)
+    want = torch.zeros((n, D))
+    ok = (ids >= 0) & (ids < V)
+    want[ok] = w[ids[ok].long()].float() * scale
+    assert np.array_equal(O.values(bits(out)), O.values(bits(want.to(dtype))), equal_nan=True)
+    assert np.array_equal(flags.cpu().numpy(), np.where(ok | (ids == -1), 0, 16))
+
+
+def test_lookup_beyond_32_bits():
+    V, D = 1100000, 4096                                # 4.5e9 elements
+    if torch.cuda.mem_get_info()[0] < 12 << 30:
+        pytest.skip("needs 12 GB")
+    w = torch.empty((V, D), dtype=BF16, device="cuda")
+    ids = torch.tensor([0, V - 1, 524288, 1048577], dtype=torch.int32, device="cuda")
+    rows = torch.randn((4, D), generator=torch.Generator().manual_seed(1)).to(BF16).cuda()
+    w[ids.long()] = rows
+    out = torch.empty((4, D), dtype=BF16, device="cuda")
+    P.sv_embedding(w, ids, out)
+    assert torch.equal(out, rows)
+    ws = torch.empty(P.sv_embedding_grad_workspace_bytes(4, V, D), dtype=torch.uint8, device="cuda")
+    P.sv_embedding_grad(rows, ids, w, ws=ws)
+    assert torch.equal(w[ids.long()], rows)
+    assert not w[V - 2].any() and not w[1].any() and not w[524289].any()
+
+
+def check_grad(n, V, D, dtype, out_dtype, kind, accumulate=False, seed=0, scale=1.5):
+    gen = torch.Generator().manual_seed(seed + n + D)
+    g = torch.randn((n, D), generator=gen).to(dtype)
+    ids = tokens(n, V, seed + V, kind)
+    old = torch.randn((V, D), generator=gen).to(out_dtype)
+    table = old.cuda() if accumulate else torch.full((V, D), 7.0, dtype=out_dtype, device="cuda")
+    ws = torch.empty(P.sv_embedding_grad_workspace_bytes(n, V, D), dtype=torch.uint8, device="cuda").fill_(255)
+    P.sv_embedding_grad(g.cuda(), ids.cuda(), table, scale, accumulate, ws)
+    s, a, c = O.embedding_grad(bits(g), ids.numpy(), V, scale, O.values(bits(old)) if accumulate else None)
+    got = O.values(bits(table))
+    tol = (c + 2)[:, None] * 2.0 ** -24 * a + 2.0 ** -24 * np.abs(s) + 1e-38
+    assert O.within(got, s, tol, out_dtype == BF16).all()
+    if accumulate:
+        assert np.array_equal(bits(table)[c == 0], bits(old)[c == 0])
+    else:
+        assert not got[c == 0].any()
+    return table
+
+
+@pytest.mark.parametrize("dtype, out_dtype", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)])
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("n, V, D", [(1, 5, 3), (37, 1, 8), (300, 501, 64), (1024, 700, 100), (1025, 700, 100),
+                                     (5000, 3001, 257), (12289, 300, 40)])
+def test_gradient(dtype, out_dtype, accumulate, n, V, D):
+    check_grad(n, V, D, dtype, out_dtype, "zipf", accumulate)
+
+
+@pytest.mark.parametrize("kind", ["one", "uniform", "runs"])
+@pytest.mark.parametrize("n", [2, 63, 64, 65, 129, 1000, 4097, 20000])
+def test_gradient_counts(kind, n):
+    for dtype, D in ((BF16, 72), (F32, 9)):
+        check_grad(n, 333, D, dtype, F32, kind)
+
+
+@pytest.mark.parametrize("V", [511, 512, 513, 262143, 262144, 300000])
+def test_gradient_digits(V):
+    """Numbers of tokens about the powers of two of a sort's digits."""
+    for n in (100, 3000):
+        check_grad(n, V, 8, BF16, F32, "uniform")
+
+
+def test_gradient_wide_rows():
+    check_grad(700, 50, 4099, BF16, BF16, "zipf")
+    check_grad(2000, 50, 2504, F32, F32, "zipf")
+
+
+def test_the_same_bits_every_time():
+    a = [check_grad(20000, 100, 64, BF16, F32, "zipf") for _ in range(3)]
+    assert torch.equal(a[0], a[1]) and torch.equal(a[0], a[2])
+
+
+def test_no_tokens_and_other_values():
+    table = torch.full((11, 5), 7.0, device="cuda")
+    ids = torch.zeros(0, dtype=torch.int32, device="cuda")
+    ws = torch.empty(P.sv_embedding_grad_workspace_bytes(0, 11, 5), dtype=torch.uint8, device="cuda")
+    P.sv_embedding_grad(torch.zeros((0, 5), device="cuda"), ids, table, accumulate=True, ws=ws)
+    assert (table == 7.0).all()
+    P.sv_embedding_grad(torch.zeros((0, 5), device="cuda"), ids, table, ws=ws)
+    assert not table.any()
+    P.sv_embedding(table, ids, torch.zeros((0, 5), device="cuda"))
+    # every token is padding; a NaN in a padded row goes nowhere
+    ids = torch.full((70,), -1, dtype=torch.int32, device="cuda")
+    g = torch.full((70, 5), float("nan"), device="cuda")
+    ws = torch.empty(P.sv_embedding_grad_workspace_bytes(70, 11, 5), dtype=torch.uint8, device="cuda")
+    table.fill_(3.0)
+    P.sv_embedding_grad(g, ids, table, ws=ws)
+    assert not table.any()
+
+
+def test_other_streams_and_graphs():
+    n, V, D = 3000, 900, 48
+    gen = torch.Generator().manual_seed(5)
+    g = torch.randn((n, D), generator=gen).cuda()
+    ids = tokens(n, V, 5).cuda()
+    w = torch.randn((V, D), generator=gen).cuda()
+    ws = torch.empty(P.sv_embedding_grad_workspace_bytes(n, V, D), dtype=torch.uint8, device="cuda")
+    out, table = torch.empty((n, D), device="cuda"), torch.empty((V, D), device="cuda")
+
+    def call(s=None):
+        P.sv_embedding(w, ids, out, 2.0, stream=s)
+        P.sv_embedding_grad(g, ids, table, 2.0, ws=ws, stream=s)
+
+    call()
+    want = out.clone(), table.clone()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    out.zero_(), table.zero_()
+    torch.cuda.synchronize()
+    call(side)
+    side.synchronize()
+    assert torch.equal(out, want[0]) and torch.equal(table, want[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for k in range(3):
+        ids.copy_(tokens(n, V, 50 + k).cuda())
+        call()
+        want = out.clone(), table.clone()
+        out.fill_(1), table.fill_(1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(table, want[1])
+
+
+def test_refusals():
+    w = torch.zeros((4, 8), device="cuda")
+    ids = torch.zeros(2, dtype=torch.int32, device="cuda")
+    out = torch.zeros((2, 8), device="cuda")
+    ws = torch.empty(P.sv_embedding_grad_workspace_bytes(2, 4, 8), dtype=torch.uint8, device="cuda")
+    cases = [
+        (Bd.SV_ERR_DTYPE, lambda: P.sv_embedding(w.half(), ids, out.half())),
+        (Bd.SV_ERR_DTYPE, lambda: P.sv_embedding(w, ids.long(), out)),
+        (Bd.SV_ERR_INVALID_ARG, lambda: P.sv_embedding(w, ids, out.bfloat16())),
+        (Bd.SV_ERR_INVALID_ARG, lambda: P.sv_embedding(w, ids, out[:1])),
+        (Bd.SV_ERR_INVALID_ARG, lambda: P.sv_embedding_grad(out[:1], ids, w, ws=ws)),
+        (Bd.SV_ERR_WORKSPACE, lambda: P.sv_embedding_grad(out, ids, w)),
+        (Bd.SV_ERR_WORKSPACE, lambda: P.sv_embedding_grad(out, ids, w, ws=ws[:100])),
+        (Bd.SV_ERR_DTYPE, lambda: P.sv_embedding_grad(out.half(), ids, w, ws=ws)),
+    ]
+    for code, call in cases:
+        with pytest.raises(P.SvError) as e:
+            call()
+        assert e.value.status == code
+    with pytest.raises(ValueError):
+        P.sv_embedding(w.cpu(), ids, out)
+    assert P.sv_embedding_grad_workspace_bytes(-1, 4, 8) == 0
+    assert P.sv_embedding_grad_workspace_bytes(1 << 25, 4, 8) == 0
