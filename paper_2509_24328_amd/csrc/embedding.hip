@@ -189,48 +189,189 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortPa
 // sums
 // ---------------------------------------------------------------------------
 constexpr int kRowsPerGroup = 16;       // rows of the table of one workgroup
+constexpr int kPiece = 64;              // sorted positions summed by one group of lanes; a token with more is joined from pieces
+constexpr int kDirectTokens = 1024;     // up to here every workgroup looks through all tokens itself
 
 struct GradRows {
   const void* g;
   void* table;
+  const int32_t* ids;                   // direct form: the tokens as given
   const uint32_t* key;                  // sorted tokens
   const int32_t* pos;                   // their positions
+  int32_t *first, *last;                // [V] range of a token's sorted positions; of tokens that occur
+  float* part;                          // [pieces, 2, D] sums of a piece over a token that began before it / goes on after it
   int n, V, D, lanes, accumulate;
   float scale;
 };
 
+// sum += the rows of positions at(lo) .. at(hi - 1), in this order; kAhead of them are under way at a time.
+template <int DT, class At>
+__device__ __forceinline__ void add_rows(const GradRows& a, int c, int lo, int hi, At&& at, float (&sum)[kChunkCols]) {
+  constexpr int kAhead = 4;
+  const char* g = static_cast<const char*>(a.g);
+  const size_t bytes = (size_t)a.D * Elem<DT>::bytes;
+  int i = lo;
+  for (; i + kAhead <= hi; i += kAhead) {
+    float f[kAhead][kChunkCols];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) load_chunk<DT>(g + at(i + u) * bytes, a.D, c, f[u]);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int j = 0; j < kChunkCols; ++j) sum[j] += f[u][j];
+  }
+  for (; i < hi; ++i) {
+    float f[kChunkCols];
+    load_chunk<DT>(g + at(i) * bytes, a.D, c, f);
+#pragma unroll
+    for (int j = 0; j < kChunkCols; ++j) sum[j] += f[j];
+  }
+}
+
+template <int DTW>
+__device__ __forceinline__ void store_sum(const GradRows& a, int v, int c, float (&sum)[kChunkCols]) {
+  char* to = static_cast<char*>(a.table) + (size_t)v * a.D * Elem<DTW>::bytes;
+  float old[kChunkCols] = {};
+  if (a.accumulate) load_chunk<DTW>(to, a.D, c, old);
+#pragma unroll
+  for (int j = 0; j < kChunkCols; ++j) sum[j] = __builtin_fmaf(sum[j], a.scale, old[j]);
+  store_chunk<DTW>(to, a.D, c, sum);
+}
+
+// Few tokens: one launch.  A workgroup of kRowsPerGroup rows picks the tokens of its rows out of all, in order.
 template <int DTG, int DTW>
-__global__ __launch_bounds__(kEmbThreads) void embedding_grad_kernel(const GradRows a) {
-  __shared__ int start[kRowsPerGroup + 1];
-  const int v0 = blockIdx.x * kRowsPerGroup;
-  if (threadIdx.x <= kRowsPerGroup) {                  // first sorted position of a token at least v0 + lane
-    const uint32_t v = (uint32_t)min(v0 + (int)threadIdx.x, a.V);
-    int lo = 0, hi = a.n;
-    while (lo < hi) {
-      const int mid = lo + (hi - lo) / 2;
-      if (a.key[mid] < v) lo = mid + 1; else hi = mid;
-    }
-    start[threadIdx.x] = lo;
+__global__ __launch_bounds__(kEmbThreads) void embedding_grad_direct_kernel(const GradRows a) {
+  constexpr int kWaves = kEmbThreads / kWave;
+  __shared__ uint32_t found[kDirectTokens];            // row of the workgroup << 16 | position, by position
+  __shared__ uint16_t pos[kDirectTokens];              // positions by row, then by position
+  __shared__ int count[kWaves], start[kRowsPerGroup + 1];
+  const int v0 = blockIdx.x * kRowsPerGroup, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t below = (1ull << lane) - 1;
+  // a wavefront looks through a run of tokens
+  constexpr int kRounds = kDirectTokens / kEmbThreads;
+  uint64_t hit[kRounds];
+  int row[kRounds], mine = 0;
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const int i = (wave * kRounds + r) * kWave + lane;
+    const int id = i < a.n ? max(a.ids[i], -1) : -1;
+    row[r] = id - v0;
+    hit[r] = __ballot(id >= v0 && row[r] < kRowsPerGroup && id < a.V);
+    mine += __popcll(hit[r]);
+  }
+  if (lane == 0) count[wave] = mine;
+  __syncthreads();
+  int to = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    to += w < wave ? count[w] : 0;
+    total += count[w];
+  }
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    if (hit[r] >> lane & 1)
+      found[to + __popcll(hit[r] & below)] = (uint32_t)row[r] << 16 | ((wave * kRounds + r) * kWave + lane);
+    to += __popcll(hit[r]);
   }
   __syncthreads();
-  const int groups = kEmbThreads / a.lanes, l = threadIdx.x % a.lanes;
-  for (int r = threadIdx.x / a.lanes; r < kRowsPerGroup && v0 + r < a.V; r += groups) {
+  for (int r = wave; r < kRowsPerGroup; r += kWaves) {  // tokens of the rows before r, and those of r in order
+    int before = 0;
+    for (int i0 = 0; i0 < total; i0 += kWave)
+      before += __popcll(__ballot(i0 + lane < total && (int)(found[min(i0 + lane, total - 1)] >> 16) < r));
+    if (lane == 0) start[r] = before;
+    for (int i0 = 0; i0 < total; i0 += kWave) {
+      const uint32_t f = found[min(i0 + lane, total - 1)];
+      const uint64_t here = __ballot(i0 + lane < total && (int)(f >> 16) == r);
+      if (here >> lane & 1) pos[before + __popcll(here & below)] = (uint16_t)f;
+      before += __popcll(here);
+    }
+  }
+  if (threadIdx.x == 0) start[kRowsPerGroup] = total;
+  __syncthreads();
+  const int l = threadIdx.x % a.lanes;
+  for (int r = threadIdx.x / a.lanes; r < kRowsPerGroup && v0 + r < a.V; r += kEmbThreads / a.lanes) {
     const int lo = start[r], hi = start[r + 1];
     if (lo == hi && a.accumulate) continue;
-    char* to = static_cast<char*>(a.table) + (size_t)(v0 + r) * a.D * Elem<DTW>::bytes;
     for (int c = l; c * kChunkCols < a.D; c += a.lanes) {
       float sum[kChunkCols] = {};
-      for (int i = lo; i < hi; ++i) {
-        float f[kChunkCols];
-        load_chunk<DTG>(static_cast<const char*>(a.g) + (size_t)a.pos[i] * a.D * Elem<DTG>::bytes, a.D, c, f);
-#pragma unroll
-        for (int j = 0; j < kChunkCols; ++j) sum[j] += f[j];
+      add_rows<DTG>(a, c, lo, hi, [&](int i) { return (size_t)pos[i]; }, sum);
+      store_sum<DTW>(a, v0 + r, c, sum);
+    }
+  }
+}
+
+// Many tokens, first launch: where the tokens' sorted positions begin and end, and the sums of pieces of those
+// that have more than kPiece.  Such a token is in a piece from its first position on, or up to its last.
+template <int DTG>
+__global__ __launch_bounds__(kEmbThreads) void embedding_grad_pieces_kernel(const GradRows a) {
+  const int pieces = kEmbThreads / a.lanes;            // of the workgroup
+  const long long base = (long long)blockIdx.x * pieces * kPiece;
+  for (int j = threadIdx.x; j < pieces * kPiece; j += kEmbThreads) {
+    const long long i = base + j;
+    if (i >= a.n) break;
+    const uint32_t k = a.key[i];
+    if (k >= (uint32_t)a.V) continue;
+    if (i == 0 || a.key[i - 1] != k) a.first[k] = (int)i;
+    if (i == a.n - 1 || a.key[i + 1] != k) a.last[k] = (int)i + 1;
+  }
+  const int l = threadIdx.x % a.lanes;
+  const long long piece = (long long)blockIdx.x * pieces + threadIdx.x / a.lanes;
+  if (piece * kPiece >= a.n) return;
+  const int lo = (int)(piece * kPiece), hi = min(lo + kPiece, a.n);
+  auto sum_piece = [&](int from, int to, int slot) {
+    for (int c = l; c * kChunkCols < a.D; c += a.lanes) {
+      float sum[kChunkCols] = {};
+      add_rows<DTG>(a, c, from, to, [&](int i) { return (size_t)a.pos[i]; }, sum);
+      store_chunk<DT_F32>(a.part + ((size_t)piece * 2 + slot) * a.D, a.D, c, sum);
+    }
+  };
+  auto search = [&](uint32_t k, bool after) {          // first position of the piece with a key at least / above k
+    int x = lo, y = hi;
+    while (x < y) {
+      const int mid = (x + y) / 2;
+      if (a.key[mid] < k || (after && a.key[mid] == k)) x = mid + 1; else y = mid;
+    }
+    return x;
+  };
+  const uint32_t k0 = a.key[lo], k1 = a.key[hi - 1];
+  const int end = search(k0, true);
+  // more than kPiece of k0: kPiece positions before its last one here is another, or it goes on after a whole piece
+  const bool long0 = (end - 1 >= kPiece && a.key[end - 1 - kPiece] == k0) || (end - lo == kPiece && hi < a.n && a.key[hi] == k0);
+  if (k0 < (uint32_t)a.V && long0) sum_piece(lo, end, 0);
+  if (end == hi || k1 >= (uint32_t)a.V) return;
+  const int from = search(k1, false);
+  if (from + kPiece < a.n && a.key[from + kPiece] == k1) sum_piece(from, hi, 1);
+}
+
+// Second launch: every row of the table.
+template <int DTG, int DTW>
+__global__ __launch_bounds__(kEmbThreads) void embedding_grad_rows_kernel(const GradRows a) {
+  __shared__ int start[kRowsPerGroup], end[kRowsPerGroup];
+  const int v0 = blockIdx.x * kRowsPerGroup;
+  if (threadIdx.x < kRowsPerGroup) {
+    // what the arrays hold for a token that does not occur is from elsewhere: no sorted position has that token
+    const int v = v0 + threadIdx.x;
+    const int lo = v < a.V ? a.first[v] : -1;
+    const bool occurs = lo >= 0 && lo < a.n && a.key[lo] == (uint32_t)v;
+    start[threadIdx.x] = occurs ? lo : 0;
+    end[threadIdx.x] = occurs ? a.last[v] : 0;
+  }
+  __syncthreads();
+  const int l = threadIdx.x % a.lanes;
+  for (int r = threadIdx.x / a.lanes; r < kRowsPerGroup && v0 + r < a.V; r += kEmbThreads / a.lanes) {
+    const int lo = start[r], hi = end[r];
+    if (lo == hi && a.accumulate) continue;
+    for (int c = l; c * kChunkCols < a.D; c += a.lanes) {
+      float sum[kChunkCols] = {};
+      if (hi - lo <= kPiece) {
+        add_rows<DTG>(a, c, lo, hi, [&](int i) { return (size_t)a.pos[i]; }, sum);
+      } else {
+        const GradRows parts = {a.part, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0, a.D, 0, 0, 0.f};
+        const int p0 = lo / kPiece, slot0 = lo % kPiece != 0;
+        add_rows<DT_F32>(parts, c, p0, (hi - 1) / kPiece + 1, [&](int p) { return (size_t)p * 2 + (p == p0 ? slot0 : 0); },
+                         sum);
       }
-      float old[kChunkCols] = {};
-      if (a.accumulate) load_chunk<DTW>(to, a.D, c, old);
-#pragma unroll
-      for (int j = 0; j < kChunkCols; ++j) sum[j] = __builtin_fmaf(sum[j], a.scale, old[j]);
-      store_chunk<DTW>(to, a.D, c, sum);
+      store_sum<DTW>(a, v0 + r, c, sum);
     }
   }
 }
@@ -239,11 +380,14 @@ struct EmbeddingWs {
   uint32_t* key[2];
   int32_t* pos[2];
   int32_t* hist;
+  int32_t *first, *last;
+  float* part;
   size_t bytes;
 };
 inline int sort_tiles(int n) { return (n + kSortTile - 1) / kSortTile; }
-inline EmbeddingWs carve_embedding_ws(void* base, int n) {
-  EmbeddingWs w;
+inline EmbeddingWs carve_embedding_ws(void* base, int n, int V, int D) {
+  EmbeddingWs w = {};
+  if (n <= kDirectTokens) return w;
   char* p = static_cast<char*>(base);
   size_t off = 0;
   auto take = [&](size_t bytes) { char* q = p ? p + off : nullptr; off += ws_round(bytes); return q; };
@@ -252,6 +396,9 @@ inline EmbeddingWs carve_embedding_ws(void* base, int n) {
     w.pos[i] = reinterpret_cast<int32_t*>(take((size_t)n * 4));
   }
   w.hist = reinterpret_cast<int32_t*>(take((size_t)sort_tiles(n) * kDigits * 4));
+  w.first = reinterpret_cast<int32_t*>(take((size_t)V * 4));
+  w.last = reinterpret_cast<int32_t*>(take((size_t)V * 4));
+  w.part = reinterpret_cast<float*>(take((size_t)((n + kPiece - 1) / kPiece) * 2 * D * 4));
   w.bytes = off;
   return w;
 }
@@ -259,8 +406,15 @@ inline EmbeddingWs carve_embedding_ws(void* base, int n) {
 template <int DTG>
 void launch_grad_rows(const GradRows& a, int table_dtype, hipStream_t st) {
   const dim3 grid((unsigned)((a.V + kRowsPerGroup - 1) / kRowsPerGroup)), block(kEmbThreads);
-  if (table_dtype == SV_F32) hipLaunchKernelGGL((embedding_grad_kernel<DTG, DT_F32>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((embedding_grad_kernel<DTG, DT_BF16>), grid, block, 0, st, a);
+  if (!a.key) {                                          // (of no tokens at all the list may be NULL as well)
+    if (table_dtype == SV_F32) hipLaunchKernelGGL((embedding_grad_direct_kernel<DTG, DT_F32>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((embedding_grad_direct_kernel<DTG, DT_BF16>), grid, block, 0, st, a);
+    return;
+  }
+  const int per = kEmbThreads / a.lanes * kPiece;
+  hipLaunchKernelGGL(embedding_grad_pieces_kernel<DTG>, dim3((unsigned)((a.n + per - 1) / per)), block, 0, st, a);
+  if (table_dtype == SV_F32) hipLaunchKernelGGL((embedding_grad_rows_kernel<DTG, DT_F32>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((embedding_grad_rows_kernel<DTG, DT_BF16>), grid, block, 0, st, a);
 }
 
 }  // namespace sv
@@ -288,7 +442,7 @@ extern "C" int sv_embedding(const void* table, const int32_t* ids, int n, int V,
 
 extern "C" size_t sv_embedding_grad_workspace_bytes(int n, int V, int D) {
   if (n < 0 || n > SV_EMBEDDING_MAX_TOKENS || V < 1 || V > (1 << 24) || D < 1 || D > (1 << 24)) return 0;
-  const size_t need = sv::carve_embedding_ws(nullptr, n).bytes;
+  const size_t need = sv::carve_embedding_ws(nullptr, n, V, D).bytes;
   return need < sv::kWsAlign ? sv::kWsAlign : need;
 }
 
@@ -306,18 +460,21 @@ extern "C" int sv_embedding_grad(const void* grad_out, int dtype, const int32_t*
              SV_ERR_ALIGN);
   SV_REQUIRE(ws && is_aligned(ws, kWsAlign) && ws_bytes >= sv_embedding_grad_workspace_bytes(n, V, D), SV_ERR_WORKSPACE);
   hipStream_t st = as_stream(stream);
-  const EmbeddingWs w = carve_embedding_ws(ws, n);
-  int bits = 1;
-  while ((V >> bits) != 0) ++bits;                       // keys 0 .. V
-  int at = 0;
-  for (int shift = 0; n > 0 && shift < bits; shift += kDigitBits) {
-    SortPass p = {shift == 0 ? ids : nullptr, w.key[at], w.pos[at], w.key[1 - at], w.pos[1 - at], w.hist, n, V, shift};
-    const dim3 grid((unsigned)sort_tiles(n)), block(kSortThreads);
-    hipLaunchKernelGGL(sort_count_kernel, grid, block, 0, st, p);
-    hipLaunchKernelGGL(sort_scatter_kernel, grid, block, 0, st, p, sort_tiles(n));
-    at = 1 - at;
+  GradRows a = {grad_out, grad_table, ids, nullptr, nullptr, nullptr, nullptr, nullptr, n, V, D, lanes_per_row(D),
+                accumulate != 0, scale};
+  if (n > kDirectTokens) {
+    const EmbeddingWs w = carve_embedding_ws(ws, n, V, D);
+    int bits = 1, at = 0;
+    while ((V >> bits) != 0) ++bits;                     // keys 0 .. V
+    for (int shift = 0; shift < bits; shift += kDigitBits) {
+      const SortPass p = {shift == 0 ? ids : nullptr, w.key[at], w.pos[at], w.key[1 - at], w.pos[1 - at], w.hist, n, V, shift};
+      const dim3 grid((unsigned)sort_tiles(n)), block(kSortThreads);
+      hipLaunchKernelGGL(sort_count_kernel, grid, block, 0, st, p);
+      hipLaunchKernelGGL(sort_scatter_kernel, grid, block, 0, st, p, sort_tiles(n));
+      at = 1 - at;
+    }
+    a.key = w.key[at]; a.pos = w.pos[at]; a.first = w.first; a.last = w.last; a.part = w.part;
   }
-  const GradRows a = {grad_out, grad_table, w.key[at], w.pos[at], n, V, D, lanes_per_row(D), accumulate != 0, scale};
   if (dtype == SV_F32) launch_grad_rows<DT_F32>(a, table_dtype, st);
   else launch_grad_rows<DT_BF16>(a, table_dtype, st);
   return launch_status();
