@@ -10,6 +10,7 @@ namespace sv {
 
 constexpr int kChunkCols = 8;           // columns of one lane: 16 bytes of bfloat16, 32 of float32
 constexpr int kEmbThreads = 256;
+constexpr int kMinLanes = 8;            // lanes of a row at least
 
 // Columns 8c .. 8c + 7 of a row of D; columns past D are 0 and are not written.
 template <int DT>
@@ -55,7 +56,7 @@ __device__ __forceinline__ void store_chunk(void* row, int D, int c, const float
 // Lanes that share a row: a power of two, so that a workgroup holds a whole number of rows.
 inline int lanes_per_row(int D) {
   const int chunks = (D + kChunkCols - 1) / kChunkCols;
-  int lanes = 1;
+  int lanes = kMinLanes;
   while (lanes < chunks && lanes < kEmbThreads) lanes *= 2;
   return lanes;
 }
@@ -134,6 +135,21 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortPa
     key[j] = i < p.n ? sort_key(p, i) : 0;
     pos[j] = i < p.n ? (p.ids ? i : p.pos_in[i]) : 0;
   }
+  // entries of a digit in the tiles before this one, and in all: all loads under way before the first is used
+  constexpr int kAhead = 16;
+  int before = 0, total = 0;
+  if (tid < kDigits) {
+    for (int t0 = 0; t0 < tiles; t0 += kAhead) {
+      int c[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) c[u] = t0 + u < tiles ? p.hist[(size_t)(t0 + u) * kDigits + tid] : 0;
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        before += t0 + u < (int)blockIdx.x ? c[u] : 0;
+        total += c[u];
+      }
+    }
+  }
   volatile int* mine = count[wave];
 #pragma unroll
   for (int j = 0; j < kSortPerLane; ++j) {
@@ -146,22 +162,15 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortPa
       same &= (d >> b) & 1 ? set : ~set;
     }
     const int below = __popcll(same & ((1ull << lane) - 1));
-    const int before = mine[d];
-    rank[j] = before + below;
+    const int so_far = mine[d];
+    rank[j] = so_far + below;
     __builtin_amdgcn_wave_barrier();                   // (every lane has read before one of them writes)
-    if (on && below == 0) mine[d] = before + __popcll(same);
+    if (on && below == 0) mine[d] = so_far + __popcll(same);
     __builtin_amdgcn_wave_barrier();
   }
   __syncthreads();
   // where a digit's entries of this tile start, and each wavefront's within them
-  int before = 0, total = 0, own = 0;
-  if (tid < kDigits) {
-    for (int t = 0; t < tiles; ++t) {
-      const int c = p.hist[(size_t)t * kDigits + tid];
-      before += t < (int)blockIdx.x ? c : 0;
-      total += c;
-    }
-  }
+  int own = 0;
   const int scan = wave_scan_i32(total);
   if (lane == kWave - 1) wave_sum[wave] = scan;
   __syncthreads();
@@ -188,9 +197,16 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortPa
 // ---------------------------------------------------------------------------
 // sums
 // ---------------------------------------------------------------------------
-constexpr int kRowsPerGroup = 16;       // rows of the table of one workgroup
+constexpr int kRounds = 8;              // rows of the table of one group of lanes
+constexpr int kMaxGroups = kEmbThreads / kMinLanes, kMaxRows = kRounds * kMaxGroups;
 constexpr int kPiece = 64;              // sorted positions summed by one group of lanes; a token with more is joined from pieces
 constexpr int kDirectTokens = 1024;     // up to here every workgroup looks through all tokens itself
+
+// Row of the table that group `group` of workgroup `block` has in round k: frequent tokens, whose numbers
+// often lie together, are spread over the workgroups.
+__device__ __forceinline__ long long row_of(int block, int group, int groups, int k) {
+  return ((long long)k * gridDim.x + block) * groups + group;
+}
 
 struct GradRows {
   const void* g;
@@ -204,27 +220,50 @@ struct GradRows {
   float scale;
 };
 
-// sum += the rows of positions at(lo) .. at(hi - 1), in this order; kAhead of them are under way at a time.
+// sum += the rows of positions at(lo) .. at(hi - 1), in this order; eight 16-byte loads of a lane are under way at a time.
 template <int DT, class At>
 __device__ __forceinline__ void add_rows(const GradRows& a, int c, int lo, int hi, At&& at, float (&sum)[kChunkCols]) {
-  constexpr int kAhead = 4;
+  constexpr int kVecs = kChunkCols / Elem<DT>::per_vec, kAhead = 8 / kVecs;
   const char* g = static_cast<const char*>(a.g);
   const size_t bytes = (size_t)a.D * Elem<DT>::bytes;
+  if ((c + 1) * kChunkCols > a.D) {                    // the last columns of a row that is no multiple of 8
+    for (int i = lo; i < hi; ++i) {
+      float f[kChunkCols];
+      load_chunk<DT>(g + at(i) * bytes, a.D, c, f);
+#pragma unroll
+      for (int j = 0; j < kChunkCols; ++j) sum[j] += f[j];
+    }
+    return;
+  }
+  auto add = [&](const u32x4 (&q)[kVecs]) {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      float f[Elem<DT>::per_vec];
+      unpack<DT>(q[k], f);
+#pragma unroll
+      for (int j = 0; j < Elem<DT>::per_vec; ++j) sum[k * Elem<DT>::per_vec + j] += f[j];
+    }
+  };
+  auto load = [&](int i, u32x4 (&q)[kVecs]) {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) q[k] = load_vec(g + at(i) * bytes, c * kVecs + k);
+  };
   int i = lo;
   for (; i + kAhead <= hi; i += kAhead) {
-    float f[kAhead][kChunkCols];
+    u32x4 q[kAhead][kVecs];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) load_chunk<DT>(g + at(i + u) * bytes, a.D, c, f[u]);
+    for (int u = 0; u < kAhead; ++u) load(i + u, q[u]);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-      for (int j = 0; j < kChunkCols; ++j) sum[j] += f[u][j];
+    for (int u = 0; u < kAhead; ++u) add(q[u]);
   }
-  for (; i < hi; ++i) {
-    float f[kChunkCols];
-    load_chunk<DT>(g + at(i) * bytes, a.D, c, f);
+  if (i < hi) {                                        // the last, partial round
+    u32x4 q[kAhead - 1][kVecs];
 #pragma unroll
-    for (int j = 0; j < kChunkCols; ++j) sum[j] += f[j];
+    for (int u = 0; u < kAhead - 1; ++u)
+      if (i + u < hi) load(i + u, q[u]);
+#pragma unroll
+    for (int u = 0; u < kAhead - 1; ++u)
+      if (i + u < hi) add(q[u]);
   }
 }
 
@@ -238,26 +277,28 @@ __device__ __forceinline__ void store_sum(const GradRows& a, int v, int c, float
   store_chunk<DTW>(to, a.D, c, sum);
 }
 
-// Few tokens: one launch.  A workgroup of kRowsPerGroup rows picks the tokens of its rows out of all, in order.
+// Few tokens: one launch.  A workgroup picks the tokens of its rows out of all, in the order of their positions.
 template <int DTG, int DTW>
 __global__ __launch_bounds__(kEmbThreads) void embedding_grad_direct_kernel(const GradRows a) {
-  constexpr int kWaves = kEmbThreads / kWave;
-  __shared__ uint32_t found[kDirectTokens];            // row of the workgroup << 16 | position, by position
+  constexpr int kWaves = kEmbThreads / kWave, kLooks = kDirectTokens / kEmbThreads;
+  __shared__ uint32_t found[kDirectTokens];            // row of the workgroup << 16 | position
   __shared__ uint16_t pos[kDirectTokens];              // positions by row, then by position
-  __shared__ int count[kWaves], start[kRowsPerGroup + 1];
-  const int v0 = blockIdx.x * kRowsPerGroup, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint64_t below = (1ull << lane) - 1;
+  __shared__ uint16_t start[kMaxRows], end[kMaxRows];
+  __shared__ int count[kWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int groups = kEmbThreads / a.lanes;
+  for (int r = threadIdx.x; r < kRounds * groups; r += kEmbThreads) start[r] = end[r] = 0;
   // a wavefront looks through a run of tokens
-  constexpr int kRounds = kDirectTokens / kEmbThreads;
-  uint64_t hit[kRounds];
-  int row[kRounds], mine = 0;
+  uint64_t hit[kLooks];
+  int row[kLooks], mine = 0;
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
-    const int i = (wave * kRounds + r) * kWave + lane;
-    const int id = i < a.n ? max(a.ids[i], -1) : -1;
-    row[r] = id - v0;
-    hit[r] = __ballot(id >= v0 && row[r] < kRowsPerGroup && id < a.V);
-    mine += __popcll(hit[r]);
+  for (int j = 0; j < kLooks; ++j) {
+    const int i = (wave * kLooks + j) * kWave + lane;
+    const int id = i < a.n ? a.ids[i] : -1;
+    const uint32_t unit = (uint32_t)max(id, 0) / (uint32_t)groups, k = unit / gridDim.x;
+    row[j] = (int)k * groups + max(id, 0) % groups;
+    hit[j] = __ballot(id >= 0 && id < a.V && unit - k * gridDim.x == blockIdx.x);
+    mine += __popcll(hit[j]);
   }
   if (lane == 0) count[wave] = mine;
   __syncthreads();
@@ -268,34 +309,35 @@ __global__ __launch_bounds__(kEmbThreads) void embedding_grad_direct_kernel(cons
     total += count[w];
   }
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
-    if (hit[r] >> lane & 1)
-      found[to + __popcll(hit[r] & below)] = (uint32_t)row[r] << 16 | ((wave * kRounds + r) * kWave + lane);
-    to += __popcll(hit[r]);
+  for (int j = 0; j < kLooks; ++j) {
+    if (hit[j] >> lane & 1)
+      found[to + __popcll(hit[j] & ((1ull << lane) - 1))] = (uint32_t)row[j] << 16 | ((wave * kLooks + j) * kWave + lane);
+    to += __popcll(hit[j]);
   }
   __syncthreads();
-  for (int r = wave; r < kRowsPerGroup; r += kWaves) {  // tokens of the rows before r, and those of r in order
-    int before = 0;
-    for (int i0 = 0; i0 < total; i0 += kWave)
-      before += __popcll(__ballot(i0 + lane < total && (int)(found[min(i0 + lane, total - 1)] >> 16) < r));
-    if (lane == 0) start[r] = before;
-    for (int i0 = 0; i0 < total; i0 += kWave) {
-      const uint32_t f = found[min(i0 + lane, total - 1)];
-      const uint64_t here = __ballot(i0 + lane < total && (int)(f >> 16) == r);
-      if (here >> lane & 1) pos[before + __popcll(here & below)] = (uint16_t)f;
-      before += __popcll(here);
+  for (int i = threadIdx.x; i < total; i += kEmbThreads) {
+    const uint32_t f = found[i], r = f >> 16;
+    int smaller = 0, same = 0, earlier = 0;
+    for (int m = 0; m < total; ++m) {
+      const uint32_t o = found[m] >> 16;
+      smaller += o < r;
+      same += o == r;
+      earlier += o == r && m < i;
     }
+    pos[smaller + earlier] = (uint16_t)f;
+    if (earlier == 0) { start[r] = (uint16_t)smaller; end[r] = (uint16_t)(smaller + same); }
   }
-  if (threadIdx.x == 0) start[kRowsPerGroup] = total;
   __syncthreads();
-  const int l = threadIdx.x % a.lanes;
-  for (int r = threadIdx.x / a.lanes; r < kRowsPerGroup && v0 + r < a.V; r += kEmbThreads / a.lanes) {
-    const int lo = start[r], hi = start[r + 1];
+  const int l = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes;
+  for (int k = 0; k < kRounds; ++k) {
+    const long long v = row_of(blockIdx.x, group, groups, k);
+    if (v >= a.V) break;
+    const int lo = start[k * groups + group], hi = end[k * groups + group];
     if (lo == hi && a.accumulate) continue;
     for (int c = l; c * kChunkCols < a.D; c += a.lanes) {
       float sum[kChunkCols] = {};
       add_rows<DTG>(a, c, lo, hi, [&](int i) { return (size_t)pos[i]; }, sum);
-      store_sum<DTW>(a, v0 + r, c, sum);
+      store_sum<DTW>(a, (int)v, c, sum);
     }
   }
 }
@@ -304,74 +346,82 @@ __global__ __launch_bounds__(kEmbThreads) void embedding_grad_direct_kernel(cons
 // that have more than kPiece.  Such a token is in a piece from its first position on, or up to its last.
 template <int DTG>
 __global__ __launch_bounds__(kEmbThreads) void embedding_grad_pieces_kernel(const GradRows a) {
+  __shared__ uint32_t key[kMaxGroups * kPiece];
+  __shared__ int32_t pos[kMaxGroups * kPiece];
   const int pieces = kEmbThreads / a.lanes;            // of the workgroup
   const long long base = (long long)blockIdx.x * pieces * kPiece;
-  for (int j = threadIdx.x; j < pieces * kPiece; j += kEmbThreads) {
-    const long long i = base + j;
-    if (i >= a.n) break;
+  for (int j = threadIdx.x; j < pieces * kPiece && base + j < a.n; j += kEmbThreads) {
+    const int i = (int)(base + j);
     const uint32_t k = a.key[i];
+    const uint32_t left = i > 0 ? a.key[i - 1] : ~0u, right = i < a.n - 1 ? a.key[i + 1] : ~0u;
+    key[j] = k;
+    pos[j] = a.pos[i];
     if (k >= (uint32_t)a.V) continue;
-    if (i == 0 || a.key[i - 1] != k) a.first[k] = (int)i;
-    if (i == a.n - 1 || a.key[i + 1] != k) a.last[k] = (int)i + 1;
+    if (left != k) a.first[k] = i;
+    if (right != k) a.last[k] = i + 1;
   }
-  const int l = threadIdx.x % a.lanes;
-  const long long piece = (long long)blockIdx.x * pieces + threadIdx.x / a.lanes;
-  if (piece * kPiece >= a.n) return;
-  const int lo = (int)(piece * kPiece), hi = min(lo + kPiece, a.n);
+  __syncthreads();
+  const int l = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes;
+  const long long lo = base + group * kPiece;
+  if (lo >= a.n) return;
+  const int size = (int)min((long long)kPiece, a.n - lo);
+  const uint32_t* mine = key + group * kPiece;
   auto sum_piece = [&](int from, int to, int slot) {
     for (int c = l; c * kChunkCols < a.D; c += a.lanes) {
       float sum[kChunkCols] = {};
-      add_rows<DTG>(a, c, from, to, [&](int i) { return (size_t)a.pos[i]; }, sum);
-      store_chunk<DT_F32>(a.part + ((size_t)piece * 2 + slot) * a.D, a.D, c, sum);
+      add_rows<DTG>(a, c, from, to, [&](int i) { return (size_t)pos[group * kPiece + i]; }, sum);
+      store_chunk<DT_F32>(a.part + ((size_t)(lo / kPiece) * 2 + slot) * a.D, a.D, c, sum);
     }
   };
-  auto search = [&](uint32_t k, bool after) {          // first position of the piece with a key at least / above k
-    int x = lo, y = hi;
+  auto search = [&](uint32_t k) {                      // first entry of the piece with a key of at least k
+    int x = 0, y = size;
     while (x < y) {
       const int mid = (x + y) / 2;
-      if (a.key[mid] < k || (after && a.key[mid] == k)) x = mid + 1; else y = mid;
+      if (mine[mid] < k) x = mid + 1; else y = mid;
     }
     return x;
   };
-  const uint32_t k0 = a.key[lo], k1 = a.key[hi - 1];
-  const int end = search(k0, true);
-  // more than kPiece of k0: kPiece positions before its last one here is another, or it goes on after a whole piece
-  const bool long0 = (end - 1 >= kPiece && a.key[end - 1 - kPiece] == k0) || (end - lo == kPiece && hi < a.n && a.key[hi] == k0);
-  if (k0 < (uint32_t)a.V && long0) sum_piece(lo, end, 0);
-  if (end == hi || k1 >= (uint32_t)a.V) return;
-  const int from = search(k1, false);
-  if (from + kPiece < a.n && a.key[from + kPiece] == k1) sum_piece(from, hi, 1);
+  auto has = [&](long long i, uint32_t k) { return i >= 0 && i < a.n && a.key[i] == k; };
+  const uint32_t k0 = mine[0], k1 = mine[size - 1];
+  const int to = search(k0 + 1), from = search(k1);
+  // more than kPiece positions: the first token's begin before the piece, or fill it and go on
+  if (k0 < (uint32_t)a.V && (has(lo + to - 1 - kPiece, k0) || (to == kPiece && has(lo + kPiece, k0)))) sum_piece(0, to, 0);
+  if (to < size && k1 < (uint32_t)a.V && has(lo + from + kPiece, k1)) sum_piece(from, size, 1);
 }
 
 // Second launch: every row of the table.
 template <int DTG, int DTW>
 __global__ __launch_bounds__(kEmbThreads) void embedding_grad_rows_kernel(const GradRows a) {
-  __shared__ int start[kRowsPerGroup], end[kRowsPerGroup];
-  const int v0 = blockIdx.x * kRowsPerGroup;
-  if (threadIdx.x < kRowsPerGroup) {
+  __shared__ int start[kMaxRows], end[kMaxRows];
+  const int groups = kEmbThreads / a.lanes;
+  for (int r = threadIdx.x; r < kRounds * groups; r += kEmbThreads) {
     // what the arrays hold for a token that does not occur is from elsewhere: no sorted position has that token
-    const int v = v0 + threadIdx.x;
+    const long long v = row_of(blockIdx.x, r % groups, groups, r / groups);
     const int lo = v < a.V ? a.first[v] : -1;
     const bool occurs = lo >= 0 && lo < a.n && a.key[lo] == (uint32_t)v;
-    start[threadIdx.x] = occurs ? lo : 0;
-    end[threadIdx.x] = occurs ? a.last[v] : 0;
+    start[r] = occurs ? lo : 0;
+    end[r] = occurs ? a.last[v] : 0;
   }
   __syncthreads();
-  const int l = threadIdx.x % a.lanes;
-  for (int r = threadIdx.x / a.lanes; r < kRowsPerGroup && v0 + r < a.V; r += kEmbThreads / a.lanes) {
-    const int lo = start[r], hi = end[r];
+  const int l = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes;
+  for (int k = 0; k < kRounds; ++k) {
+    const long long v = row_of(blockIdx.x, group, groups, k);
+    if (v >= a.V) break;
+    const int lo = start[k * groups + group], hi = end[k * groups + group];
     if (lo == hi && a.accumulate) continue;
     for (int c = l; c * kChunkCols < a.D; c += a.lanes) {
       float sum[kChunkCols] = {};
       if (hi - lo <= kPiece) {
         add_rows<DTG>(a, c, lo, hi, [&](int i) { return (size_t)a.pos[i]; }, sum);
       } else {
-        const GradRows parts = {a.part, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0, a.D, 0, 0, 0.f};
+        GradRows parts = {};
+        parts.g = a.part;
+        parts.D = a.D;
         const int p0 = lo / kPiece, slot0 = lo % kPiece != 0;
         add_rows<DT_F32>(parts, c, p0, (hi - 1) / kPiece + 1, [&](int p) { return (size_t)p * 2 + (p == p0 ? slot0 : 0); },
                          sum);
       }
-      store_sum<DTW>(a, v0 + r, c, sum);
+      store_sum<DTW>(a, (int)v, c, sum);
     }
   }
 }
@@ -405,7 +455,8 @@ inline EmbeddingWs carve_embedding_ws(void* base, int n, int V, int D) {
 
 template <int DTG>
 void launch_grad_rows(const GradRows& a, int table_dtype, hipStream_t st) {
-  const dim3 grid((unsigned)((a.V + kRowsPerGroup - 1) / kRowsPerGroup)), block(kEmbThreads);
+  const int rows = kEmbThreads / a.lanes * kRounds;
+  const dim3 grid((unsigned)((a.V + rows - 1) / rows)), block(kEmbThreads);
   if (!a.key) {                                          // (of no tokens at all the list may be NULL as well)
     if (table_dtype == SV_F32) hipLaunchKernelGGL((embedding_grad_direct_kernel<DTG, DT_F32>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((embedding_grad_direct_kernel<DTG, DT_BF16>), grid, block, 0, st, a);
