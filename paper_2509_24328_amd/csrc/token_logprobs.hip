@@ -20,10 +20,11 @@ constexpr float kLowY = -200.f;        // 2^y is 0 in fp32 below: stands in for 
 struct RowSums {
   float c, limit;     // reference; logits above the limit raise it
   float m;            // largest logit of the lane
+  int best;           // the first of its vectors that holds it (where alternatives are asked for)
   double s, w;        // sum 2^y, sum 2^y y
   int ahead;          // entries before the token in the order of the alternatives
 
-  __device__ __forceinline__ void init(float L) { c = kRefFloor; limit = c / L; m = -INFINITY; s = w = 0; ahead = 0; }
+  __device__ __forceinline__ void init(float L) { c = kRefFloor; limit = c / L; m = -INFINITY; s = w = 0; best = 0; ahead = 0; }
 
   // (all lanes of the wavefront)
   __device__ __forceinline__ void raise(float largest, float L) {
@@ -74,7 +75,7 @@ __device__ __forceinline__ u32x4 load_row_vec(const void* row, int V, int i) {
 }
 
 // Adds U vectors of a lane (i, i + step, ...).  All lanes of the wavefront.
-template <int DT, int U, bool ENT>
+template <int DT, int U, bool ENT, bool TOP>
 __device__ __forceinline__ void add_vectors(const u32x4 (&q)[U], int i, int step, float L, float zt, int token,
                                             RowSums& r) {
   constexpr int EPV = Elem<DT>::per_vec;
@@ -83,11 +84,18 @@ __device__ __forceinline__ void add_vectors(const u32x4 (&q)[U], int i, int step
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     unpack<DT>(q[u], f[u]);
+    float vm = f[u][0];
 #pragma unroll
-    for (int j = 0; j < EPV; j += 2) gm = fmaxf(fmaxf(gm, f[u][j]), f[u][j + 1]);
+    for (int j = 1; j + 1 < EPV; j += 2) vm = fmaxf(fmaxf(vm, f[u][j]), f[u][j + 1]);
+    vm = fmaxf(vm, f[u][EPV - 1]);
+    gm = fmaxf(gm, vm);
+    if (TOP && vm > r.m) {
+      r.m = vm;
+      r.best = i + u * step;
+    }
   }
   if (__any(gm > r.limit)) r.raise(gm, L);
-  r.m = fmaxf(r.m, gm);
+  if (!TOP) r.m = fmaxf(r.m, gm);
   if (__any(gm >= zt)) {                               // (NaN without a token: never)
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -147,20 +155,21 @@ __device__ __forceinline__ RowTotals fold_row(const RowSums& r, RowScratch& sm) 
   return t;
 }
 
-template <int DT, bool ENT>
-__device__ __forceinline__ RowTotals sweep_row(const void* row, int V, float L, float zt, int token, RowScratch& sm) {
+// Sweep of a row by a workgroup of NT lanes; r keeps the lane's own part.
+template <int DT, int NT, bool ENT, bool TOP>
+__device__ __forceinline__ RowTotals sweep_row(const void* row, int V, float L, float zt, int token, RowSums& r,
+                                               RowScratch& sm) {
   constexpr int EPV = Elem<DT>::per_vec, U = 4;
-  const int n = (V + EPV - 1) / EPV, nt = blockDim.x;
-  RowSums r;
+  const int n = (V + EPV - 1) / EPV;
   r.init(L);
-  for (int i0 = 0; i0 < n; i0 += U * nt) {             // (the same number of rounds in every lane)
+  for (int i0 = 0; i0 < n; i0 += U * NT) {             // (the same number of rounds in every lane)
     u32x4 q[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * nt + (int)threadIdx.x;
+      const int i = i0 + u * NT + (int)threadIdx.x;
       q[u] = i < n ? load_row_vec<DT>(row, V, i) : no_mass<DT>();
     }
-    add_vectors<DT, U, ENT>(q, i0 + (int)threadIdx.x, nt, L, zt, token, r);
+    add_vectors<DT, U, ENT, TOP>(q, i0 + (int)threadIdx.x, NT, L, zt, token, r);
   }
   return fold_row(r, sm);
 }
@@ -212,13 +221,99 @@ __device__ __forceinline__ void write_blank(const ScoreArgs& a, long long at, bo
   if (a.flags) a.flags[at] = bad ? SV_FLAG_BAD_ROW : 0;
 }
 
-constexpr int kScoreThreads = 1024;
+// The n first entries of a row in the order by value and, among equal ones, by token.  After the sweep every lane knows
+// its largest entry.  The n lanes that are first by (value, vector) hold the n first entries: an entry of any
+// other lane has n before it.  So the lanes are ranked (only those that a bound lets through, which each
+// wavefront forms from its own), the n lanes' vectors read again, and what is not behind the n-th lane's best ranked
+// in turn.  Ranks by counting: the keys are distinct, and about n lanes and little more than n entries are
+// left.  The sweep pays two instructions a vector for this, whatever the row holds.
+constexpr int kCandidates = 1024;
 
-template <int DT, bool ENT>
-__global__ __launch_bounds__(kScoreThreads) void token_logprobs_kernel(const ScoreArgs a) {
-  constexpr int EPV = Elem<DT>::per_vec;
+template <int NT>
+struct TopScratch {
+  uint64_t lanes[NT], first[SV_TOP_MAX], found[kCandidates];
+  float bound[NT / kWave];
+  int n_lanes, n_found;
+};
+
+template <int DT, int NT, class Emit>
+__device__ __forceinline__ void alternatives(const void* row, int V, float L, int n, float best, int best_vec,
+                                             TopScratch<NT>& sm, Emit&& emit) {
+  constexpr int EPV = Elem<DT>::per_vec, kWaves = NT / kWave;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n_vec = (V + EPV - 1) / EPV;
+  if (!(best * L >= kRefFloor)) best = -INFINITY;      // nothing with mass
+  // n lanes at least are not below the lowest, over the wavefronts, of their n / kWaves-th lanes
+  float left = best, low = 0.f;
+  for (int j = 0; j < n; j += kWaves) {
+    low = wave_max_f32(left);
+    if (lane == __builtin_ctzll(__ballot(left == low))) left = -INFINITY;
+  }
+  if (lane == 0) sm.bound[wave] = low;
+  if (tid == 0) sm.n_lanes = sm.n_found = 0;
+  __syncthreads();
+  for (int w = 0; w < kWaves; ++w) low = fminf(low, sm.bound[w]);
+  if (best >= low && best > -INFINITY)
+    sm.lanes[atomicAdd(&sm.n_lanes, 1)] = (uint64_t)ordered(best) << 32 | (uint32_t)~best_vec;
+  __syncthreads();
+  const int n_lanes = sm.n_lanes, n_first = min(n, n_lanes);
+  if (tid < n_lanes) {
+    const uint64_t key = sm.lanes[tid];
+    int rank = 0;
+    for (int m = 0; m < n_lanes; ++m) rank += sm.lanes[m] > key;
+    if (rank < n) sm.first[rank] = key;
+  }
+  __syncthreads();
+  const uint64_t last = n_lanes >= n ? sm.first[n - 1] : 0;
+  const float last_z = last ? from_ordered((uint32_t)(last >> 32)) : -INFINITY;
+  const int last_vec = last ? (int)~(uint32_t)last : V;
+  const int per_lane = (n_vec + NT - 1) / NT;
+  auto visit = [&](auto&& take) {                      // the entries of the first lanes that may be among the n
+    for (int p = tid; p < n_first * per_lane; p += NT) {
+      const int i = (int)~(uint32_t)sm.first[p % n_first] % NT + p / n_first * NT;
+      if (i >= n_vec) continue;
+      float f[EPV];
+      unpack<DT>(load_row_vec<DT>(row, V, i), f);
+#pragma unroll
+      for (int j = 0; j < EPV; ++j)
+        if ((f[j] > last_z || (f[j] == last_z && i <= last_vec)) && f[j] * L >= kRefFloor)
+          take((uint64_t)ordered(f[j]) << 32 | (uint32_t)~(i * EPV + j));
+    }
+  };
+  visit([&](uint64_t key) {
+    const int at = atomicAdd(&sm.n_found, 1);
+    if (at < kCandidates) sm.found[at] = key;
+  });
+  __syncthreads();
+  const int n_found = sm.n_found;
+  if (n_found <= kCandidates) {
+    for (int t = tid; t < n_found; t += NT) {
+      const uint64_t key = sm.found[t];
+      int rank = 0;
+      for (int m = 0; m < n_found; ++m) rank += sm.found[m] > key;
+      if (rank < n) emit(rank, key);
+    }
+    if (tid < n && tid >= n_found) emit(tid, 0);
+    return;
+  }
+  // large entries that all lie in few lanes: the largest one below the one before, n times
+  uint64_t before = ~0ull;
+  for (int r = 0; r < n; ++r) {
+    uint64_t key = 0;
+    visit([&](uint64_t k) { key = k < before && k > key ? k : key; });
+    key = wave_max_u64(key);
+    if (lane == 0) sm.lanes[wave] = key;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) key = sm.lanes[w] > key ? sm.lanes[w] : key;
+    __syncthreads();
+    if (tid == 0) emit(r, key);
+    before = key;
+  }
+}
+
+template <int DT, int NT, bool ENT, bool TOP>
+__global__ __launch_bounds__(NT) void token_logprobs_kernel(const ScoreArgs a) {
   __shared__ RowScratch sm;
-  __shared__ uint64_t best_of[16];
   const long long at = blockIdx.x;
   const int V = a.V;
   int token = -1;
@@ -237,7 +332,8 @@ __global__ __launch_bounds__(kScoreThreads) void token_logprobs_kernel(const Sco
   const void* row = static_cast<const char*>(a.z) + (size_t)at_row * (size_t)a.stride * Elem<DT>::bytes;
   const bool given = token >= 0 && token < V;
   const float zt = given ? load_elem<DT>(row, token) : __builtin_nanf("");
-  const RowTotals t = sweep_row<DT, ENT>(row, V, a.sc.L, zt, token, sm);
+  RowSums r;
+  const RowTotals t = sweep_row<DT, NT, ENT, TOP>(row, V, a.sc.L, zt, token, r, sm);
   if (t.bad()) return write_blank(a, at, true);
   const double lse = t.lse(a.sc);
   auto logprob_of = [&](float z) {
@@ -250,30 +346,22 @@ __global__ __launch_bounds__(kScoreThreads) void token_logprobs_kernel(const Sco
     if (a.rank) a.rank[at] = given ? 1 + t.ahead : 0;
     if (a.flags) a.flags[at] = a.tokens && !given ? SV_FLAG_BAD_TOKEN : 0;
   }
-  // alternatives: the largest key (value, then lowest id) below the one before it
-  uint64_t before = ~0ull;
-  for (int r = 0; r < a.n_top; ++r) {
-    uint64_t best = 0;
-    for (int i = threadIdx.x; i * EPV < V; i += blockDim.x) {
-      float f[EPV];
-      unpack<DT>(load_row_vec<DT>(row, V, i), f);
-#pragma unroll
-      for (int j = 0; j < EPV; ++j) {
-        const uint64_t key = ((uint64_t)ordered(f[j]) << 32) | (uint32_t)~(i * EPV + j);
-        if (f[j] * a.sc.L >= kRefFloor && key < before && key > best) best = key;
-      }
-    }
-    best = wave_max_u64(best);
-    if ((threadIdx.x & 63) == 0) best_of[threadIdx.x >> 6] = best;
-    __syncthreads();
-    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) best = best_of[w] > best ? best_of[w] : best;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      a.top_token[at * a.n_top + r] = best ? (int)~(uint32_t)best : -1;
-      a.top_logprob[at * a.n_top + r] = best ? logprob_of(from_ordered((uint32_t)(best >> 32))) : -INFINITY;
-    }
-    before = best;                                     // (0: nothing is below it)
+  if constexpr (TOP) {
+    __shared__ TopScratch<NT> top;
+    alternatives<DT, NT>(row, V, a.sc.L, a.n_top, r.m, r.best, top, [&](int rank, uint64_t key) {
+      a.top_token[at * a.n_top + rank] = key ? (int)~(uint32_t)key : -1;
+      a.top_logprob[at * a.n_top + rank] = key ? logprob_of(from_ordered((uint32_t)(key >> 32))) : -INFINITY;
+    });
   }
+}
+
+constexpr int kGradThreads = 1024;
+
+template <int DT, bool ENT>
+void launch_score(const ScoreArgs& a, long long rows, hipStream_t st) {
+  const dim3 grid((unsigned)rows);
+  if (a.n_top > 0) hipLaunchKernelGGL((token_logprobs_kernel<DT, 1024, ENT, true>), grid, dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL((token_logprobs_kernel<DT, 1024, ENT, false>), grid, dim3(1024), 0, st, a);
 }
 
 struct GradArgs {
@@ -309,7 +397,7 @@ __device__ __forceinline__ void store_row_vec(void* row, int V, int i, const flo
 }
 
 template <int DT, bool ENT>
-__global__ __launch_bounds__(kScoreThreads) void token_logprobs_grad_kernel(const GradArgs a) {
+__global__ __launch_bounds__(kGradThreads) void token_logprobs_grad_kernel(const GradArgs a) {
   constexpr int EPV = Elem<DT>::per_vec;
   __shared__ RowScratch sm;
   const long long at = blockIdx.x;
@@ -332,7 +420,8 @@ __global__ __launch_bounds__(kScoreThreads) void token_logprobs_grad_kernel(cons
   }
   const bool given = token >= 0 && token < V;
   const float zt = given ? load_elem<DT>(row, token) : __builtin_nanf("");
-  const RowTotals t = sweep_row<DT, ENT>(row, V, a.sc.L, __builtin_nanf(""), -1, sm);
+  RowSums r;
+  const RowTotals t = sweep_row<DT, kGradThreads, ENT, false>(row, V, a.sc.L, __builtin_nanf(""), -1, r, sm);
   const bool bad = t.bad();
   if (threadIdx.x == 0) {
     const double x = bad || !given ? (double)__builtin_nanf("")
@@ -390,14 +479,14 @@ extern "C" int sv_token_logprobs(const void* z, int64_t z_stride, const int32_t*
   a.P = P; a.V = V; a.n_top = n_top;
   a.logprob = logprob_or_null; a.lse = lse_or_null; a.entropy = entropy_or_null; a.rank = rank_or_null;
   a.top_token = top_token_or_null; a.top_logprob = top_logprob_or_null; a.flags = flags_or_null;
-  const dim3 grid((unsigned)((long long)B * P)), block(kScoreThreads);
+  const long long rows = (long long)B * P;
   hipStream_t st = as_stream(stream);
   if (dtype == SV_F32) {
-    if (entropy_or_null) hipLaunchKernelGGL((token_logprobs_kernel<DT_F32, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((token_logprobs_kernel<DT_F32, false>), grid, block, 0, st, a);
+    if (entropy_or_null) launch_score<DT_F32, true>(a, rows, st);
+    else launch_score<DT_F32, false>(a, rows, st);
   } else {
-    if (entropy_or_null) hipLaunchKernelGGL((token_logprobs_kernel<DT_BF16, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((token_logprobs_kernel<DT_BF16, false>), grid, block, 0, st, a);
+    if (entropy_or_null) launch_score<DT_BF16, true>(a, rows, st);
+    else launch_score<DT_BF16, false>(a, rows, st);
   }
   return launch_status();
 }
@@ -423,7 +512,7 @@ extern "C" int sv_token_logprobs_grad(const void* z, int64_t z_stride, const int
   a.g_logprob = g_logprob; a.g_entropy = g_entropy_or_null; a.logprob = logprob_or_null; a.entropy = entropy_or_null;
   a.flags = flags_or_null; a.V = V;
   const bool ent = entropy_or_null || g_entropy_or_null;
-  const dim3 grid((unsigned)rows), block(kScoreThreads);
+  const dim3 grid((unsigned)rows), block(kGradThreads);
   hipStream_t st = as_stream(stream);
   if (dtype == SV_F32) {
     if (ent) hipLaunchKernelGGL((token_logprobs_grad_kernel<DT_F32, true>), grid, block, 0, st, a);
