@@ -614,13 +614,20 @@ int sv_accept_ratio_sparse(const int32_t* count_t, const int32_t* token_t, const
  * of the logits) has log-probability -inf and is no alternative: past the last one
  * top_token is -1 and top_logprob -inf.  Bad rows: NaN, rank 0, top_token -1.  Bad token:
  * logprob NaN and rank 0, the rest as ever.
+ *   ws_or_null                    256-byte aligned, of sv_token_logprobs_workspace_bytes(B*P, V, dtype, n_top)
  * V <= 16777216, temperature in [1e-3, 1e3].
  */
 int sv_token_logprobs(const void* z, int64_t z_stride, const int32_t* t_offsets_or_null, int n_rows,
                       const int32_t* tokens_or_null, int B, int P, int V, int dtype, float temperature, int n_top,
                       float* logprob_or_null, float* lse_or_null, float* entropy_or_null, int32_t* rank_or_null,
                       int32_t* top_token_or_null, float* top_logprob_or_null, uint32_t* flags_or_null,
-                      sv_stream_t stream);
+                      void* ws_or_null, size_t ws_bytes, sv_stream_t stream);
+
+/* Bytes of device scratch with which sv_token_logprobs on rows = B*P positions, or sv_token_logprobs_grad on `rows`
+ * (n_top = 0), divides its rows among more workgroups where there are few rows (0: it never does, or the
+ * shape is invalid).  Without scratch one workgroup sweeps each row: the same results, but for the order of the
+ * sums, in more time. */
+size_t sv_token_logprobs_workspace_bytes(int64_t rows, int V, int dtype, int n_top);
 
 /*
  * Gradient of  sum_r ( g_logprob[r] * logprob[r] + g_entropy[r] * entropy[r] )  with respect to
@@ -635,12 +642,13 @@ int sv_token_logprobs(const void* z, int64_t z_stride, const int32_t* t_offsets_
  *   logprob_or_null, entropy_or_null [rows] float                    out
  *   flags_or_null [rows] uint32   SV_FLAG_BAD_ROW / SV_FLAG_BAD_TOKEN: dz[r, :] is NaN then
  * bfloat16 gradients are rounded once, to nearest-even.  Columns of dz past V are left as they are.
+ *   ws_or_null   256-byte aligned, of sv_token_logprobs_workspace_bytes(rows, V, dtype, 0)
  * V <= 16777216, temperature in [1e-3, 1e3].
  */
 int sv_token_logprobs_grad(const void* z, int64_t z_stride, const int32_t* tokens, int rows, int V, int dtype,
                            float temperature, const float* g_logprob, const float* g_entropy_or_null,
                            float* logprob_or_null, float* entropy_or_null, void* dz, int64_t dz_stride,
-                           uint32_t* flags_or_null, sv_stream_t stream);
+                           uint32_t* flags_or_null, void* ws_or_null, size_t ws_bytes, sv_stream_t stream);
 
 /*
  * Embedding rows of tokens: out[i, :] = scale * table[ids[i], :], formed in float32 and rounded once.

@@ -9,7 +9,7 @@ from .binding import (sv_warp_cutoffs_multi, sv_warp_compact_multi, sv_accept_ra
                       alloc_workspace, sv_accept_estimate, sv_row_stats, sv_select_length,
                       sv_set_timing_events, sv_strerror, sv_verify_sample, sv_verify_sample_static,
                       sv_verify_sample_chained, sv_verify_sample_warped_chained, sv_estimate_select, sv_repetition_penalty, sv_repetition_penalty_multi,
-                      sv_token_logprobs, sv_token_logprobs_grad, sv_embedding, sv_embedding_grad,
+                      sv_token_logprobs, sv_token_logprobs_grad, sv_token_logprobs_workspace_bytes, sv_embedding, sv_embedding_grad,
                       sv_embedding_grad_workspace_bytes, sv_grad_norm, sv_clip_grad_norm,
                       sv_grad_norm_workspace_bytes, SV_TOP_MAX,
                       sv_workspace_bytes)

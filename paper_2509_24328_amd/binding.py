@@ -35,7 +35,8 @@ EXPORTS = ("sv_strerror", "sv_workspace_bytes", "sv_row_stats", "sv_accept_estim
            "sv_accept_ratio_sparse", "sv_verify_sample_static", "sv_accept_ratio_warped",
            "sv_warp_cutoffs_multi", "sv_warp_compact_multi", "sv_verify_sample_chained",
            "sv_verify_sample_warped_chained", "sv_estimate_select", "sv_repetition_penalty",
-           "sv_repetition_penalty_multi", "sv_token_logprobs", "sv_token_logprobs_grad", "sv_embedding",
+           "sv_repetition_penalty_multi", "sv_token_logprobs", "sv_token_logprobs_grad",
+           "sv_token_logprobs_workspace_bytes", "sv_embedding",
            "sv_embedding_grad_workspace_bytes", "sv_embedding_grad", "sv_grad_norm_workspace_bytes", "sv_grad_norm",
            "sv_clip_grad_norm")
 SV_WARP_MAX_TENSORS = 8
@@ -116,9 +117,12 @@ lib.sv_uniforms.restype = _i
 lib.sv_uniforms.argtypes = [ctypes.c_uint64, ctypes.c_uint32, _i, _i, _vp, _vp, _vp]
 _ll = ctypes.c_longlong
 lib.sv_token_logprobs.restype = _i
-lib.sv_token_logprobs.argtypes = [_vp, _ll, _vp, _i, _vp, _i, _i, _i, _i, _f, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+lib.sv_token_logprobs.argtypes = [_vp, _ll, _vp, _i, _vp, _i, _i, _i, _i, _f, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                  _vp, _sz, _vp]
+lib.sv_token_logprobs_workspace_bytes.restype = _sz
+lib.sv_token_logprobs_workspace_bytes.argtypes = [_ll, _i, _i, _i]
 lib.sv_token_logprobs_grad.restype = _i
-lib.sv_token_logprobs_grad.argtypes = [_vp, _ll, _vp, _i, _i, _i, _f, _vp, _vp, _vp, _vp, _vp, _ll, _vp, _vp]
+lib.sv_token_logprobs_grad.argtypes = [_vp, _ll, _vp, _i, _i, _i, _f, _vp, _vp, _vp, _vp, _vp, _ll, _vp, _vp, _sz, _vp]
 lib.sv_embedding.restype = _i
 lib.sv_embedding.argtypes = [_vp, _vp, _i, _i, _i, _i, _f, _vp, _vp, _vp]
 lib.sv_embedding_grad_workspace_bytes.restype = _sz
@@ -500,10 +504,29 @@ def _f32(*tensors):
             raise SvError(SV_ERR_DTYPE)
 
 
+def sv_token_logprobs_workspace_bytes(rows, V, dtype, n_top=0):
+    return int(lib.sv_token_logprobs_workspace_bytes(rows, V, dtype, n_top))
+
+
+def _row_scratch(ws, rows, V, tag, n_top, stream):
+    """(scratch of the scoring calls, its bytes): the caller's, or torch's own on the stream of the call, which may
+    hand it to a later call of that stream."""
+    if ws is None:
+        n = lib.sv_token_logprobs_workspace_bytes(rows, V, tag, n_top)
+        if n == 0:
+            return None, 0
+        if stream is None:
+            ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        else:
+            with torch.cuda.stream(stream):
+                ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    return ws, ws.numel()
+
+
 def sv_token_logprobs(z, tokens, logprob, lse=None, entropy=None, rank=None, top_token=None, top_logprob=None,
-                      flags=None, temperature=1.0, t_offsets=None, stream=None):
+                      flags=None, temperature=1.0, t_offsets=None, ws=None, stream=None):
     """z: [B, P, V] (or [N, V]) with tokens [B, P] ([N]); or packed [n_rows, V] with t_offsets [B+1] and tokens
-    [B, P].  tokens None: every row of z is swept, logprob and rank are None."""
+    [B, P].  tokens None: every row of z is swept, logprob and rank are None.  ws None: scratch is torch's."""
     V = z.shape[-1]
     if t_offsets is not None:
         if tokens is None or tokens.dim() != 2 or z.dim() != 2 or t_offsets.numel() != tokens.shape[0] + 1:
@@ -520,14 +543,18 @@ def sv_token_logprobs(z, tokens, logprob, lse=None, entropy=None, rank=None, top
     _outputs((B, P), logprob, lse, entropy, rank, flags)
     _outputs((B, P, n_top), top_token, top_logprob)
     addr, stride = _strided(z)
-    _check(lib.sv_token_logprobs(addr, stride, _ptr(t_offsets), n_rows, _ptr(tokens), B, P, V, _dtype_tag(z),
+    tag = _dtype_tag(z)
+    ws, ws_bytes = _row_scratch(ws, B * P, V, tag, n_top, stream)
+    _check(lib.sv_token_logprobs(addr, stride, _ptr(t_offsets), n_rows, _ptr(tokens), B, P, V, tag,
                                  temperature, n_top, _ptr(logprob), _ptr(lse), _ptr(entropy), _ptr(rank),
-                                 _ptr(top_token), _ptr(top_logprob), _ptr(flags), _stream(stream)))
+                                 _ptr(top_token), _ptr(top_logprob), _ptr(flags), _ptr(ws), ws_bytes,
+                                 _stream(stream)))
 
 
 def sv_token_logprobs_grad(z, tokens, g_logprob, dz, g_entropy=None, logprob=None, entropy=None, flags=None,
-                           temperature=1.0, stream=None):
-    """z, dz: [..., V], dz may be z; tokens, g_logprob, g_entropy, logprob, entropy: one entry per row."""
+                           temperature=1.0, ws=None, stream=None):
+    """z, dz: [..., V], dz may be z; tokens, g_logprob, g_entropy, logprob, entropy: one entry per row.
+    ws None: scratch is torch's."""
     V = z.shape[-1]
     rows = z.numel() // V if V else 0
     if dz.shape != z.shape or dz.dtype != z.dtype:
@@ -537,9 +564,11 @@ def sv_token_logprobs_grad(z, tokens, g_logprob, dz, g_entropy=None, logprob=Non
     _outputs((rows,), tokens, g_logprob, g_entropy, logprob, entropy, flags)
     addr, stride = _strided(z)
     d_addr, d_stride = _strided(dz)
-    _check(lib.sv_token_logprobs_grad(addr, stride, _ptr(tokens), rows, V, _dtype_tag(z), temperature,
+    tag = _dtype_tag(z)
+    ws, ws_bytes = _row_scratch(ws, rows, V, tag, 0, stream)
+    _check(lib.sv_token_logprobs_grad(addr, stride, _ptr(tokens), rows, V, tag, temperature,
                                       _ptr(g_logprob), _ptr(g_entropy), _ptr(logprob), _ptr(entropy), d_addr,
-                                      d_stride, _ptr(flags), _stream(stream)))
+                                      d_stride, _ptr(flags), _ptr(ws), ws_bytes, _stream(stream)))
 
 
 def sv_embedding(table, ids, out, scale=1.0, flags=None, stream=None):

@@ -23,6 +23,8 @@ OWN_FLAGS = {
     # over pairs they take dozens of the registers that hold the rows.  (Not for the others: the sweeps of
     # deep nuclei in warp.hip are 2 % slower with it.)
     "row_stats.hip": ["-mllvm", "-disable-machine-licm"],
+    # likewise: the logits of a row stay in registers from its sums to its gradient
+    "token_logprobs.hip": ["-mllvm", "-disable-machine-licm"],
 }
 
 
