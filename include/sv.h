@@ -654,7 +654,7 @@ int sv_token_logprobs_grad(const void* z, int64_t z_stride, const int32_t* token
  * Embedding rows of tokens: out[i, :] = scale * table[ids[i], :], formed in float32 and rounded once.
  *   table [V, D] dtype, ids [n] int32   in;   out [n, D] dtype   out (must not overlap table)
  *   flags_or_null [n] uint32            out  SV_FLAG_BAD_TOKEN for ids outside [0, V) other than -1
- * Rows of id -1 (padding) and of bad tokens are zeros.  n >= 0.
+ * Rows of id -1 (padding) and of bad tokens are zeros.  n >= 0.  Limits: V <= 16777216, D <= 1048576.
  */
 int sv_embedding(const void* table, const int32_t* ids, int n, int V, int D, int dtype, float scale,
                  void* out, uint32_t* flags_or_null, sv_stream_t stream);
@@ -671,7 +671,7 @@ size_t sv_embedding_grad_workspace_bytes(int n, int V, int D);
  *   grad_table [V, D] table_dtype    out  every row is written; with accumulate != 0 (a table
  *            tied to the output projection) only rows of tokens that occur are touched
  *   ws: at least sv_embedding_grad_workspace_bytes(n, V, D) bytes, 256-byte aligned
- * Limits: n <= SV_EMBEDDING_MAX_TOKENS, V <= 16777216.
+ * Limits: n <= SV_EMBEDDING_MAX_TOKENS, V <= 16777216, D <= 1048576.
  */
 int sv_embedding_grad(const void* grad_out, int dtype, const int32_t* ids, int n, int V, int D, float scale,
                       void* grad_table, int table_dtype, int accumulate,

@@ -1,8 +1,9 @@
 // sv_embedding: scaled rows of a table.  sv_embedding_grad: the gradient of that table.
 //
-// The gradient sorts the tokens (least significant digit first, kDigitBits bits a pass, stable) and then
-// sums, for every row of the table, the rows of the token's positions in their order: no atomics
-// on the result, the same bits from every call.  Positions whose id is no row sort behind all others.
+// The gradient sorts the tokens (least significant digit first, kDigitBits bits a pass, stable) and sums the rows of
+// equal tokens in the order of their positions: no atomics on the result, the same bits from every call.
+// Positions whose id is no row sort behind all others.  The sort occupies a few workgroups for some
+// microseconds a launch; the other workgroups of its launches write the table's zeros meanwhile.
 #include "sv_device.hpp"
 #include "sv_host.hpp"
 
@@ -28,13 +29,20 @@ __device__ __forceinline__ void load_chunk(const void* row, int D, int c, float 
 #pragma unroll
   for (int j = 0; j < kChunkCols; ++j) f[j] = c * kChunkCols + j < D ? load_elem<DT>(row, c * kChunkCols + j) : 0.f;
 }
-template <int DT>
+__device__ __forceinline__ void store_nt(void* row, int i, const u32x4& q) {      // not read again soon
+  __builtin_nontemporal_store(q, reinterpret_cast<u32x4_row*>(row) + i);
+}
+// ONCE: the results are more than the last-level cache keeps for a later reader, and are written past it.
+template <int DT, bool ONCE = true>
 __device__ __forceinline__ void store_chunk(void* row, int D, int c, const float (&f)[kChunkCols]) {
+  auto put = [&](int i, const u32x4& q) {
+    if constexpr (ONCE) store_nt(row, i, q);
+    else reinterpret_cast<u32x4_row*>(row)[i] = q;
+  };
   if constexpr (DT == DT_F32) {
     if ((c + 1) * kChunkCols <= D) {
-      u32x4_row* p = reinterpret_cast<u32x4_row*>(row) + 2 * c;
-      p[0] = u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
-      p[1] = u32x4{__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])};
+      put(2 * c, u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
+      put(2 * c + 1, u32x4{__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])});
       return;
     }
 #pragma unroll
@@ -43,7 +51,7 @@ __device__ __forceinline__ void store_chunk(void* row, int D, int c, const float
   } else {
     const u32x4 q = {pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
     if ((c + 1) * kChunkCols <= D) {
-      reinterpret_cast<u32x4_row*>(row)[c] = q;
+      put(c, q);
       return;
     }
 #pragma unroll
@@ -61,7 +69,7 @@ inline int lanes_per_row(int D) {
   return lanes;
 }
 
-template <int DT>
+template <int DT, bool ONCE>
 __global__ __launch_bounds__(kEmbThreads) void embedding_kernel(const void* table, const int32_t* ids, int n, int V,
                                                                 int D, float scale, void* out, uint32_t* flags,
                                                                 int lanes) {
@@ -77,16 +85,33 @@ __global__ __launch_bounds__(kEmbThreads) void embedding_kernel(const void* tabl
     if (given) load_chunk<DT>(from, D, c, f);
 #pragma unroll
     for (int j = 0; j < kChunkCols; ++j) f[j] = given ? f[j] * scale : 0.f;
-    store_chunk<DT>(to, D, c, f);
+    store_chunk<DT, ONCE>(to, D, c, f);
   }
 }
 
 // ---------------------------------------------------------------------------
-// stable sort of (token, position) by token
+// stable sort of (token, position) by token, and the zeros of the table
 // ---------------------------------------------------------------------------
 constexpr int kSortThreads = 1024, kSortPerLane = 4, kSortTile = kSortThreads * kSortPerLane;
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kSortWaves = kSortThreads / kWave;
+
+// A share of the table to be cleared by the workgroups of a launch from `first_block` on.
+struct Clear {
+  char* at;
+  size_t bytes;                // 0: nothing (accumulating)
+  int first_block;
+};
+constexpr size_t kClearBytes = 128 << 10;      // of one workgroup
+
+__device__ __forceinline__ void clear_share(const Clear& z) {
+  const size_t lo = (size_t)((int)blockIdx.x - z.first_block) * kClearBytes;
+  const size_t n = lo < z.bytes ? min(kClearBytes, z.bytes - lo) : 0;
+  const int vecs = (int)(n / 16);
+  for (int i = threadIdx.x; i < vecs; i += blockDim.x) store_nt(z.at + lo, i, u32x4{0, 0, 0, 0});
+  for (int i = vecs * 16 + threadIdx.x * 2; i < (int)n; i += blockDim.x * 2) *reinterpret_cast<uint16_t*>(z.at + lo + i) = 0;
+}
+inline unsigned clear_blocks(const Clear& z) { return (unsigned)((z.bytes + kClearBytes - 1) / kClearBytes); }
 
 struct SortPass {
   const int32_t* ids;          // first pass: the tokens as given
@@ -98,13 +123,13 @@ struct SortPass {
   int n, V, shift;
 };
 
+__device__ __forceinline__ uint32_t key_of_id(int id, int V) { return id >= 0 && id < V ? (uint32_t)id : (uint32_t)V; }
 __device__ __forceinline__ uint32_t sort_key(const SortPass& p, int i) {
-  if (!p.ids) return p.key_in[i];
-  const int id = p.ids[i];
-  return id >= 0 && id < p.V ? (uint32_t)id : (uint32_t)p.V;
+  return p.ids ? key_of_id(p.ids[i], p.V) : p.key_in[i];
 }
 
-__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortPass p) {
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortPass p, const Clear z) {
+  if ((int)blockIdx.x >= z.first_block) return clear_share(z);
   __shared__ int count[kDigits];
   const int tid = threadIdx.x;
   if (tid < kDigits) count[tid] = 0;
@@ -119,19 +144,67 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortPass
   if (tid < kDigits) p.hist[(size_t)blockIdx.x * kDigits + tid] = count[tid];
 }
 
-// A wavefront owns kSortPerLane * 64 consecutive entries of the tile.
-__global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortPass p, int tiles) {
-  __shared__ int count[kSortWaves][kDigits];
-  __shared__ int wave_sum[kSortWaves];
+struct SortScratch {
+  int count[kSortWaves][kDigits];
+  int wave_sum[kSortWaves];
+};
+
+// Ranks of a tile's entries among those of their wavefront with the same digit; count[wave][digit] are the wavefront's numbers.
+// Entries base .. base + 64 kSortPerLane - 1 of the tile are the wavefront's, `n` of the tile are there.
+__device__ __forceinline__ void rank_digits(const uint32_t (&key)[kSortPerLane], int shift, int base, int n,
+                                            int (&rank)[kSortPerLane], SortScratch& sm) {
+  const int lane = threadIdx.x & 63;
+  volatile int* mine = sm.count[threadIdx.x >> 6];
+#pragma unroll
+  for (int j = 0; j < kSortPerLane; ++j) {
+    const bool on = base + j * kWave + lane < n;
+    const int d = (key[j] >> shift) & (kDigits - 1);
+    uint64_t same = __ballot(on);
+#pragma unroll
+    for (int b = 0; b < kDigitBits; ++b) {
+      const uint64_t set = __ballot((d >> b) & 1);
+      same &= (d >> b) & 1 ? set : ~set;
+    }
+    const int below = __popcll(same & ((1ull << lane) - 1));
+    const int so_far = mine[d];
+    rank[j] = so_far + below;
+    __builtin_amdgcn_wave_barrier();                   // (every lane has read before one of them writes)
+    if (on && below == 0) mine[d] = so_far + __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// count[wave][digit] becomes where that wavefront's entries of the digit go: after those of smaller digits (`total` of each
+// digit in all, of the lane whose number it is), of earlier tiles (`before`) and of earlier wavefronts.
+__device__ __forceinline__ void place_digits(int before, int total, SortScratch& sm) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int i = tid; i < kSortWaves * kDigits; i += kSortThreads) (&count[0][0])[i] = 0;
+  const int scan = wave_scan_i32(tid < kDigits ? total : 0);
+  if (lane == kWave - 1) sm.wave_sum[wave] = scan;
   __syncthreads();
-  const int base = blockIdx.x * kSortTile + wave * kSortPerLane * kWave;
+  if (tid < kDigits) {
+    int to = scan - total + before;
+    for (int w = 0; w < wave; ++w) to += sm.wave_sum[w];
+    for (int w = 0; w < kSortWaves; ++w) {
+      const int c = sm.count[w][tid];
+      sm.count[w][tid] = to;
+      to += c;
+    }
+  }
+  __syncthreads();
+}
+
+__global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortPass p, int tiles, const Clear z) {
+  if ((int)blockIdx.x >= z.first_block) return clear_share(z);
+  __shared__ SortScratch sm;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int i = tid; i < kSortWaves * kDigits; i += kSortThreads) (&sm.count[0][0])[i] = 0;
+  __syncthreads();
+  const int tile = blockIdx.x * kSortTile, base = wave * kSortPerLane * kWave, n = min(kSortTile, p.n - tile);
   uint32_t key[kSortPerLane];
   int pos[kSortPerLane], rank[kSortPerLane];
 #pragma unroll
   for (int j = 0; j < kSortPerLane; ++j) {
-    const int i = base + j * kWave + lane;
+    const int i = tile + base + j * kWave + lane;
     key[j] = i < p.n ? sort_key(p, i) : 0;
     pos[j] = i < p.n ? (p.ids ? i : p.pos_in[i]) : 0;
   }
@@ -150,92 +223,111 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortPa
       }
     }
   }
-  volatile int* mine = count[wave];
+  rank_digits(key, p.shift, base, n, rank, sm);
+  place_digits(before, total, sm);
 #pragma unroll
   for (int j = 0; j < kSortPerLane; ++j) {
-    const bool on = base + j * kWave + lane < p.n;
-    const int d = (key[j] >> p.shift) & (kDigits - 1);
-    uint64_t same = __ballot(on);
-#pragma unroll
-    for (int b = 0; b < kDigitBits; ++b) {
-      const uint64_t set = __ballot((d >> b) & 1);
-      same &= (d >> b) & 1 ? set : ~set;
-    }
-    const int below = __popcll(same & ((1ull << lane) - 1));
-    const int so_far = mine[d];
-    rank[j] = so_far + below;
-    __builtin_amdgcn_wave_barrier();                   // (every lane has read before one of them writes)
-    if (on && below == 0) mine[d] = so_far + __popcll(same);
-    __builtin_amdgcn_wave_barrier();
-  }
-  __syncthreads();
-  // where a digit's entries of this tile start, and each wavefront's within them
-  int own = 0;
-  const int scan = wave_scan_i32(total);
-  if (lane == kWave - 1) wave_sum[wave] = scan;
-  __syncthreads();
-  int start = scan - total;
-  for (int w = 0; w < wave; ++w) start += wave_sum[w];
-  if (tid < kDigits) {
-    own = start + before;
-    for (int w = 0; w < kSortWaves; ++w) {
-      const int c = count[w][tid];
-      count[w][tid] = own;
-      own += c;
-    }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < kSortPerLane; ++j) {
-    if (base + j * kWave + lane >= p.n) continue;
-    const int to = count[wave][(key[j] >> p.shift) & (kDigits - 1)] + rank[j];
+    if (base + j * kWave + lane >= n) continue;
+    const int to = sm.count[wave][(key[j] >> p.shift) & (kDigits - 1)] + rank[j];
     p.key_out[to] = key[j];
     p.pos_out[to] = pos[j];
+  }
+}
+
+// Up to a tile of tokens: all passes in one workgroup.
+__global__ __launch_bounds__(kSortThreads) void sort_tile_kernel(const SortPass p, int bits, const Clear z) {
+  if ((int)blockIdx.x >= z.first_block) return clear_share(z);
+  __shared__ SortScratch sm;
+  __shared__ uint32_t keys[kSortTile];
+  __shared__ int32_t positions[kSortTile];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, base = wave * kSortPerLane * kWave;
+  uint32_t key[kSortPerLane];
+  int pos[kSortPerLane], rank[kSortPerLane];
+#pragma unroll
+  for (int j = 0; j < kSortPerLane; ++j) {
+    pos[j] = base + j * kWave + lane;
+    key[j] = pos[j] < p.n ? key_of_id(p.ids[pos[j]], p.V) : 0;
+  }
+#pragma unroll 1
+  for (int shift = 0; shift < bits; shift += kDigitBits) {
+    for (int i = tid; i < kSortWaves * kDigits; i += kSortThreads) (&sm.count[0][0])[i] = 0;
+    __syncthreads();
+    rank_digits(key, shift, base, p.n, rank, sm);
+    __syncthreads();
+    int total = 0;
+    if (tid < kDigits)
+      for (int w = 0; w < kSortWaves; ++w) total += sm.count[w][tid];
+    place_digits(0, total, sm);
+#pragma unroll
+    for (int j = 0; j < kSortPerLane; ++j) {
+      if (base + j * kWave + lane >= p.n) continue;
+      const int to = sm.count[wave][(key[j] >> shift) & (kDigits - 1)] + rank[j];
+      keys[to] = key[j];
+      positions[to] = pos[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kSortPerLane; ++j) {
+      const int i = base + j * kWave + lane;
+      if (i < p.n) { key[j] = keys[i]; pos[j] = positions[i]; }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kSortPerLane; ++j) {
+    const int i = base + j * kWave + lane;
+    if (i < p.n) { p.key_out[i] = key[j]; p.pos_out[i] = pos[j]; }
   }
 }
 
 // ---------------------------------------------------------------------------
 // sums
 // ---------------------------------------------------------------------------
-constexpr int kRounds = 8;              // rows of the table of one group of lanes
-constexpr int kMaxGroups = kEmbThreads / kMinLanes, kMaxRows = kRounds * kMaxGroups;
-constexpr int kPiece = 64;              // sorted positions summed by one group of lanes; a token with more is joined from pieces
-constexpr int kDirectTokens = 1024;     // up to here every workgroup looks through all tokens itself
-
-// Row of the table that group `group` of workgroup `block` has in round k: frequent tokens, whose numbers
-// often lie together, are spread over the workgroups.
-__device__ __forceinline__ long long row_of(int block, int group, int groups, int k) {
-  return ((long long)k * gridDim.x + block) * groups + group;
-}
+constexpr int kMaxGroups = kEmbThreads / kMinLanes;
+constexpr int kMaxPiece = 64;
+// Sorted positions that one group of lanes goes through, and the most a token may have to be summed by one group.
+inline int piece_of(int n) { return n <= 8192 ? 8 : kMaxPiece; }
 
 struct GradRows {
   const void* g;
   void* table;
-  const int32_t* ids;                   // direct form: the tokens as given
   const uint32_t* key;                  // sorted tokens
   const int32_t* pos;                   // their positions
-  int32_t *first, *last;                // [V] range of a token's sorted positions; of tokens that occur
-  float* part;                          // [pieces, 2, D] sums of a piece over a token that began before it / goes on after it
-  int n, V, D, lanes, accumulate;
+  int32_t* begins;                      // [pieces] 2 * the token that begins in the piece and has more than a piece of positions,
+                                        // + 1 if not with the piece's first; or -1
+  int32_t* last;                        // [V] end of the sorted positions of such a token
+  float* part;                          // [pieces, 2, D] sums over a piece of such a token: of the one that has the piece's
+                                        // first position, and of another that begins in the piece
+  int n, V, D, lanes, accumulate, piece;
   float scale;
 };
 
-// sum += the rows of positions at(lo) .. at(hi - 1), in this order; eight 16-byte loads of a lane are under way at a time.
-template <int DT, class At>
-__device__ __forceinline__ void add_rows(const GradRows& a, int c, int lo, int hi, At&& at, float (&sum)[kChunkCols]) {
-  constexpr int kVecs = kChunkCols / Elem<DT>::per_vec, kAhead = 8 / kVecs;
-  const char* g = static_cast<const char*>(a.g);
-  const size_t bytes = (size_t)a.D * Elem<DT>::bytes;
-  if ((c + 1) * kChunkCols > a.D) {                    // the last columns of a row that is no multiple of 8
-    for (int i = lo; i < hi; ++i) {
-      float f[kChunkCols];
-      load_chunk<DT>(g + at(i) * bytes, a.D, c, f);
+// The vectors of one chunk of a row.
+template <int DT>
+struct Chunk {
+  static constexpr int kVecs = kChunkCols / Elem<DT>::per_vec;
+  u32x4 q[kVecs];
+  __device__ __forceinline__ void load(const void* row, int D, int c) {
+    if ((c + 1) * kChunkCols <= D) {
 #pragma unroll
-      for (int j = 0; j < kChunkCols; ++j) sum[j] += f[j];
+      for (int k = 0; k < kVecs; ++k) q[k] = load_vec(row, c * kVecs + k);
+      return;
     }
-    return;
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) q[k] = u32x4{0, 0, 0, 0};
+    for (int j = c * kChunkCols; j < D; ++j) {         // the last columns of a row that is no multiple of 8
+      const int at = j - c * kChunkCols;
+      if constexpr (DT == DT_F32) {
+        const uint32_t x = static_cast<const uint32_t*>(row)[j];
+#pragma unroll
+        for (int k = 0; k < kChunkCols; ++k) q[k / 4][k % 4] = k == at ? x : q[k / 4][k % 4];
+      } else {
+        const uint32_t x = (uint32_t)static_cast<const uint16_t*>(row)[j] << (16 * (at & 1));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q[0][k] |= k == at / 2 ? x : 0;
+      }
+    }
   }
-  auto add = [&](const u32x4 (&q)[kVecs]) {
+  __device__ __forceinline__ void add_to(float (&sum)[kChunkCols]) const {
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
       float f[Elem<DT>::per_vec];
@@ -243,32 +335,11 @@ __device__ __forceinline__ void add_rows(const GradRows& a, int c, int lo, int h
 #pragma unroll
       for (int j = 0; j < Elem<DT>::per_vec; ++j) sum[k * Elem<DT>::per_vec + j] += f[j];
     }
-  };
-  auto load = [&](int i, u32x4 (&q)[kVecs]) {
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k) q[k] = load_vec(g + at(i) * bytes, c * kVecs + k);
-  };
-  int i = lo;
-  for (; i + kAhead <= hi; i += kAhead) {
-    u32x4 q[kAhead][kVecs];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) load(i + u, q[u]);
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) add(q[u]);
   }
-  if (i < hi) {                                        // the last, partial round
-    u32x4 q[kAhead - 1][kVecs];
-#pragma unroll
-    for (int u = 0; u < kAhead - 1; ++u)
-      if (i + u < hi) load(i + u, q[u]);
-#pragma unroll
-    for (int u = 0; u < kAhead - 1; ++u)
-      if (i + u < hi) add(q[u]);
-  }
-}
+};
 
 template <int DTW>
-__device__ __forceinline__ void store_sum(const GradRows& a, int v, int c, float (&sum)[kChunkCols]) {
+__device__ __forceinline__ void store_sum(const GradRows& a, uint32_t v, int c, float (&sum)[kChunkCols]) {
   char* to = static_cast<char*>(a.table) + (size_t)v * a.D * Elem<DTW>::bytes;
   float old[kChunkCols] = {};
   if (a.accumulate) load_chunk<DTW>(to, a.D, c, old);
@@ -277,167 +348,143 @@ __device__ __forceinline__ void store_sum(const GradRows& a, int v, int c, float
   store_chunk<DTW>(to, a.D, c, sum);
 }
 
-// Few tokens: one launch.  A workgroup picks the tokens of its rows out of all, in the order of their positions.
-template <int DTG, int DTW>
-__global__ __launch_bounds__(kEmbThreads) void embedding_grad_direct_kernel(const GradRows a) {
-  constexpr int kWaves = kEmbThreads / kWave, kLooks = kDirectTokens / kEmbThreads;
-  __shared__ uint32_t found[kDirectTokens];            // row of the workgroup << 16 | position
-  __shared__ uint16_t pos[kDirectTokens];              // positions by row, then by position
-  __shared__ uint16_t start[kMaxRows], end[kMaxRows];
-  __shared__ int count[kWaves];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int groups = kEmbThreads / a.lanes;
-  for (int r = threadIdx.x; r < kRounds * groups; r += kEmbThreads) start[r] = end[r] = 0;
-  // a wavefront looks through a run of tokens
-  uint64_t hit[kLooks];
-  int row[kLooks], mine = 0;
-#pragma unroll
-  for (int j = 0; j < kLooks; ++j) {
-    const int i = (wave * kLooks + j) * kWave + lane;
-    const int id = i < a.n ? a.ids[i] : -1;
-    const uint32_t unit = (uint32_t)max(id, 0) / (uint32_t)groups, k = unit / gridDim.x;
-    row[j] = (int)k * groups + max(id, 0) % groups;
-    hit[j] = __ballot(id >= 0 && id < a.V && unit - k * gridDim.x == blockIdx.x);
-    mine += __popcll(hit[j]);
-  }
-  if (lane == 0) count[wave] = mine;
-  __syncthreads();
-  int to = 0, total = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    to += w < wave ? count[w] : 0;
-    total += count[w];
-  }
-#pragma unroll
-  for (int j = 0; j < kLooks; ++j) {
-    if (hit[j] >> lane & 1)
-      found[to + __popcll(hit[j] & ((1ull << lane) - 1))] = (uint32_t)row[j] << 16 | ((wave * kLooks + j) * kWave + lane);
-    to += __popcll(hit[j]);
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < total; i += kEmbThreads) {
-    const uint32_t f = found[i], r = f >> 16;
-    int smaller = 0, same = 0, earlier = 0;
-    for (int m = 0; m < total; ++m) {
-      const uint32_t o = found[m] >> 16;
-      smaller += o < r;
-      same += o == r;
-      earlier += o == r && m < i;
+// What a group of lanes has to do: positions from .. to - 1 of the sorted list, the first token's sum (if it is joined) to slot
+// 0 of the piece, the last one's (if it is) to slot 1.
+struct Piece {
+  int from, to;
+  bool joins_first, joins_last;
+};
+// keys of the piece at key[0 ..], and a piece before and after it; ~0 where there is no position.
+__device__ __forceinline__ Piece look_at(const uint32_t* key, int piece, uint32_t V) {
+  auto end_of = [&](int lo, int hi, uint32_t k, bool after) {      // first entry of at least k, or above it
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (key[mid] < k || (after && key[mid] == k)) lo = mid + 1; else hi = mid;
     }
-    pos[smaller + earlier] = (uint16_t)f;
-    if (earlier == 0) { start[r] = (uint16_t)smaller; end[r] = (uint16_t)(smaller + same); }
+    return lo;
+  };
+  const int size = end_of(0, piece, V, false);         // of it, positions with a token
+  Piece p = {0, size, false, false};
+  if (size == 0) return p;
+  const uint32_t k0 = key[0], k1 = key[size - 1];
+  const int end0 = end_of(0, 2 * piece, k0, true);
+  p.joins_first = end0 > piece || key[end0 - 1 - piece] == k0;
+  if (key[-1] == k0 && !p.joins_first) p.from = min(end0, size);   // summed with the piece it begins in
+  if (k1 == k0) {
+    p.to = p.joins_first ? size : max(end0, p.from);
+    if (key[-1] == k0 && !p.joins_first) p.to = p.from;
+    return p;
   }
-  __syncthreads();
-  const int l = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes;
-  for (int k = 0; k < kRounds; ++k) {
-    const long long v = row_of(blockIdx.x, group, groups, k);
-    if (v >= a.V) break;
-    const int lo = start[k * groups + group], hi = end[k * groups + group];
-    if (lo == hi && a.accumulate) continue;
-    for (int c = l; c * kChunkCols < a.D; c += a.lanes) {
-      float sum[kChunkCols] = {};
-      add_rows<DTG>(a, c, lo, hi, [&](int i) { return (size_t)pos[i]; }, sum);
-      store_sum<DTW>(a, (int)v, c, sum);
-    }
-  }
+  const int begin1 = end_of(0, size, k1, false);
+  p.joins_last = key[begin1 + piece] == k1;
+  if (!p.joins_last) p.to = end_of(begin1, begin1 + piece, k1, true);
+  return p;
 }
 
-// Many tokens, first launch: where the tokens' sorted positions begin and end, and the sums of pieces of those
-// that have more than kPiece.  Such a token is in a piece from its first position on, or up to its last.
-template <int DTG>
+// Goes through the sorted positions, the rows of eight of them under way at a time whatever tokens they belong to, and writes a
+// token's row where its positions end.
+template <int DTG, int DTW>
 __global__ __launch_bounds__(kEmbThreads) void embedding_grad_pieces_kernel(const GradRows a) {
-  __shared__ uint32_t key[kMaxGroups * kPiece];
-  __shared__ int32_t pos[kMaxGroups * kPiece];
-  const int pieces = kEmbThreads / a.lanes;            // of the workgroup
-  const long long base = (long long)blockIdx.x * pieces * kPiece;
-  for (int j = threadIdx.x; j < pieces * kPiece && base + j < a.n; j += kEmbThreads) {
-    const int i = (int)(base + j);
-    const uint32_t k = a.key[i];
-    const uint32_t left = i > 0 ? a.key[i - 1] : ~0u, right = i < a.n - 1 ? a.key[i + 1] : ~0u;
-    key[j] = k;
-    pos[j] = a.pos[i];
-    if (k >= (uint32_t)a.V) continue;
-    if (left != k) a.first[k] = i;
-    if (right != k) a.last[k] = i + 1;
+  constexpr int kAhead = 8;
+  __shared__ uint32_t key[(kMaxGroups + 2) * kMaxPiece + 1];
+  __shared__ int32_t pos[(kMaxGroups + 1) * kMaxPiece];
+  const int groups = kEmbThreads / a.lanes, piece = a.piece;
+  const long long base = (long long)blockIdx.x * groups * piece;
+  for (int j = threadIdx.x; j < (groups + 2) * piece; j += kEmbThreads) {
+    const long long i = base - piece + j;
+    key[j] = i >= 0 && i < a.n ? a.key[i] : ~0u;
+    if (j >= piece) pos[j - piece] = i < a.n ? a.pos[i] : 0;
   }
   __syncthreads();
   const int l = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes;
-  const long long lo = base + group * kPiece;
-  if (lo >= a.n) return;
-  const int size = (int)min((long long)kPiece, a.n - lo);
-  const uint32_t* mine = key + group * kPiece;
-  auto sum_piece = [&](int from, int to, int slot) {
-    for (int c = l; c * kChunkCols < a.D; c += a.lanes) {
-      float sum[kChunkCols] = {};
-      add_rows<DTG>(a, c, from, to, [&](int i) { return (size_t)pos[group * kPiece + i]; }, sum);
-      store_chunk<DT_F32>(a.part + ((size_t)(lo / kPiece) * 2 + slot) * a.D, a.D, c, sum);
+  const uint32_t* k = key + (group + 1) * piece;
+  const int32_t* at = pos + group * piece;
+  const Piece p = look_at(k, piece, (uint32_t)a.V);
+  if (l == 0 && base + group * piece < a.n)
+    a.begins[base / piece + group] = p.joins_last ? (int)k[p.to - 1] * 2 + 1 : p.joins_first && k[-1] != k[0] ? (int)k[0] * 2 : -1;
+  if (p.from >= p.to) return;
+  const char* g = static_cast<const char*>(a.g);
+  const size_t bytes = (size_t)a.D * Elem<DTG>::bytes;
+  for (int c = l; c * kChunkCols < a.D; c += a.lanes) {
+    float sum[kChunkCols] = {};
+    for (int i = p.from; i < p.to; i += kAhead) {
+      Chunk<DTG> q[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) q[u].load(g + at[min(i + u, p.to - 1)] * bytes, a.D, c);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (i + u >= p.to) break;
+        q[u].add_to(sum);
+        const uint32_t v = k[i + u];
+        if (i + u + 1 < p.to && k[i + u + 1] == v) continue;
+        const bool first = p.joins_first && v == k[0], last = p.joins_last && i + u + 1 == p.to;
+        if (first || last) {
+          store_chunk<DT_F32>(a.part + ((size_t)(base / piece + group) * 2 + (first ? 0 : 1)) * a.D, a.D, c, sum);
+          // its last position: what the join looks for
+          if (l == 0 && c == 0 && k[i + u + 1] != v) a.last[v] = (int)(base + group * piece) + i + u + 1;
+        } else {
+          store_sum<DTW>(a, v, c, sum);
+        }
+#pragma unroll
+        for (int j = 0; j < kChunkCols; ++j) sum[j] = 0.f;
+      }
     }
-  };
-  auto search = [&](uint32_t k) {                      // first entry of the piece with a key of at least k
-    int x = 0, y = size;
-    while (x < y) {
-      const int mid = (x + y) / 2;
-      if (mine[mid] < k) x = mid + 1; else y = mid;
-    }
-    return x;
-  };
-  auto has = [&](long long i, uint32_t k) { return i >= 0 && i < a.n && a.key[i] == k; };
-  const uint32_t k0 = mine[0], k1 = mine[size - 1];
-  const int to = search(k0 + 1), from = search(k1);
-  // more than kPiece positions: the first token's begin before the piece, or fill it and go on
-  if (k0 < (uint32_t)a.V && (has(lo + to - 1 - kPiece, k0) || (to == kPiece && has(lo + kPiece, k0)))) sum_piece(0, to, 0);
-  if (to < size && k1 < (uint32_t)a.V && has(lo + from + kPiece, k1)) sum_piece(from, size, 1);
+  }
 }
 
-// Second launch: every row of the table.
-template <int DTG, int DTW>
-__global__ __launch_bounds__(kEmbThreads) void embedding_grad_rows_kernel(const GradRows a) {
-  __shared__ int start[kMaxRows], end[kMaxRows];
-  const int groups = kEmbThreads / a.lanes;
-  for (int r = threadIdx.x; r < kRounds * groups; r += kEmbThreads) {
-    // what the arrays hold for a token that does not occur is from elsewhere: no sorted position has that token
-    const long long v = row_of(blockIdx.x, r % groups, groups, r / groups);
-    const int lo = v < a.V ? a.first[v] : -1;
-    const bool occurs = lo >= 0 && lo < a.n && a.key[lo] == (uint32_t)v;
-    start[r] = occurs ? lo : 0;
-    end[r] = occurs ? a.last[v] : 0;
-  }
-  __syncthreads();
-  const int l = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes;
-  for (int k = 0; k < kRounds; ++k) {
-    const long long v = row_of(blockIdx.x, group, groups, k);
-    if (v >= a.V) break;
-    const int lo = start[k * groups + group], hi = end[k * groups + group];
-    if (lo == hi && a.accumulate) continue;
-    for (int c = l; c * kChunkCols < a.D; c += a.lanes) {
-      float sum[kChunkCols] = {};
-      if (hi - lo <= kPiece) {
-        add_rows<DTG>(a, c, lo, hi, [&](int i) { return (size_t)a.pos[i]; }, sum);
-      } else {
-        GradRows parts = {};
-        parts.g = a.part;
-        parts.D = a.D;
-        const int p0 = lo / kPiece, slot0 = lo % kPiece != 0;
-        add_rows<DT_F32>(parts, c, p0, (hi - 1) / kPiece + 1, [&](int p) { return (size_t)p * 2 + (p == p0 ? slot0 : 0); },
-                         sum);
+// Rows of tokens with more than a piece of positions: kJoin groups of up to 64 lanes to 64 chunks of each (a frequent token's
+// partial sums are a megabyte, more than one compute unit reads in the time that the rest takes), every group a run of
+// the partial sums, then added in order.
+constexpr int kJoin = 4, kJoinLanes = 64;
+template <int DTW>
+__global__ __launch_bounds__(kEmbThreads * kJoin) void embedding_grad_join_kernel(const GradRows a) {
+  __shared__ float sums[kJoin - 1][kEmbThreads][kChunkCols + 1];
+  const int lanes = min(a.lanes, kJoinLanes), groups = kEmbThreads / lanes, t = threadIdx.x % kEmbThreads;
+  const int share = threadIdx.x / kEmbThreads, c = blockIdx.y * lanes + t % lanes;
+  const long long p0 = (long long)blockIdx.x * groups + t / lanes;
+  const int begins = p0 * a.piece < a.n && c * kChunkCols < a.D ? a.begins[p0] : -1;
+  if (!__syncthreads_or(begins >= 0)) return;
+  float sum[kChunkCols] = {};
+  const uint32_t v = (uint32_t)begins >> 1;
+  if (begins >= 0) {
+    const int parts = (int)((a.last[v] - 1) / a.piece - p0) + 1, per = (parts + kJoin - 1) / kJoin;
+    const int from = min(share * per, parts), to = min(from + per, parts);
+    constexpr int kAhead = 8;
+    for (int i = from; i < to; i += kAhead) {
+      Chunk<DT_F32> q[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int j = min(i + u, to - 1);
+        q[u].load(a.part + ((size_t)(p0 + j) * 2 + (j == 0 ? begins & 1 : 0)) * a.D, a.D, c);
       }
-      store_sum<DTW>(a, (int)v, c, sum);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (i + u < to) q[u].add_to(sum);
     }
   }
+  if (share > 0)
+#pragma unroll
+    for (int j = 0; j < kChunkCols; ++j) sums[share - 1][t][j] = sum[j];
+  __syncthreads();
+  if (share > 0 || begins < 0) return;
+#pragma unroll
+  for (int s = 0; s < kJoin - 1; ++s)
+#pragma unroll
+    for (int j = 0; j < kChunkCols; ++j) sum[j] += sums[s][t][j];
+  store_sum<DTW>(a, v, c, sum);
 }
 
 struct EmbeddingWs {
   uint32_t* key[2];
   int32_t* pos[2];
   int32_t* hist;
-  int32_t *first, *last;
+  int32_t *begins, *last;
   float* part;
   size_t bytes;
 };
 inline int sort_tiles(int n) { return (n + kSortTile - 1) / kSortTile; }
 inline EmbeddingWs carve_embedding_ws(void* base, int n, int V, int D) {
   EmbeddingWs w = {};
-  if (n <= kDirectTokens) return w;
   char* p = static_cast<char*>(base);
   size_t off = 0;
   auto take = [&](size_t bytes) { char* q = p ? p + off : nullptr; off += ws_round(bytes); return q; };
@@ -446,26 +493,23 @@ inline EmbeddingWs carve_embedding_ws(void* base, int n, int V, int D) {
     w.pos[i] = reinterpret_cast<int32_t*>(take((size_t)n * 4));
   }
   w.hist = reinterpret_cast<int32_t*>(take((size_t)sort_tiles(n) * kDigits * 4));
-  w.first = reinterpret_cast<int32_t*>(take((size_t)V * 4));
+  w.begins = reinterpret_cast<int32_t*>(take((size_t)((n + piece_of(n) - 1) / piece_of(n)) * 4));
   w.last = reinterpret_cast<int32_t*>(take((size_t)V * 4));
-  w.part = reinterpret_cast<float*>(take((size_t)((n + kPiece - 1) / kPiece) * 2 * D * 4));
+  w.part = reinterpret_cast<float*>(take((size_t)((n + piece_of(n) - 1) / piece_of(n)) * 2 * D * 4));
   w.bytes = off;
   return w;
 }
 
-template <int DTG>
-void launch_grad_rows(const GradRows& a, int table_dtype, hipStream_t st) {
-  const int rows = kEmbThreads / a.lanes * kRounds;
-  const dim3 grid((unsigned)((a.V + rows - 1) / rows)), block(kEmbThreads);
-  if (!a.key) {                                          // (of no tokens at all the list may be NULL as well)
-    if (table_dtype == SV_F32) hipLaunchKernelGGL((embedding_grad_direct_kernel<DTG, DT_F32>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((embedding_grad_direct_kernel<DTG, DT_BF16>), grid, block, 0, st, a);
-    return;
-  }
-  const int per = kEmbThreads / a.lanes * kPiece;
-  hipLaunchKernelGGL(embedding_grad_pieces_kernel<DTG>, dim3((unsigned)((a.n + per - 1) / per)), block, 0, st, a);
-  if (table_dtype == SV_F32) hipLaunchKernelGGL((embedding_grad_rows_kernel<DTG, DT_F32>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((embedding_grad_rows_kernel<DTG, DT_BF16>), grid, block, 0, st, a);
+template <int DTG, int DTW>
+void launch_sums(const GradRows& a, hipStream_t st) {
+  const int per = kEmbThreads / a.lanes * a.piece;
+  const dim3 grid((unsigned)(((long long)a.n + per - 1) / per));
+  hipLaunchKernelGGL((embedding_grad_pieces_kernel<DTG, DTW>), grid, dim3(kEmbThreads), 0, st, a);
+  if (a.n <= a.piece) return;
+  const int lanes = a.lanes < kJoinLanes ? a.lanes : kJoinLanes, join_per = kEmbThreads / lanes * a.piece;
+  const int chunks = (a.D + kChunkCols - 1) / kChunkCols;
+  const dim3 join((unsigned)(((long long)a.n + join_per - 1) / join_per), (unsigned)((chunks + lanes - 1) / lanes));
+  hipLaunchKernelGGL(embedding_grad_join_kernel<DTW>, join, dim3(kEmbThreads * kJoin), 0, st, a);
 }
 
 }  // namespace sv
@@ -475,7 +519,7 @@ extern "C" int sv_embedding(const void* table, const int32_t* ids, int n, int V,
   using namespace sv;
   SV_REQUIRE(dtype == SV_F32 || dtype == SV_BF16, SV_ERR_DTYPE);
   SV_REQUIRE(n >= 0 && V >= 1 && D >= 1, SV_ERR_INVALID_ARG);
-  SV_REQUIRE(V <= (1 << 24) && D <= (1 << 24), SV_ERR_TOO_LARGE);
+  SV_REQUIRE(V <= (1 << 24) && D <= (1 << 20), SV_ERR_TOO_LARGE);
   if (n == 0) return SV_OK;
   SV_REQUIRE(table && ids && out, SV_ERR_NULL);
   SV_REQUIRE(is_aligned(table, elem_bytes(dtype)) && is_aligned(out, elem_bytes(dtype)) && is_aligned(ids, 4) &&
@@ -484,15 +528,17 @@ extern "C" int sv_embedding(const void* table, const int32_t* ids, int n, int V,
   const int lanes = lanes_per_row(D), rows = kEmbThreads / lanes;
   const dim3 grid((unsigned)(((long long)n + rows - 1) / rows)), block(kEmbThreads);
   hipStream_t st = as_stream(stream);
-  if (dtype == SV_F32)
-    hipLaunchKernelGGL(embedding_kernel<DT_F32>, grid, block, 0, st, table, ids, n, V, D, scale, out, flags_or_null, lanes);
-  else
-    hipLaunchKernelGGL(embedding_kernel<DT_BF16>, grid, block, 0, st, table, ids, n, V, D, scale, out, flags_or_null, lanes);
+  const bool once = 2LL * n * D * elem_bytes(dtype) > kCacheBytes;      // 16384 x 4096 bf16: 33 us so, 42 us through the cache
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, st, table, ids, n, V, D, scale, out, flags_or_null, lanes);
+  };
+  if (dtype == SV_F32) once ? go(embedding_kernel<DT_F32, true>) : go(embedding_kernel<DT_F32, false>);
+  else once ? go(embedding_kernel<DT_BF16, true>) : go(embedding_kernel<DT_BF16, false>);
   return launch_status();
 }
 
 extern "C" size_t sv_embedding_grad_workspace_bytes(int n, int V, int D) {
-  if (n < 0 || n > SV_EMBEDDING_MAX_TOKENS || V < 1 || V > (1 << 24) || D < 1 || D > (1 << 24)) return 0;
+  if (n < 0 || n > SV_EMBEDDING_MAX_TOKENS || V < 1 || V > (1 << 24) || D < 1 || D > (1 << 20)) return 0;
   const size_t need = sv::carve_embedding_ws(nullptr, n, V, D).bytes;
   return need < sv::kWsAlign ? sv::kWsAlign : need;
 }
@@ -503,7 +549,7 @@ extern "C" int sv_embedding_grad(const void* grad_out, int dtype, const int32_t*
   using namespace sv;
   SV_REQUIRE((dtype == SV_F32 || dtype == SV_BF16) && (table_dtype == SV_F32 || table_dtype == SV_BF16), SV_ERR_DTYPE);
   SV_REQUIRE(n >= 0 && V >= 1 && D >= 1, SV_ERR_INVALID_ARG);
-  SV_REQUIRE(n <= SV_EMBEDDING_MAX_TOKENS && V <= (1 << 24) && D <= (1 << 24), SV_ERR_TOO_LARGE);
+  SV_REQUIRE(n <= SV_EMBEDDING_MAX_TOKENS && V <= (1 << 24) && D <= (1 << 20), SV_ERR_TOO_LARGE);
   if (n == 0 && accumulate) return SV_OK;
   SV_REQUIRE(grad_table && (n == 0 || (grad_out && ids)), SV_ERR_NULL);
   SV_REQUIRE(is_aligned(grad_out, elem_bytes(dtype)) && is_aligned(grad_table, elem_bytes(table_dtype)) &&
@@ -511,22 +557,44 @@ extern "C" int sv_embedding_grad(const void* grad_out, int dtype, const int32_t*
              SV_ERR_ALIGN);
   SV_REQUIRE(ws && is_aligned(ws, kWsAlign) && ws_bytes >= sv_embedding_grad_workspace_bytes(n, V, D), SV_ERR_WORKSPACE);
   hipStream_t st = as_stream(stream);
-  GradRows a = {grad_out, grad_table, ids, nullptr, nullptr, nullptr, nullptr, nullptr, n, V, D, lanes_per_row(D),
-                accumulate != 0, scale};
-  if (n > kDirectTokens) {
-    const EmbeddingWs w = carve_embedding_ws(ws, n, V, D);
-    int bits = 1, at = 0;
-    while ((V >> bits) != 0) ++bits;                     // keys 0 .. V
+  const EmbeddingWs w = carve_embedding_ws(ws, n, V, D);
+  int bits = 1, at = 0;
+  while ((V >> bits) != 0) ++bits;                       // keys 0 .. V
+  // the table's zeros, in equal shares to the launches of the sort
+  const int passes = (bits + kDigitBits - 1) / kDigitBits, tiles = sort_tiles(n), launches = tiles <= 1 ? 1 : 2 * passes;
+  char* zeros = static_cast<char*>(grad_table);
+  size_t left = accumulate ? 0 : (size_t)V * D * elem_bytes(table_dtype);
+  const size_t share = (left / launches + kClearBytes - 1) / kClearBytes * kClearBytes;
+  auto clear = [&](int first_block) {
+    const Clear z = {zeros, share < left ? share : left, first_block};
+    zeros += z.bytes;
+    left -= z.bytes;
+    return z;
+  };
+  const dim3 block(kSortThreads);
+  if (tiles <= 1) {
+    const SortPass p = {ids, nullptr, nullptr, w.key[0], w.pos[0], nullptr, n, V, 0};
+    const Clear z = clear(n > 0 ? 1 : 0);
+    hipLaunchKernelGGL(sort_tile_kernel, dim3(z.first_block + clear_blocks(z)), block, 0, st, p, bits, z);
+  } else {
     for (int shift = 0; shift < bits; shift += kDigitBits) {
       const SortPass p = {shift == 0 ? ids : nullptr, w.key[at], w.pos[at], w.key[1 - at], w.pos[1 - at], w.hist, n, V, shift};
-      const dim3 grid((unsigned)sort_tiles(n)), block(kSortThreads);
-      hipLaunchKernelGGL(sort_count_kernel, grid, block, 0, st, p);
-      hipLaunchKernelGGL(sort_scatter_kernel, grid, block, 0, st, p, sort_tiles(n));
+      const Clear z0 = clear(tiles);
+      hipLaunchKernelGGL(sort_count_kernel, dim3(tiles + clear_blocks(z0)), block, 0, st, p, z0);
+      const Clear z1 = clear(tiles);
+      hipLaunchKernelGGL(sort_scatter_kernel, dim3(tiles + clear_blocks(z1)), block, 0, st, p, tiles, z1);
       at = 1 - at;
     }
-    a.key = w.key[at]; a.pos = w.pos[at]; a.first = w.first; a.last = w.last; a.part = w.part;
   }
-  if (dtype == SV_F32) launch_grad_rows<DT_F32>(a, table_dtype, st);
-  else launch_grad_rows<DT_BF16>(a, table_dtype, st);
+  if (n == 0) return launch_status();
+  const GradRows a = {grad_out, grad_table, w.key[at], w.pos[at], w.begins, w.last, w.part, n, V, D, lanes_per_row(D),
+                      accumulate != 0, piece_of(n), scale};
+  if (dtype == SV_F32) {
+    if (table_dtype == SV_F32) launch_sums<DT_F32, DT_F32>(a, st);
+    else launch_sums<DT_F32, DT_BF16>(a, st);
+  } else {
+    if (table_dtype == SV_F32) launch_sums<DT_BF16, DT_F32>(a, st);
+    else launch_sums<DT_BF16, DT_BF16>(a, st);
+  }
   return launch_status();
 }

@@ -2,16 +2,18 @@
 // what the norm says.
 //
 // The tensors are cut into granules; a launch takes the addresses of up to kTensors of them by
-// value.  A workgroup walks through granules one grid apart and leaves one fp64 sum of squares; one
-// workgroup adds those up in a fixed order.  Bound by the bytes: the gradients are read twice (the
-// factor is not known before all have been read) and written once.
+// value.  A workgroup walks through granules one grid apart and leaves one fp64 sum of squares.  Up to one launch of
+// tensors, every workgroup of the second launch adds those up itself, in the same order; of more, one workgroup
+// does in a launch between.  Bound by the bytes: the gradients are read twice (the factor is not known before
+// all have been read) and written once.  The second reading goes backwards: what the first one read last is still in
+// the last-level cache.
 #include "sv_device.hpp"
 #include "sv_host.hpp"
 
 namespace sv {
 
 constexpr int kTensors = 120;           // tensors of one launch: 3.8 KB of kernel arguments
-constexpr int kGranuleElems = 16384;
+constexpr int kGranuleElems = 8192;
 constexpr int kNormGroups = 1024;       // workgroups of a launch at most
 constexpr int kNormThreads = 256;
 
@@ -40,19 +42,29 @@ __device__ __forceinline__ int tensor_of(const TensorBatch& b, uint32_t granule)
 
 template <int DT>
 __device__ __forceinline__ double squares(const void* p, int n) {
-  constexpr int EPV = Elem<DT>::per_vec;
-  double s = 0.0;
-  for (int i = threadIdx.x; i < n / EPV; i += kNormThreads) {
+  constexpr int EPV = Elem<DT>::per_vec, U = 4;
+  const int vecs = n / EPV, tid = threadIdx.x;
+  double s[2] = {0.0, 0.0};
+  auto add = [&](const u32x4& q) {
     float f[EPV];
-    unpack<DT>(load_vec(p, i), f);
+    unpack<DT>(q, f);
 #pragma unroll
-    for (int j = 0; j < EPV; ++j) s = __builtin_fma((double)f[j], (double)f[j], s);
+    for (int j = 0; j < EPV; ++j) s[j & 1] = __builtin_fma((double)f[j], (double)f[j], s[j & 1]);
+  };
+  int i = tid;
+  for (; i + (U - 1) * kNormThreads < vecs; i += U * kNormThreads) {
+    u32x4 q[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) q[u] = load_vec(p, i + u * kNormThreads);
+#pragma unroll
+    for (int u = 0; u < U; ++u) add(q[u]);
   }
-  for (int i = n / EPV * EPV + threadIdx.x; i < n; i += kNormThreads) {
-    const double x = (double)load_elem<DT>(p, i);
-    s = __builtin_fma(x, x, s);
+  for (; i < vecs; i += kNormThreads) add(load_vec(p, i));
+  for (int k = vecs * EPV + tid; k < n; k += kNormThreads) {
+    const double x = (double)load_elem<DT>(p, k);
+    s[0] = __builtin_fma(x, x, s[0]);
   }
-  return s;
+  return s[0] + s[1];
 }
 
 __global__ __launch_bounds__(kNormThreads) void grad_norm_kernel(const TensorBatch b, double* part) {
@@ -69,58 +81,99 @@ __global__ __launch_bounds__(kNormThreads) void grad_norm_kernel(const TensorBat
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
-// One workgroup: norm, flag and factor from the partial sums.
-__global__ __launch_bounds__(1024) void grad_norm_finish_kernel(const double* part, int n, float max_norm, float* norm,
-                                                                uint32_t* flag, float* factor) {
-  __shared__ BlockScratch sm;
+// What the partial sums say: the norm and, if `writes`, its outputs; the factor in every lane.
+__device__ __forceinline__ float finish_norm(const double* part, int n, float max_norm, float* norm, uint32_t* flag,
+                                             bool writes, BlockScratch& sm) {
   double s = 0.0;
-  for (int i = threadIdx.x; i < n; i += 1024) s += part[i];
-  s = block_sum_f64(s, sm);
-  if (threadIdx.x != 0) return;
-  const float x = (float)sqrt(s);
+  for (int i = threadIdx.x; i < n; i += kNormThreads) s += part[i];
+  const float x = (float)sqrt(block_sum_f64(s, sm));
   const bool fine = isfinite(x);
-  *norm = x;
-  if (flag) *flag = fine ? 0 : SV_FLAG_NONFINITE;
-  *factor = fine ? (float)fmin(1.0, (double)max_norm / ((double)x + 1e-6)) : 1.f;
+  if (writes && threadIdx.x == 0) {
+    *norm = x;
+    if (flag) *flag = fine ? 0 : SV_FLAG_NONFINITE;
+  }
+  return fine ? (float)fmin(1.0, (double)max_norm / ((double)x + 1e-6)) : 1.f;
 }
 
-template <int DT, int DO>
+__global__ __launch_bounds__(kNormThreads) void grad_norm_finish_kernel(const double* part, int n, float max_norm,
+                                                                        float* norm, uint32_t* flag, float* factor) {
+  __shared__ BlockScratch sm;
+  const float by = finish_norm(part, n, max_norm, norm, flag, true, sm);
+  if (threadIdx.x == 0) *factor = by;
+}
+
+// ONCE: the results are more than the last-level cache keeps for a later reader, and are written past it.
+template <int DT, int DO, bool ONCE>
 __device__ __forceinline__ void scale_granule(const void* p, void* o, int n, float by) {
-  constexpr int EPV = Elem<DT_BF16>::per_vec;          // 8 elements a step whatever the types
-  for (int i = threadIdx.x; i < n / EPV; i += kNormThreads) {
-    float f[EPV];
+  constexpr int kIn = DT == DT_BF16 ? 1 : 2, U = 4;    // 8 elements a step whatever the types
+  const int steps = n / 8, tid = threadIdx.x;
+  auto load = [&](int i, u32x4 (&q)[kIn]) {
+#pragma unroll
+    for (int k = 0; k < kIn; ++k) q[k] = load_vec(p, kIn * i + k);
+  };
+  auto store = [&](int i, const u32x4 (&q)[kIn]) {
+    float f[8];
     if constexpr (DT == DT_BF16) {
-      unpack<DT_BF16>(load_vec(p, i), f);
+      unpack<DT_BF16>(q[0], f);
     } else {
-      const u32x4 a = load_vec(p, 2 * i), c = load_vec(p, 2 * i + 1);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) { f[j] = __uint_as_float(a[j]); f[4 + j] = __uint_as_float(c[j]); }
+      for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(q[j >> 2][j & 3]);
     }
 #pragma unroll
-    for (int j = 0; j < EPV; ++j) f[j] *= by;
+    for (int j = 0; j < 8; ++j) f[j] *= by;
+    u32x4 r[2];
+    auto put = [&](const u32x4& v, int at) {
+      u32x4_row* to = reinterpret_cast<u32x4_row*>(o) + at;
+      if constexpr (ONCE) __builtin_nontemporal_store(v, to);
+      else *to = v;
+    };
     if constexpr (DO == DT_BF16) {
-      u32x4 q;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) q[j] = pack_bf16(f[2 * j], f[2 * j + 1]);
-      reinterpret_cast<u32x4_row*>(o)[i] = q;
+      for (int j = 0; j < 4; ++j) r[0][j] = pack_bf16(f[2 * j], f[2 * j + 1]);
+      put(r[0], i);
     } else {
-      u32x4 q[2];
 #pragma unroll
-      for (int j = 0; j < EPV; ++j) q[j >> 2][j & 3] = __float_as_uint(f[j]);
-      reinterpret_cast<u32x4_row*>(o)[2 * i] = q[0];
-      reinterpret_cast<u32x4_row*>(o)[2 * i + 1] = q[1];
+      for (int j = 0; j < 8; ++j) r[j >> 2][j & 3] = __float_as_uint(f[j]);
+      put(r[0], 2 * i);
+      put(r[1], 2 * i + 1);
     }
+  };
+  int i = tid;
+  for (; i + (U - 1) * kNormThreads < steps; i += U * kNormThreads) {
+    u32x4 q[U][kIn];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load(i + u * kNormThreads, q[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) store(i + u * kNormThreads, q[u]);
   }
-  for (int i = n / EPV * EPV + threadIdx.x; i < n; i += kNormThreads) {
-    const float x = load_elem<DT>(p, i) * by;
-    if constexpr (DO == DT_F32) static_cast<float*>(o)[i] = x;
-    else static_cast<uint16_t*>(o)[i] = (uint16_t)pack_bf16(x, 0.f);
+  for (; i < steps; i += kNormThreads) {
+    u32x4 q[kIn];
+    load(i, q);
+    store(i, q);
+  }
+  for (int k = steps * 8 + tid; k < n; k += kNormThreads) {
+    const float x = load_elem<DT>(p, k) * by;
+    if constexpr (DO == DT_F32) static_cast<float*>(o)[k] = x;
+    else static_cast<uint16_t*>(o)[k] = (uint16_t)pack_bf16(x, 0.f);
   }
 }
 
-__global__ __launch_bounds__(kNormThreads) void grad_scale_kernel(const TensorBatch b, const float* factor) {
-  const float by = *factor;
-  for (uint32_t g = blockIdx.x; g < b.granules; g += gridDim.x) {
+struct Finish {
+  const double* part;                 // the partial sums, if this launch is to add them up
+  int n;
+  float max_norm;
+  float* norm;
+  uint32_t* flag;
+  const float* factor;                // else: the factor
+};
+static_assert(sizeof(TensorBatch) + sizeof(Finish) <= 4096, "kernel arguments");
+
+template <bool ONCE>
+__global__ __launch_bounds__(kNormThreads) void grad_scale_kernel(const TensorBatch b, const Finish f) {
+  __shared__ BlockScratch sm;
+  const float by = f.part ? finish_norm(f.part, f.n, f.max_norm, f.norm, f.flag, blockIdx.x == 0, sm) : *f.factor;
+  for (uint32_t k = blockIdx.x; k < b.granules; k += gridDim.x) {
+    const uint32_t g = b.granules - 1 - k;
     const TensorBatch::Entry& t = b.t[tensor_of(b, g)];
     if (by == 1.f && t.in == t.out) continue;
     const long long at = (long long)(g - t.first) * kGranuleElems;
@@ -128,11 +181,11 @@ __global__ __launch_bounds__(kNormThreads) void grad_scale_kernel(const TensorBa
     const char* in = static_cast<const char*>(t.in) + at * (t.dtype == DT_F32 ? 4 : 2);
     char* out = static_cast<char*>(t.out) + at * (t.out_dtype == DT_F32 ? 4 : 2);
     if (t.dtype == DT_F32) {
-      if (t.out_dtype == DT_F32) scale_granule<DT_F32, DT_F32>(in, out, n, by);
-      else scale_granule<DT_F32, DT_BF16>(in, out, n, by);
+      if (t.out_dtype == DT_F32) scale_granule<DT_F32, DT_F32, ONCE>(in, out, n, by);
+      else scale_granule<DT_F32, DT_BF16, ONCE>(in, out, n, by);
     } else {
-      if (t.out_dtype == DT_F32) scale_granule<DT_BF16, DT_F32>(in, out, n, by);
-      else scale_granule<DT_BF16, DT_BF16>(in, out, n, by);
+      if (t.out_dtype == DT_F32) scale_granule<DT_BF16, DT_F32, ONCE>(in, out, n, by);
+      else scale_granule<DT_BF16, DT_BF16, ONCE>(in, out, n, by);
     }
   }
 }
@@ -161,7 +214,7 @@ int norm_and_scale(int n, const void* const* grads, const int64_t* numel, const 
   using namespace sv;
   SV_REQUIRE(n >= 0, SV_ERR_INVALID_ARG);
   SV_REQUIRE(norm && (n == 0 || (grads && numel && dtype)), SV_ERR_NULL);
-  long long granules = 0;
+  long long granules = 0, bytes = 0;
   for (int i = 0; i < n; ++i) {
     SV_REQUIRE((dtype[i] == SV_F32 || dtype[i] == SV_BF16) &&
                    (!out || out_dtype[i] == SV_F32 || out_dtype[i] == SV_BF16),
@@ -171,6 +224,7 @@ int norm_and_scale(int n, const void* const* grads, const int64_t* numel, const 
     granules += (numel[i] + kGranuleElems - 1) / kGranuleElems;
     SV_REQUIRE(granules <= 0x7fffffffLL, SV_ERR_TOO_LARGE);
     if (numel[i] == 0) continue;
+    bytes += numel[i] * (elem_bytes(dtype[i]) + (out ? elem_bytes(out_dtype[i]) : 0));
     SV_REQUIRE(grads[i] && (!out || out[i]), SV_ERR_NULL);
     SV_REQUIRE(is_aligned(grads[i], elem_bytes(dtype[i])) && (!out || is_aligned(out[i], elem_bytes(out_dtype[i]))),
                SV_ERR_ALIGN);
@@ -189,12 +243,16 @@ int norm_and_scale(int n, const void* const* grads, const int64_t* numel, const 
     hipLaunchKernelGGL(grad_norm_kernel, dim3(groups), dim3(kNormThreads), 0, st, b, part + parts);
     parts += (int)groups;
   }
-  hipLaunchKernelGGL(grad_norm_finish_kernel, dim3(1), dim3(1024), 0, st, part, parts, max_norm, norm, flag, factor);
-  for (int i = 0; out && i < n; i += kTensors) {
+  const bool apart = !out || parts == 0 || n > kTensors;
+  if (apart)
+    hipLaunchKernelGGL(grad_norm_finish_kernel, dim3(1), dim3(kNormThreads), 0, st, part, parts, max_norm, norm, flag, factor);
+  for (int i = (batches(n) - 1) * kTensors; out && i >= 0; i -= kTensors) {
     const TensorBatch b = batch_of(i, n, grads, numel, dtype, out, out_dtype);
     if (b.granules == 0) continue;
     const unsigned groups = b.granules < 2u * kNormGroups ? b.granules : 2u * kNormGroups;
-    hipLaunchKernelGGL(grad_scale_kernel, dim3(groups), dim3(kNormThreads), 0, st, b, factor);
+    const Finish f = {apart ? nullptr : part, parts, max_norm, norm, flag, factor};
+    if (bytes > kCacheBytes) hipLaunchKernelGGL(grad_scale_kernel<true>, dim3(groups), dim3(kNormThreads), 0, st, b, f);
+    else hipLaunchKernelGGL(grad_scale_kernel<false>, dim3(groups), dim3(kNormThreads), 0, st, b, f);
   }
   return launch_status();
 }

@@ -25,6 +25,9 @@ constexpr int kMaxSplit = 8;          // a row may be swept by up to 8 workgroup
 constexpr double kCdfEdgeRel = 1e-6;
 constexpr double kCdfEdgeAbs = 1e-6;
 
+// What a call reads or writes beyond this goes past the last-level cache (256 MB): a later reader would not find it there.
+constexpr long long kCacheBytes = 128 << 20;
+
 inline hipStream_t as_stream(sv_stream_t s) { return reinterpret_cast<hipStream_t>(s); }
 
 inline int elem_bytes(int dtype) { return dtype == SV_F32 ? 4 : (dtype == SV_BF16 ? 2 : 0); }

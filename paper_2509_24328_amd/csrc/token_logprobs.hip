@@ -575,9 +575,6 @@ inline Split split_of(long long rows, int V, int dtype, int max_rows) {
   return {(whole.vecs + vecs - 1) / vecs, vecs};
 }
 constexpr int kScoreRows = 682, kGradRows = 192;
-// Logits beyond this are read past the last-level cache: 1024 x 152064 f32 100 us so, 112 us through it; below it is the other
-// way round, 144 x 32000 bf16 14.3 and 12.5.
-constexpr long long kCacheBytes = 128 << 20;
 
 template <int DT, bool ENT>
 void launch_score(ScoreArgs a, long long rows, hipStream_t st) {
@@ -864,6 +861,7 @@ extern "C" int sv_token_logprobs(const void* z, int64_t z_stride, const int32_t*
   a.logprob = logprob_or_null; a.lse = lse_or_null; a.entropy = entropy_or_null; a.rank = rank_or_null;
   a.top_token = top_token_or_null; a.top_logprob = top_logprob_or_null; a.flags = flags_or_null;
   const long long rows = (long long)B * P;
+  // 1024 x 152064 f32: 100 us past the last-level cache, 112 us through it; 144 x 32000 bf16: 14.3 and 12.5
   a.once = rows * V * elem_bytes(dtype) > kCacheBytes;
   a.split = ws_or_null ? split_of(rows, V, dtype, kScoreRows) : whole_row(V, dtype);
   if (ws_or_null) {
