@@ -492,9 +492,12 @@ def _outputs(shape, *tensors):
             raise SvError(SV_ERR_INVALID_ARG)
 
 
-def _i32(*tensors):                 # (unsigned ones hold flags)
+_INT32 = (torch.int32, torch.uint32)   # (unsigned ones hold flags)
+
+
+def _i32(*tensors):
     for t in tensors:
-        if t is not None and t.dtype not in (torch.int32, torch.uint32):
+        if t is not None and t.dtype not in _INT32:
             raise SvError(SV_ERR_DTYPE)
 
 
@@ -574,11 +577,13 @@ def sv_token_logprobs_grad(z, tokens, g_logprob, dz, g_entropy=None, logprob=Non
 def sv_embedding(table, ids, out, scale=1.0, flags=None, stream=None):
     V, D = table.shape
     n = ids.numel()
-    if out.dtype != table.dtype:
+    if out.dtype != table.dtype or out.numel() != n * D:
         raise SvError(SV_ERR_INVALID_ARG)
-    _i32(ids, flags)
-    _outputs((n, D), out)
-    _outputs((n,), flags)
+    if ids.dtype not in _INT32:
+        raise SvError(SV_ERR_DTYPE)
+    if flags is not None:
+        _i32(flags)
+        _outputs((n,), flags)
     _check(lib.sv_embedding(_ptr(table), _ptr(ids), n, V, D, _dtype_tag(table), scale, _ptr(out), _ptr(flags),
                             _stream(stream)))
 

@@ -61,7 +61,7 @@ class Model:
 class Fit:
     """A companion in training: its parameters, gradients, momentum and the scratch of the calls."""
 
-    def __init__(self, model, rows, lr=0.5, momentum=0.9, max_norm=1.0, entropy_weight=0.0):
+    def __init__(self, model, rows, lr=0.1, momentum=0.9, max_norm=1.0, entropy_weight=0.0):
         self.model, self.lr, self.momentum, self.max_norm = model, lr, momentum, max_norm
         self.params = [model.table, model.layer]
         self.velocity = [torch.zeros_like(p) for p in self.params]
@@ -97,7 +97,7 @@ class Fit:
             p.sub_(v, alpha=self.lr)
 
 
-def run(V=512, D=32, B=64, k=4, steps=200, seed=0, n_top=5, lr=0.5, noise=0.5, entropy_weight=0.0):
+def run(V=512, D=32, B=64, k=4, steps=200, seed=0, n_top=5, lr=0.1, noise=0.5, entropy_weight=0.0):
     """List of per-step dicts: similarity of companion and target (S of sv_row_stats), mean log-probability of the
     emitted tokens under the target and under the companion, accepted drafts per sequence, gradient norm."""
     gen = torch.Generator(device="cuda")

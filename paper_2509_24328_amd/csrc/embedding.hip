@@ -306,10 +306,11 @@ template <int DT>
 struct Chunk {
   static constexpr int kVecs = kChunkCols / Elem<DT>::per_vec;
   u32x4 q[kVecs];
+  template <bool ONCE = false>
   __device__ __forceinline__ void load(const void* row, int D, int c) {
     if ((c + 1) * kChunkCols <= D) {
 #pragma unroll
-      for (int k = 0; k < kVecs; ++k) q[k] = load_vec(row, c * kVecs + k);
+      for (int k = 0; k < kVecs; ++k) q[k] = ONCE ? load_vec_nt(row, c * kVecs + k) : load_vec(row, c * kVecs + k);
       return;
     }
 #pragma unroll
@@ -383,7 +384,7 @@ __device__ __forceinline__ Piece look_at(const uint32_t* key, int piece, uint32_
 
 // Goes through the sorted positions, the rows of eight of them under way at a time whatever tokens they belong to, and writes a
 // token's row where its positions end.
-template <int DTG, int DTW>
+template <int DTG, int DTW, bool ONCE>
 __global__ __launch_bounds__(kEmbThreads) void embedding_grad_pieces_kernel(const GradRows a) {
   constexpr int kAhead = 8;
   __shared__ uint32_t key[(kMaxGroups + 2) * kMaxPiece + 1];
@@ -410,7 +411,7 @@ __global__ __launch_bounds__(kEmbThreads) void embedding_grad_pieces_kernel(cons
     for (int i = p.from; i < p.to; i += kAhead) {
       Chunk<DTG> q[kAhead];
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) q[u].load(g + at[min(i + u, p.to - 1)] * bytes, a.D, c);
+      for (int u = 0; u < kAhead; ++u) q[u].template load<ONCE>(g + at[min(i + u, p.to - 1)] * bytes, a.D, c);
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
         if (i + u >= p.to) break;
@@ -504,7 +505,10 @@ template <int DTG, int DTW>
 void launch_sums(const GradRows& a, hipStream_t st) {
   const int per = kEmbThreads / a.lanes * a.piece;
   const dim3 grid((unsigned)(((long long)a.n + per - 1) / per));
-  hipLaunchKernelGGL((embedding_grad_pieces_kernel<DTG, DTW>), grid, dim3(kEmbThreads), 0, st, a);
+  if ((long long)a.n * a.D * Elem<DTG>::bytes > kCacheBytes)           // 65536 x 2048 bf16: 71 us past the cache, 75 us through it
+    hipLaunchKernelGGL((embedding_grad_pieces_kernel<DTG, DTW, true>), grid, dim3(kEmbThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL((embedding_grad_pieces_kernel<DTG, DTW, false>), grid, dim3(kEmbThreads), 0, st, a);
   if (a.n <= a.piece) return;
   const int lanes = a.lanes < kJoinLanes ? a.lanes : kJoinLanes, join_per = kEmbThreads / lanes * a.piece;
   const int chunks = (a.D + kChunkCols - 1) / kChunkCols;

@@ -394,19 +394,33 @@ __device__ __forceinline__ void alternatives(const void* row, int V, float L, in
     last_z = value_of(sm.first[n - 1]);
   }
   const int per_lane = split.vecs / lanes_apart;
-  auto visit = [&](auto&& take) {
-    for (int p = tid; p < n_lanes * per_lane; p += NT) {
-      const int e = (int)((uint32_t)p / (uint32_t)n_lanes), of = number_of(lanes[p - e * n_lanes]);
-      const int part = split.n == 1 ? 0 : (int)((uint32_t)of / (uint32_t)split.vecs) * split.vecs;
-      const int i = part + (int)((uint32_t)(of - part) % (uint32_t)lanes_apart) + e * lanes_apart;
-      if (i >= n_vec) continue;
-      float f[EPV];
-      unpack<DT>(load_row_vec<DT>(row, V, i), f);
+  auto visit = [&](auto&& take) {                      // (kAhead vectors of a lane under way: a trip to memory for most rows)
+    const int n_visits = n_lanes * per_lane;
+    for (int p0 = tid; p0 < n_visits; p0 += kAhead * NT) {
+      u32x4 q[kAhead];
+      int number[kAhead];
 #pragma unroll
-      for (int j = 0; j < EPV; ++j) {
-        if (!(f[j] >= last_z)) continue;
-        const uint64_t key = key_of(f[j], i * EPV + j, L);
-        if (key && (f[j] > last_z || i <= last_vec)) take(key);
+      for (int u = 0; u < kAhead; ++u) {
+        const int p = p0 + u * NT;
+        number[u] = n_vec;
+        q[u] = no_mass<DT>();
+        if (p >= n_visits) continue;
+        const int e = (int)((uint32_t)p / (uint32_t)n_lanes), of = number_of(lanes[p - e * n_lanes]);
+        const int part = split.n == 1 ? 0 : (int)((uint32_t)of / (uint32_t)split.vecs) * split.vecs;
+        number[u] = part + (int)((uint32_t)(of - part) % (uint32_t)lanes_apart) + e * lanes_apart;
+        if (number[u] < n_vec) q[u] = load_row_vec<DT>(row, V, number[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (number[u] >= n_vec) continue;
+        float f[EPV];
+        unpack<DT>(q[u], f);
+#pragma unroll
+        for (int j = 0; j < EPV; ++j) {
+          if (!(f[j] >= last_z)) continue;
+          const uint64_t key = key_of(f[j], number[u] * EPV + j, L);
+          if (key && (f[j] > last_z || number[u] <= last_vec)) take(key);
+        }
       }
     }
   };
