@@ -13,51 +13,81 @@ constexpr int kChunkCols = 8;           // columns of one lane: 16 bytes of bflo
 constexpr int kEmbThreads = 256;
 constexpr int kMinLanes = 8;            // lanes of a row at least
 
-// Columns 8c .. 8c + 7 of a row of D; columns past D are 0 and are not written.
-template <int DT>
-__device__ __forceinline__ void load_chunk(const void* row, int D, int c, float (&f)[kChunkCols]) {
-  if ((c + 1) * kChunkCols <= D) {
-    if constexpr (DT == DT_F32) {
-      const u32x4 a = load_vec(row, 2 * c), b = load_vec(row, 2 * c + 1);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) { f[j] = __uint_as_float(a[j]); f[4 + j] = __uint_as_float(b[j]); }
-    } else {
-      unpack<DT_BF16>(load_vec(row, c), f);
-    }
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < kChunkCols; ++j) f[j] = c * kChunkCols + j < D ? load_elem<DT>(row, c * kChunkCols + j) : 0.f;
+// The eight columns of chunk c of a row of D: 8c .. 8c + 7, or the row's last eight, of which the first `skip` are the chunk's
+// before.  (A row of fewer than eight has its own, one by one.)
+struct Columns {
+  int at, skip;
+};
+__device__ __forceinline__ Columns columns_of(int D, int c) {
+  const int at = max(min(c * kChunkCols, D - kChunkCols), 0);
+  return {at, c * kChunkCols - at};
 }
+template <int DT>
+struct Chunk {
+  static constexpr int kVecs = kChunkCols / Elem<DT>::per_vec;
+  u32x4 q[kVecs];
+  template <bool ONCE = false>
+  __device__ __forceinline__ void load(const void* row, int D, int c) {
+    const char* p = static_cast<const char*>(row) + (size_t)columns_of(D, c).at * Elem<DT>::bytes;
+    if (D >= kChunkCols) {
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) q[k] = ONCE ? load_vec_nt(p, k) : load_vec(p, k);
+      return;
+    }
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) q[k] = u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < kChunkCols; ++j) {
+      if (j >= D) continue;
+      if constexpr (DT == DT_F32) q[j / 4][j % 4] = reinterpret_cast<const uint32_t*>(p)[j];
+      else q[0][j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[j] << (16 * (j & 1));
+    }
+  }
+  __device__ __forceinline__ void get(float (&f)[kChunkCols]) const {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      float v[Elem<DT>::per_vec];
+      unpack<DT>(q[k], v);
+#pragma unroll
+      for (int j = 0; j < Elem<DT>::per_vec; ++j) f[k * Elem<DT>::per_vec + j] = v[j];
+    }
+  }
+  __device__ __forceinline__ void add_to(float (&sum)[kChunkCols]) const {
+    float f[kChunkCols];
+    get(f);
+#pragma unroll
+    for (int j = 0; j < kChunkCols; ++j) sum[j] += f[j];
+  }
+};
+
 __device__ __forceinline__ void store_nt(void* row, int i, const u32x4& q) {      // not read again soon
   __builtin_nontemporal_store(q, reinterpret_cast<u32x4_row*>(row) + i);
 }
 // ONCE: the results are more than the last-level cache keeps for a later reader, and are written past it.
 template <int DT, bool ONCE = true>
 __device__ __forceinline__ void store_chunk(void* row, int D, int c, const float (&f)[kChunkCols]) {
-  auto put = [&](int i, const u32x4& q) {
-    if constexpr (ONCE) store_nt(row, i, q);
-    else reinterpret_cast<u32x4_row*>(row)[i] = q;
-  };
+  const Columns w = columns_of(D, c);
+  char* p = static_cast<char*>(row) + (size_t)w.at * Elem<DT>::bytes;
+  u32x4 q[2];
   if constexpr (DT == DT_F32) {
-    if ((c + 1) * kChunkCols <= D) {
-      put(2 * c, u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
-      put(2 * c + 1, u32x4{__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])});
-      return;
-    }
 #pragma unroll
-    for (int j = 0; j < kChunkCols; ++j)
-      if (c * kChunkCols + j < D) reinterpret_cast<float*>(row)[c * kChunkCols + j] = f[j];
+    for (int j = 0; j < kChunkCols; ++j) q[j / 4][j % 4] = __float_as_uint(f[j]);
   } else {
-    const u32x4 q = {pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
-    if ((c + 1) * kChunkCols <= D) {
-      put(c, q);
-      return;
-    }
+    q[0] = u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
+  }
+  if (w.skip == 0 && D >= kChunkCols) {
 #pragma unroll
-    for (int j = 0; j < kChunkCols; ++j)
-      if (c * kChunkCols + j < D)
-        reinterpret_cast<uint16_t*>(row)[c * kChunkCols + j] = (uint16_t)(q[j >> 1] >> (16 * (j & 1)));
+    for (int k = 0; k < Chunk<DT>::kVecs; ++k) {
+      if constexpr (ONCE) store_nt(p, k, q[k]);
+      else reinterpret_cast<u32x4_row*>(p)[k] = q[k];
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < kChunkCols; ++j) {
+    if (j < w.skip || j >= D) continue;
+    if constexpr (DT == DT_F32) reinterpret_cast<uint32_t*>(p)[j] = q[j / 4][j % 4];
+    else reinterpret_cast<uint16_t*>(p)[j] = (uint16_t)(q[0][j / 2] >> (16 * (j & 1)));
   }
 }
 
@@ -82,7 +112,11 @@ __global__ __launch_bounds__(kEmbThreads) void embedding_kernel(const void* tabl
   if (flags && l == 0) flags[i] = given || id == -1 ? 0 : SV_FLAG_BAD_TOKEN;
   for (int c = l; c * kChunkCols < D; c += lanes) {
     float f[kChunkCols] = {};
-    if (given) load_chunk<DT>(from, D, c, f);
+    if (given) {
+      Chunk<DT> q;
+      q.load(from, D, c);
+      q.get(f);
+    }
 #pragma unroll
     for (int j = 0; j < kChunkCols; ++j) f[j] = given ? f[j] * scale : 0.f;
     store_chunk<DT, ONCE>(to, D, c, f);
@@ -283,9 +317,16 @@ __global__ __launch_bounds__(kSortThreads) void sort_tile_kernel(const SortPass 
 // sums
 // ---------------------------------------------------------------------------
 constexpr int kMaxGroups = kEmbThreads / kMinLanes;
-constexpr int kMaxPiece = 64;
-// Sorted positions that one group of lanes goes through, and the most a token may have to be summed by one group.
-inline int piece_of(int n) { return n <= 8192 ? 8 : kMaxPiece; }
+constexpr int kMinPiece = 8, kMaxPiece = 64;
+// Sorted positions that one group of lanes goes through, and the most a token may have to be summed by one group: 64, whose
+// partial sums are a thirty-second of what is read, less where that would leave compute units without a workgroup
+// (512 x 896 f32: 9.9 us with 16, 6.8 with 8).
+inline int piece_of(int n, int D) {
+  const long long groups = (long long)n * lanes_per_row(D) / kEmbThreads;        // positions by workgroups' groups
+  int piece = kMinPiece;
+  while (piece < kMaxPiece && groups >= 512LL * 2 * piece) piece *= 2;
+  return piece;
+}
 
 struct GradRows {
   const void* g;
@@ -301,49 +342,15 @@ struct GradRows {
   float scale;
 };
 
-// The vectors of one chunk of a row.
-template <int DT>
-struct Chunk {
-  static constexpr int kVecs = kChunkCols / Elem<DT>::per_vec;
-  u32x4 q[kVecs];
-  template <bool ONCE = false>
-  __device__ __forceinline__ void load(const void* row, int D, int c) {
-    if ((c + 1) * kChunkCols <= D) {
-#pragma unroll
-      for (int k = 0; k < kVecs; ++k) q[k] = ONCE ? load_vec_nt(row, c * kVecs + k) : load_vec(row, c * kVecs + k);
-      return;
-    }
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k) q[k] = u32x4{0, 0, 0, 0};
-    for (int j = c * kChunkCols; j < D; ++j) {         // the last columns of a row that is no multiple of 8
-      const int at = j - c * kChunkCols;
-      if constexpr (DT == DT_F32) {
-        const uint32_t x = static_cast<const uint32_t*>(row)[j];
-#pragma unroll
-        for (int k = 0; k < kChunkCols; ++k) q[k / 4][k % 4] = k == at ? x : q[k / 4][k % 4];
-      } else {
-        const uint32_t x = (uint32_t)static_cast<const uint16_t*>(row)[j] << (16 * (at & 1));
-#pragma unroll
-        for (int k = 0; k < 4; ++k) q[0][k] |= k == at / 2 ? x : 0;
-      }
-    }
-  }
-  __device__ __forceinline__ void add_to(float (&sum)[kChunkCols]) const {
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k) {
-      float f[Elem<DT>::per_vec];
-      unpack<DT>(q[k], f);
-#pragma unroll
-      for (int j = 0; j < Elem<DT>::per_vec; ++j) sum[k * Elem<DT>::per_vec + j] += f[j];
-    }
-  }
-};
-
 template <int DTW>
 __device__ __forceinline__ void store_sum(const GradRows& a, uint32_t v, int c, float (&sum)[kChunkCols]) {
   char* to = static_cast<char*>(a.table) + (size_t)v * a.D * Elem<DTW>::bytes;
   float old[kChunkCols] = {};
-  if (a.accumulate) load_chunk<DTW>(to, a.D, c, old);
+  if (a.accumulate) {
+    Chunk<DTW> q;
+    q.load(to, a.D, c);
+    q.get(old);
+  }
 #pragma unroll
   for (int j = 0; j < kChunkCols; ++j) sum[j] = __builtin_fmaf(sum[j], a.scale, old[j]);
   store_chunk<DTW>(to, a.D, c, sum);
@@ -433,22 +440,22 @@ __global__ __launch_bounds__(kEmbThreads) void embedding_grad_pieces_kernel(cons
   }
 }
 
-// Rows of tokens with more than a piece of positions: kJoin groups of up to 64 lanes to 64 chunks of each (a frequent token's
-// partial sums are a megabyte, more than one compute unit reads in the time that the rest takes), every group a run of
-// the partial sums, then added in order.
-constexpr int kJoin = 4, kJoinLanes = 64;
+// Rows of tokens with more than a piece of positions.  A workgroup has kJoinPieces pieces and up to 64 chunks of their rows (a
+// frequent token's partial sums are a megabyte, more than one compute unit reads in the time that the rest takes);
+// its groups of lanes sum a run of a token's partial sums each, and those sums are added in order.
+constexpr int kJoinThreads = 1024, kJoinPieces = 4, kJoinLanes = 64;
 template <int DTW>
-__global__ __launch_bounds__(kEmbThreads * kJoin) void embedding_grad_join_kernel(const GradRows a) {
-  __shared__ float sums[kJoin - 1][kEmbThreads][kChunkCols + 1];
-  const int lanes = min(a.lanes, kJoinLanes), groups = kEmbThreads / lanes, t = threadIdx.x % kEmbThreads;
-  const int share = threadIdx.x / kEmbThreads, c = blockIdx.y * lanes + t % lanes;
-  const long long p0 = (long long)blockIdx.x * groups + t / lanes;
+__global__ __launch_bounds__(kJoinThreads) void embedding_grad_join_kernel(const GradRows a) {
+  __shared__ float sums[kJoinThreads][kChunkCols + 1];
+  const int lanes = min(a.lanes, kJoinLanes), per_share = kJoinPieces * lanes, shares = kJoinThreads / per_share;
+  const int share = threadIdx.x / per_share, t = threadIdx.x % per_share, c = blockIdx.y * lanes + t % lanes;
+  const long long p0 = (long long)blockIdx.x * kJoinPieces + t / lanes;
   const int begins = p0 * a.piece < a.n && c * kChunkCols < a.D ? a.begins[p0] : -1;
   if (!__syncthreads_or(begins >= 0)) return;
   float sum[kChunkCols] = {};
   const uint32_t v = (uint32_t)begins >> 1;
   if (begins >= 0) {
-    const int parts = (int)((a.last[v] - 1) / a.piece - p0) + 1, per = (parts + kJoin - 1) / kJoin;
+    const int parts = (int)((a.last[v] - 1) / a.piece - p0) + 1, per = (parts + shares - 1) / shares;
     const int from = min(share * per, parts), to = min(from + per, parts);
     constexpr int kAhead = 8;
     for (int i = from; i < to; i += kAhead) {
@@ -463,15 +470,13 @@ __global__ __launch_bounds__(kEmbThreads * kJoin) void embedding_grad_join_kerne
         if (i + u < to) q[u].add_to(sum);
     }
   }
-  if (share > 0)
 #pragma unroll
-    for (int j = 0; j < kChunkCols; ++j) sums[share - 1][t][j] = sum[j];
+  for (int j = 0; j < kChunkCols; ++j) sums[threadIdx.x][j] = sum[j];
   __syncthreads();
   if (share > 0 || begins < 0) return;
+  for (int s = 1; s < shares; ++s)
 #pragma unroll
-  for (int s = 0; s < kJoin - 1; ++s)
-#pragma unroll
-    for (int j = 0; j < kChunkCols; ++j) sum[j] += sums[s][t][j];
+    for (int j = 0; j < kChunkCols; ++j) sum[j] += sums[s * per_share + t][j];
   store_sum<DTW>(a, v, c, sum);
 }
 
@@ -488,15 +493,16 @@ inline EmbeddingWs carve_embedding_ws(void* base, int n, int V, int D) {
   EmbeddingWs w = {};
   char* p = static_cast<char*>(base);
   size_t off = 0;
+  const int piece = piece_of(n, D), pieces = (n + piece - 1) / piece;
   auto take = [&](size_t bytes) { char* q = p ? p + off : nullptr; off += ws_round(bytes); return q; };
   for (int i = 0; i < 2; ++i) {
     w.key[i] = reinterpret_cast<uint32_t*>(take((size_t)n * 4));
     w.pos[i] = reinterpret_cast<int32_t*>(take((size_t)n * 4));
   }
   w.hist = reinterpret_cast<int32_t*>(take((size_t)sort_tiles(n) * kDigits * 4));
-  w.begins = reinterpret_cast<int32_t*>(take((size_t)((n + piece_of(n) - 1) / piece_of(n)) * 4));
+  w.begins = reinterpret_cast<int32_t*>(take((size_t)pieces * 4));
   w.last = reinterpret_cast<int32_t*>(take((size_t)V * 4));
-  w.part = reinterpret_cast<float*>(take((size_t)((n + piece_of(n) - 1) / piece_of(n)) * 2 * D * 4));
+  w.part = reinterpret_cast<float*>(take((size_t)pieces * 2 * D * 4));
   w.bytes = off;
   return w;
 }
@@ -510,10 +516,10 @@ void launch_sums(const GradRows& a, hipStream_t st) {
   else
     hipLaunchKernelGGL((embedding_grad_pieces_kernel<DTG, DTW, false>), grid, dim3(kEmbThreads), 0, st, a);
   if (a.n <= a.piece) return;
-  const int lanes = a.lanes < kJoinLanes ? a.lanes : kJoinLanes, join_per = kEmbThreads / lanes * a.piece;
-  const int chunks = (a.D + kChunkCols - 1) / kChunkCols;
+  const int lanes = a.lanes < kJoinLanes ? a.lanes : kJoinLanes, chunks = (a.D + kChunkCols - 1) / kChunkCols;
+  const int join_per = kJoinPieces * a.piece;
   const dim3 join((unsigned)(((long long)a.n + join_per - 1) / join_per), (unsigned)((chunks + lanes - 1) / lanes));
-  hipLaunchKernelGGL(embedding_grad_join_kernel<DTW>, join, dim3(kEmbThreads * kJoin), 0, st, a);
+  hipLaunchKernelGGL(embedding_grad_join_kernel<DTW>, join, dim3(kJoinThreads), 0, st, a);
 }
 
 }  // namespace sv
@@ -592,7 +598,7 @@ extern "C" int sv_embedding_grad(const void* grad_out, int dtype, const int32_t*
   }
   if (n == 0) return launch_status();
   const GradRows a = {grad_out, grad_table, w.key[at], w.pos[at], w.begins, w.last, w.part, n, V, D, lanes_per_row(D),
-                      accumulate != 0, piece_of(n), scale};
+                      accumulate != 0, piece_of(n, D), scale};
   if (dtype == SV_F32) {
     if (table_dtype == SV_F32) launch_sums<DT_F32, DT_F32>(a, st);
     else launch_sums<DT_F32, DT_BF16>(a, st);
