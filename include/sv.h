@@ -665,8 +665,8 @@ size_t sv_embedding_grad_workspace_bytes(int n, int V, int D);
 /*
  * Gradient of the table of sv_embedding:
  *   grad_table[v, :] = scale * sum over {i : ids[i] = v} of grad_out[i, :]   (+ grad_table[v, :] if accumulate)
- * in float32, rounded once.  The tokens are sorted first and the rows of one token are
- * summed in the order of their positions, so the result does not depend on timing.
+ * in float32, rounded once.  The rows of one token are summed in an order that the positions
+ * fix, so the result does not depend on timing.
  *   grad_out [n, D] dtype, ids [n] int32 (ids outside [0, V) contribute nothing)   in
  *   grad_table [V, D] table_dtype    out  every row is written; with accumulate != 0 (a table
  *            tied to the output projection) only rows of tokens that occur are touched

@@ -2,8 +2,11 @@
 //
 // The gradient sorts the tokens (least significant digit first, kDigitBits bits a pass, stable) and sums the rows of
 // equal tokens in the order of their positions: no atomics on the result, the same bits from every call.
+// Few tokens need no sort: one launch finds, orders and sums them.
 // Positions whose id is no row sort behind all others.  The sort occupies a few workgroups for some
 // microseconds a launch; the other workgroups of its launches write the table's zeros meanwhile.
+#include <algorithm>
+
 #include "sv_device.hpp"
 #include "sv_host.hpp"
 
@@ -345,7 +348,7 @@ struct GradRows {
   float scale;
 };
 
-template <int DTW>
+template <int DTW, bool ONCE = true>
 __device__ __forceinline__ void store_sum(const GradRows& a, uint32_t v, int c, float (&sum)[kChunkCols]) {
   char* to = static_cast<char*>(a.table) + (size_t)v * a.D * Elem<DTW>::bytes;
   float old[kChunkCols] = {};
@@ -356,7 +359,7 @@ __device__ __forceinline__ void store_sum(const GradRows& a, uint32_t v, int c, 
   }
 #pragma unroll
   for (int j = 0; j < kChunkCols; ++j) sum[j] = __builtin_fmaf(sum[j], a.scale, old[j]);
-  store_chunk<DTW>(to, a.D, c, sum);
+  store_chunk<DTW, ONCE>(to, a.D, c, sum);
 }
 
 // What a group of lanes has to do: positions from .. to - 1 of the sorted list, the first token's sum (if it is joined) to slot
@@ -483,6 +486,105 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_grad_join_kernel(const
   store_sum<DTW>(a, v, c, sum);
 }
 
+// Few tokens: one launch.  Every workgroup looks through all tokens for those of its rows, orders them by row and position, and
+// writes its rows, sums and zeros alike.  Rows of a group of lanes lie a grid apart, so that frequent tokens, whose numbers often
+// lie together, are spread.  One group sums all of a token's rows, 0.13 us a row: with the limit at 256, that many of one token
+// took 40 us here and 19 us sorted.  128 tokens, here and sorted: 7.5 and 20 us (5000 x 64 bf16), 14 and 20 us (32001 x 896 bf16),
+// 100 and 120 us (152064 x 2048 bf16, 6.2 TB/s), 90 and 103 us (128256 x 1024 f32); all of one token 23 and 18 us (5000 x 64).
+// A small table has one row a group (5000 x 64: 8.6 us in 20 workgroups of eight rounds, 7.5 in 157).
+// Stores past the cache cost a float table 114 us where these take 50 (32000 x 2048): a lane's two vectors are half lines.
+constexpr int kDirectTokens = 128, kRounds = 8, kDirectGroups = 1024;
+static_assert(kDirectTokens <= kEmbThreads, "a lane has one token");
+
+// Row v of the table: the sum of rows at[lo .. hi - 1] of the gradient, columns of lane l of `lanes`.
+template <int DTG, int DTW>
+__device__ __forceinline__ void write_row(const GradRows& a, uint32_t v, const uint16_t* at, int lo, int hi, int l, int lanes) {
+  constexpr int kAhead = 16 / Chunk<DTG>::kVecs;
+  const char* g = static_cast<const char*>(a.g);
+  const size_t bytes = (size_t)a.D * Elem<DTG>::bytes;
+  for (int c = l; c * kChunkCols < a.D; c += lanes) {
+    float sum[kChunkCols] = {};
+    for (int i = lo; i < hi; i += kAhead) {
+      Chunk<DTG> q[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (i + u < hi) q[u].load(g + at[i + u] * bytes, a.D, c);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (i + u < hi) q[u].add_to(sum);
+    }
+    store_sum<DTW, false>(a, v, c, sum);
+  }
+}
+
+// The positions of this workgroup's lanes that hit, in their order, to found[]; -> how many.  A wavefront's lanes call it together.
+__device__ __forceinline__ int collect(bool here, int* count, uint16_t* found, int& to) {
+  constexpr int kWaves = kEmbThreads / kWave;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t hit = __ballot(here);
+  if (lane == 0) count[wave] = __popcll(hit);
+  __syncthreads();
+  int total = 0;
+  to = __popcll(hit & ((1ull << lane) - 1));
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    to += w < wave ? count[w] : 0;
+    total += count[w];
+  }
+  if (here) found[to] = (uint16_t)threadIdx.x;
+  return total;
+}
+
+template <int DTG, int DTW>
+__global__ __launch_bounds__(kEmbThreads) void embedding_grad_direct_kernel(const GradRows a, const int32_t* ids) {
+  __shared__ uint16_t found[kDirectTokens], at[kDirectTokens], row_found[kDirectTokens];
+  __shared__ uint16_t start[kRounds * kMaxGroups], end[kRounds * kMaxGroups];
+  __shared__ int count[kEmbThreads / kWave];
+  const int tid = threadIdx.x, groups = kEmbThreads / a.lanes;
+  for (int r = tid; r < kRounds * groups; r += kEmbThreads) start[r] = end[r] = 0;
+  const int id = tid < a.n ? ids[tid] : -1;
+  const uint32_t unit = (uint32_t)max(id, 0) / (uint32_t)groups, round = unit / gridDim.x;
+  const bool here = id >= 0 && id < a.V && unit - round * gridDim.x == blockIdx.x;
+  int to;
+  const int total = collect(here, count, found, to);
+  if (here) row_found[to] = (uint16_t)(round * groups + (uint32_t)id % (uint32_t)groups);
+  __syncthreads();
+  if (tid < total) {
+    const int r = row_found[tid];
+    int smaller = 0, same = 0, earlier = 0;
+    for (int m = 0; m < total; ++m) {
+      const int o = row_found[m];
+      smaller += o < r;
+      same += o == r;
+      earlier += o == r && m < tid;
+    }
+    at[smaller + earlier] = found[tid];
+    if (earlier == 0) { start[r] = (uint16_t)smaller; end[r] = (uint16_t)(smaller + same); }
+  }
+  __syncthreads();
+  const int l = tid % a.lanes, group = tid / a.lanes;
+#pragma unroll 1
+  for (int k = 0; k < kRounds; ++k) {
+    const long long v = ((long long)k * gridDim.x + blockIdx.x) * groups + group;
+    if (v >= a.V) return;
+    write_row<DTG, DTW>(a, (uint32_t)v, at, start[k * groups + group], end[k * groups + group], l, a.lanes);
+  }
+}
+
+// Few tokens added to a table: only their rows are touched, so there is a workgroup for each token, and the first of equal ones
+// sums them all.  16 tokens of 152064 x 2048 bf16: 6.7 us (the host's call), 49 us by the table's rows as above, 18 us sorted.
+template <int DTG, int DTW>
+__global__ __launch_bounds__(kEmbThreads) void embedding_grad_add_kernel(const GradRows a, const int32_t* ids) {
+  __shared__ uint16_t found[kDirectTokens];
+  __shared__ int count[kEmbThreads / kWave];
+  const int id = ids[blockIdx.x];
+  if (id < 0 || id >= a.V) return;
+  int to;
+  const int total = collect((int)threadIdx.x < a.n && ids[min((int)threadIdx.x, a.n - 1)] == id, count, found, to);
+  __syncthreads();
+  if (found[0] == blockIdx.x) write_row<DTG, DTW>(a, (uint32_t)id, found, 0, total, threadIdx.x, kEmbThreads);
+}
+
 struct EmbeddingWs {
   uint32_t* key[2];
   int32_t* pos[2];
@@ -494,6 +596,7 @@ struct EmbeddingWs {
 inline int sort_tiles(int n) { return (n + kSortTile - 1) / kSortTile; }
 inline EmbeddingWs carve_embedding_ws(void* base, int n, int V, int D) {
   EmbeddingWs w = {};
+  if (n <= kDirectTokens) return w;
   char* p = static_cast<char*>(base);
   size_t off = 0;
   const int piece = piece_of(n, D), pieces = (n + piece - 1) / piece;
@@ -511,7 +614,17 @@ inline EmbeddingWs carve_embedding_ws(void* base, int n, int V, int D) {
 }
 
 template <int DTG, int DTW>
-void launch_sums(const GradRows& a, hipStream_t st) {
+void launch_sums(const GradRows& a, const int32_t* ids, hipStream_t st) {
+  if (a.n <= kDirectTokens && a.accumulate) {
+    hipLaunchKernelGGL((embedding_grad_add_kernel<DTG, DTW>), dim3((unsigned)a.n), dim3(kEmbThreads), 0, st, a, ids);
+    return;
+  }
+  if (a.n <= kDirectTokens) {
+    const int units = (a.V + kEmbThreads / a.lanes - 1) / (kEmbThreads / a.lanes);
+    const dim3 grid((unsigned)std::max((units + kRounds - 1) / kRounds, std::min(units, kDirectGroups)));
+    hipLaunchKernelGGL((embedding_grad_direct_kernel<DTG, DTW>), grid, dim3(kEmbThreads), 0, st, a, ids);
+    return;
+  }
   const int per = kEmbThreads / a.lanes * a.piece;
   const dim3 grid((unsigned)(((long long)a.n + per - 1) / per));
   if ((long long)a.n * a.D * Elem<DTG>::bytes > kCacheBytes)           // 65536 x 2048 bf16: 71 us past the cache, 75 us through it
@@ -571,43 +684,45 @@ extern "C" int sv_embedding_grad(const void* grad_out, int dtype, const int32_t*
   SV_REQUIRE(ws && is_aligned(ws, kWsAlign) && ws_bytes >= sv_embedding_grad_workspace_bytes(n, V, D), SV_ERR_WORKSPACE);
   hipStream_t st = as_stream(stream);
   const EmbeddingWs w = carve_embedding_ws(ws, n, V, D);
-  int bits = 1, at = 0;
-  while ((V >> bits) != 0) ++bits;                       // keys 0 .. V
-  // the table's zeros, in equal shares to the launches of the sort
-  const int passes = (bits + kDigitBits - 1) / kDigitBits, tiles = sort_tiles(n), launches = tiles <= 1 ? 1 : 2 * passes;
-  char* zeros = static_cast<char*>(grad_table);
-  size_t left = accumulate ? 0 : (size_t)V * D * elem_bytes(table_dtype);
-  const size_t share = (left / launches + kClearBytes - 1) / kClearBytes * kClearBytes;
-  auto clear = [&](int first_block) {
-    const Clear z = {zeros, share < left ? share : left, first_block};
-    zeros += z.bytes;
-    left -= z.bytes;
-    return z;
-  };
-  const dim3 block(kSortThreads);
-  if (tiles <= 1) {
-    const SortPass p = {ids, nullptr, nullptr, w.key[0], w.pos[0], nullptr, n, V, 0};
-    const Clear z = clear(n > 0 ? 1 : 0);
-    hipLaunchKernelGGL(sort_tile_kernel, dim3(z.first_block + clear_blocks(z)), block, 0, st, p, bits, z);
-  } else {
-    for (int shift = 0; shift < bits; shift += kDigitBits) {
-      const SortPass p = {shift == 0 ? ids : nullptr, w.key[at], w.pos[at], w.key[1 - at], w.pos[1 - at], w.hist, n, V, shift};
-      const Clear z0 = clear(tiles);
-      hipLaunchKernelGGL(sort_count_kernel, dim3(tiles + clear_blocks(z0)), block, 0, st, p, z0);
-      const Clear z1 = clear(tiles);
-      hipLaunchKernelGGL(sort_scatter_kernel, dim3(tiles + clear_blocks(z1)), block, 0, st, p, tiles, z1);
-      at = 1 - at;
+  int at = 0;
+  if (n > kDirectTokens) {
+    int bits = 1;
+    while ((V >> bits) != 0) ++bits;                     // keys 0 .. V
+    // the table's zeros, in equal shares to the launches of the sort
+    const int passes = (bits + kDigitBits - 1) / kDigitBits, tiles = sort_tiles(n), launches = tiles == 1 ? 1 : 2 * passes;
+    char* zeros = static_cast<char*>(grad_table);
+    size_t left = accumulate ? 0 : (size_t)V * D * elem_bytes(table_dtype);
+    const size_t share = (left / launches + kClearBytes - 1) / kClearBytes * kClearBytes;
+    auto clear = [&](int first_block) {
+      const Clear z = {zeros, share < left ? share : left, first_block};
+      zeros += z.bytes;
+      left -= z.bytes;
+      return z;
+    };
+    const dim3 block(kSortThreads);
+    if (tiles == 1) {
+      const SortPass p = {ids, nullptr, nullptr, w.key[0], w.pos[0], nullptr, n, V, 0};
+      const Clear z = clear(1);
+      hipLaunchKernelGGL(sort_tile_kernel, dim3(1 + clear_blocks(z)), block, 0, st, p, bits, z);
+    } else {
+      for (int shift = 0; shift < bits; shift += kDigitBits) {
+        const SortPass p = {shift == 0 ? ids : nullptr, w.key[at], w.pos[at], w.key[1 - at], w.pos[1 - at], w.hist, n, V, shift};
+        const Clear z0 = clear(tiles);
+        hipLaunchKernelGGL(sort_count_kernel, dim3(tiles + clear_blocks(z0)), block, 0, st, p, z0);
+        const Clear z1 = clear(tiles);
+        hipLaunchKernelGGL(sort_scatter_kernel, dim3(tiles + clear_blocks(z1)), block, 0, st, p, tiles, z1);
+        at = 1 - at;
+      }
     }
   }
-  if (n == 0) return launch_status();
   const GradRows a = {grad_out, grad_table, w.key[at], w.pos[at], w.begins, w.last, w.part, n, V, D, lanes_per_row(D),
                       accumulate != 0, piece_of(n, D), scale};
   if (dtype == SV_F32) {
-    if (table_dtype == SV_F32) launch_sums<DT_F32, DT_F32>(a, st);
-    else launch_sums<DT_F32, DT_BF16>(a, st);
+    if (table_dtype == SV_F32) launch_sums<DT_F32, DT_F32>(a, ids, st);
+    else launch_sums<DT_F32, DT_BF16>(a, ids, st);
   } else {
-    if (table_dtype == SV_F32) launch_sums<DT_BF16, DT_F32>(a, st);
-    else launch_sums<DT_BF16, DT_BF16>(a, st);
+    if (table_dtype == SV_F32) launch_sums<DT_BF16, DT_F32>(a, ids, st);
+    else launch_sums<DT_BF16, DT_BF16>(a, ids, st);
   }
   return launch_status();
 }

@@ -200,3 +200,12 @@ def test_refusals():
         P.sv_embedding(w.cpu(), ids, out)
     assert P.sv_embedding_grad_workspace_bytes(-1, 4, 8) == 0
     assert P.sv_embedding_grad_workspace_bytes(1 << 25, 4, 8) == 0
+
+
+@pytest.mark.parametrize("n", [15, 16, 17, 127, 128, 129, 257])
+@pytest.mark.parametrize("kind", ["one", "zipf", "uniform"])
+def test_gradient_of_few_tokens(n, kind):
+    """About the number up to which one launch does it all; tables of less and of more rows than a workgroup has."""
+    for V, D in ((1, 8), (7, 2048), (300, 5), (1000, 513), (40001, 33)):
+        check_grad(n, V, D, BF16, F32, kind)
+        check_grad(n, V, D, F32, BF16, kind, accumulate=True)
