@@ -6,6 +6,7 @@ fallback: if the library has not been built, importing this module fails.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 
@@ -611,36 +612,40 @@ _TAGS = {torch.float32: SV_F32, torch.bfloat16: SV_BF16}
 
 def _tensor_lists(tensors):
     """HOST arrays of the addresses, sizes and types of a list of contiguous device tensors.  (A list of a few hundred
-    is built for every call: one pass each, 0.2 us a tensor.)"""
-    n = len(tensors)
+    is built for every call, and a model of small tensors waits for it: arrays of the array module are filled in a
+    third of the time of ctypes arrays.)"""
     if not all([t.is_cuda and t.is_contiguous() for t in tensors]):
         raise ValueError("sv: tensors must be contiguous device tensors")
-    tags = [_TAGS.get(t.dtype, -1) for t in tensors]
-    if -1 in tags:
-        raise SvError(SV_ERR_DTYPE)
-    numel = [t.numel() for t in tensors]
-    return (n, (ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors]), (ctypes.c_longlong * n)(*numel),
-            (ctypes.c_int * n)(*tags), numel)
+    try:
+        tags = array.array("i", [_TAGS[t.dtype] for t in tensors])
+    except KeyError:
+        raise SvError(SV_ERR_DTYPE) from None
+    return array.array("Q", [t.data_ptr() for t in tensors]), array.array("q", [t.numel() for t in tensors]), tags
+
+
+def _host(a):
+    return a.buffer_info()[0]
 
 
 def sv_grad_norm(grads, norm, flag=None, ws=None, stream=None):
     """grads: a list of tensors; norm: [1] float32."""
-    n, ptrs, numel, tags, _ = _tensor_lists(grads)
+    ptrs, numel, tags = _tensor_lists(grads)
     _f32(norm)
     _i32(flag)
-    _check(lib.sv_grad_norm(n, ptrs, numel, tags, _ptr(norm), _ptr(flag), _ptr(ws), 0 if ws is None else ws.numel(),
-                            _stream(stream)))
+    _check(lib.sv_grad_norm(len(tags), _host(ptrs), _host(numel), _host(tags), _ptr(norm), _ptr(flag), _ptr(ws),
+                            0 if ws is None else ws.numel(), _stream(stream)))
 
 
 def sv_clip_grad_norm(grads, max_norm, norm, out=None, flag=None, ws=None, stream=None):
     """out: a list of tensors of the same numbers of elements (None: in place)."""
-    n, ptrs, numel, tags, sizes = _tensor_lists(grads)
+    ptrs, numel, tags = _tensor_lists(grads)
     o_ptrs, o_tags = ptrs, tags
     if out is not None:
-        _, o_ptrs, _, o_tags, o_sizes = _tensor_lists(out)
-        if o_sizes != sizes:
+        o_ptrs, o_numel, o_tags = _tensor_lists(out)
+        if o_numel != numel:
             raise SvError(SV_ERR_INVALID_ARG)
     _f32(norm)
     _i32(flag)
-    _check(lib.sv_clip_grad_norm(n, ptrs, numel, tags, max_norm, o_ptrs, o_tags, _ptr(norm), _ptr(flag), _ptr(ws),
-                                 0 if ws is None else ws.numel(), _stream(stream)))
+    _check(lib.sv_clip_grad_norm(len(tags), _host(ptrs), _host(numel), _host(tags), max_norm, _host(o_ptrs),
+                                 _host(o_tags), _ptr(norm), _ptr(flag), _ptr(ws), 0 if ws is None else ws.numel(),
+                                 _stream(stream)))
