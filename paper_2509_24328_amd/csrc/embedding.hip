@@ -692,7 +692,7 @@ extern "C" int sv_embedding_grad(const void* grad_out, int dtype, const int32_t*
     const int passes = (bits + kDigitBits - 1) / kDigitBits, tiles = sort_tiles(n), launches = tiles == 1 ? 1 : 2 * passes;
     char* zeros = static_cast<char*>(grad_table);
     size_t left = accumulate ? 0 : (size_t)V * D * elem_bytes(table_dtype);
-    const size_t share = (left / launches + kClearBytes - 1) / kClearBytes * kClearBytes;
+    const size_t least = launches * kClearBytes, share = (left + least - 1) / least * kClearBytes;      // (launches * share >= left)
     auto clear = [&](int first_block) {
       const Clear z = {zeros, share < left ? share : left, first_block};
       zeros += z.bytes;
