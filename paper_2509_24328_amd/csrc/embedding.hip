@@ -107,8 +107,8 @@ inline int lanes_per_row(int D) {
 template <int DT, bool ONCE>
 __global__ __launch_bounds__(kEmbThreads) void embedding_kernel(const void* table, const int32_t* ids, int n, int V,
                                                                 int D, float scale, void* out, uint32_t* flags,
-                                                                int lanes) {
-  const long long i = (long long)blockIdx.x * (kEmbThreads / lanes) + threadIdx.x / lanes;
+                                                                int lanes, long long first) {
+  const long long i = (first + blockIdx.x) * (kEmbThreads / lanes) + threadIdx.x / lanes;
   if (i >= n) return;
   const int id = ids[i], l = threadIdx.x % lanes;
   const bool given = id >= 0 && id < V;
@@ -652,11 +652,12 @@ extern "C" int sv_embedding(const void* table, const int32_t* ids, int n, int V,
                  is_aligned(flags_or_null, 4),
              SV_ERR_ALIGN);
   const int lanes = lanes_per_row(D), rows = kEmbThreads / lanes;
-  const dim3 grid((unsigned)(((long long)n + rows - 1) / rows)), block(kEmbThreads);
   hipStream_t st = as_stream(stream);
   const bool once = 2LL * n * D * elem_bytes(dtype) > kCacheBytes;      // 16384 x 4096 bf16: 33 us so, 42 us through the cache
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, block, 0, st, table, ids, n, V, D, scale, out, flags_or_null, lanes);
+    in_launches(((long long)n + rows - 1) / rows, kEmbThreads, [&](long long first, dim3 grid) {
+      hipLaunchKernelGGL(kernel, grid, dim3(kEmbThreads), 0, st, table, ids, n, V, D, scale, out, flags_or_null, lanes, first);
+    });
   };
   if (dtype == SV_F32) once ? go(embedding_kernel<DT_F32, true>) : go(embedding_kernel<DT_F32, false>);
   else once ? go(embedding_kernel<DT_BF16, true>) : go(embedding_kernel<DT_BF16, false>);

@@ -90,6 +90,15 @@ inline VerifyWs carve_verify_ws(void* base, int B, int k, int V) {
   return w;
 }
 
+// f(first, grid) for every launch that `groups` workgroups of `lanes` lanes take.  A launch of 2^32 lanes or more is not refused:
+// their number wraps, and the workgroups past it do not run (16777221 rows of 256 lanes: five of them were swept).
+template <class F>
+inline void in_launches(long long groups, int lanes, F&& f) {
+  const long long most = 0xffffffffLL / lanes;
+  for (long long first = 0; first < groups; first += most)
+    f(first, dim3((unsigned)(groups - first < most ? groups - first : most)));
+}
+
 inline int launch_status() { return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_LAUNCH; }
 
 // Optional hipEvent pair recorded right before / after a kernel (api.hip).

@@ -242,6 +242,7 @@ struct ScoreArgs {
   RowPart* parts;                    // [rows, split.n]
   uint64_t* keys;                    // [rows, split.n, split.keys()] the lanes' largest entries
   bool once;
+  long long first;                   // position of the launch's first workgroup (whole rows)
 };
 
 // Value in the order of the logits as a whole number (no NaN); -0 like 0.
@@ -512,7 +513,7 @@ __device__ __forceinline__ void write_row(const ScoreArgs& a, long long at, cons
 template <int DT, int NT, bool ENT, bool TOP>
 __global__ __launch_bounds__(NT, 8) void token_logprobs_kernel(const ScoreArgs a) {
   __shared__ RowScratch sm;
-  const long long at = blockIdx.x;
+  const long long at = a.first + blockIdx.x;
   const Position p = locate<DT>(a, at);
   if (!p.row) return write_blank(a, at, p.bad);
   const float zt = token_logit<DT>(p.row, p.token, a.V);
@@ -595,9 +596,8 @@ constexpr int kScoreRows = 682, kGradRows = 192;
 
 template <int DT, bool ENT>
 void launch_score(ScoreArgs a, long long rows, hipStream_t st) {
-  const dim3 grid((unsigned)rows);
-  if (a.split.n > 1) {
-    const dim3 parts((unsigned)(rows * a.split.n)), block(kPartThreads);
+  if (a.split.n > 1) {                                 // (few rows)
+    const dim3 grid((unsigned)rows), parts((unsigned)(rows * a.split.n)), block(kPartThreads);
     if (a.n_top > 0) {
       hipLaunchKernelGGL((token_logprobs_part_kernel<DT, ENT, true>), parts, block, 0, st, a);
       hipLaunchKernelGGL((token_logprobs_join_kernel<DT, true>), grid, block, 0, st, a);
@@ -610,8 +610,11 @@ void launch_score(ScoreArgs a, long long rows, hipStream_t st) {
   auto go = [&](auto nt) {
     constexpr int NT = decltype(nt)::value;
     a.split.vecs = round_up(a.split.vecs, NT);
-    if (a.n_top > 0) hipLaunchKernelGGL((token_logprobs_kernel<DT, NT, ENT, true>), grid, dim3(NT), 0, st, a);
-    else hipLaunchKernelGGL((token_logprobs_kernel<DT, NT, ENT, false>), grid, dim3(NT), 0, st, a);
+    in_launches(rows, NT, [&](long long first, dim3 grid) {
+      a.first = first;
+      if (a.n_top > 0) hipLaunchKernelGGL((token_logprobs_kernel<DT, NT, ENT, true>), grid, dim3(NT), 0, st, a);
+      else hipLaunchKernelGGL((token_logprobs_kernel<DT, NT, ENT, false>), grid, dim3(NT), 0, st, a);
+    });
   };
   // many short rows: small workgroups, whose ends overlap other rows' sweeps (4096 x 8000 bf16, 20 alternatives: 36 us, 48 with
   // 512 lanes); few rows: more lanes to each (144 x 32000: 13 us, 17 with 256)
@@ -631,6 +634,7 @@ struct GradArgs {
   Scale sc;
   Split split;
   RowPart* parts;                    // [rows, split.n]
+  long long first;                   // row of the launch's first workgroup (whole rows)
 };
 
 __device__ __forceinline__ u32x4 load_bytes(const char* row, uint32_t at) {
@@ -746,7 +750,7 @@ __device__ __forceinline__ void store_grads(const void* row, void* out, int V, i
 template <int DT, int NT, int R, int WAVES, bool ENT>
 __global__ __launch_bounds__(NT, WAVES) void token_logprobs_grad_kernel(const GradArgs a) {
   __shared__ RowScratch sm;
-  const long long at = blockIdx.x;
+  const long long at = a.first + blockIdx.x;
   const int V = a.V, token = a.tokens[at], n_vec = vectors_of<DT>(V), whole = V / Elem<DT>::per_vec, tid = threadIdx.x;
   const char* row = static_cast<const char*>(a.z) + (size_t)at * (size_t)a.stride * Elem<DT>::bytes;
   char* out = static_cast<char*>(a.dz) + (size_t)at * (size_t)a.dz_stride * Elem<DT>::bytes;
@@ -820,7 +824,7 @@ __global__ __launch_bounds__(kPartThreads) void token_logprobs_grad_part_kernel(
 }
 
 template <int DT, bool ENT>
-void launch_grad(const GradArgs& a, int rows, hipStream_t st) {
+void launch_grad(GradArgs a, int rows, hipStream_t st) {
   if (a.split.n > 1) {
     ScoreArgs s = {};
     s.z = a.z; s.stride = a.stride; s.tokens = a.tokens; s.P = 1; s.V = a.V; s.sc = a.sc; s.split = a.split; s.parts = a.parts;
@@ -829,13 +833,18 @@ void launch_grad(const GradArgs& a, int rows, hipStream_t st) {
     hipLaunchKernelGGL((token_logprobs_grad_part_kernel<DT, ENT>), grid, block, 0, st, a);
     return;
   }
-  const dim3 grid((unsigned)rows);
   const int n_vec = (a.V + Elem<DT>::per_vec - 1) / Elem<DT>::per_vec;
+  auto go = [&](auto kernel, int lanes) {
+    in_launches(rows, lanes, [&](long long first, dim3 grid) {
+      a.first = first;
+      hipLaunchKernelGGL(kernel, grid, dim3(lanes), 0, st, a);
+    });
+  };
   // lanes and registers by the row's length, so that a short row leaves the compute unit room for others
-  if (n_vec <= 256 * 8) hipLaunchKernelGGL((token_logprobs_grad_kernel<DT, 256, 8, 6, ENT>), grid, dim3(256), 0, st, a);
-  else if (n_vec <= 512 * 8) hipLaunchKernelGGL((token_logprobs_grad_kernel<DT, 512, 8, 6, ENT>), grid, dim3(512), 0, st, a);
-  else if (n_vec <= 512 * 16) hipLaunchKernelGGL((token_logprobs_grad_kernel<DT, 512, 12, 5, ENT>), grid, dim3(512), 0, st, a);
-  else hipLaunchKernelGGL((token_logprobs_grad_kernel<DT, 1024, 19, 4, ENT>), grid, dim3(1024), 0, st, a);
+  if (n_vec <= 256 * 8) go(token_logprobs_grad_kernel<DT, 256, 8, 6, ENT>, 256);
+  else if (n_vec <= 512 * 8) go(token_logprobs_grad_kernel<DT, 512, 8, 6, ENT>, 512);
+  else if (n_vec <= 512 * 16) go(token_logprobs_grad_kernel<DT, 512, 12, 5, ENT>, 512);
+  else go(token_logprobs_grad_kernel<DT, 1024, 19, 4, ENT>, 1024);
 }
 
 // Parts and, with alternatives, the lanes' keys of the rows that are divided.
