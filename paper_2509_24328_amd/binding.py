@@ -473,10 +473,17 @@ def _strided(z):
     columns [:V] of a contiguous tensor with wider rows do; other layouts are refused."""
     if z.is_cuda and z.is_contiguous():
         return z.data_ptr(), z.shape[-1]
-    stride = z.stride(-2) if z.dim() >= 2 else 0
-    ok = z.is_cuda and z.dim() >= 2 and (z.stride(-1) == 1 or z.shape[-1] == 1) and stride >= z.shape[-1]
-    for d in range(z.dim() - 2):
-        ok = ok and (z.shape[d] == 1 or z.stride(d) == z.stride(d + 1) * z.shape[d + 1])
+    V = z.shape[-1]
+    ok = z.is_cuda and z.dim() >= 2 and (z.stride(-1) == 1 or V == 1)
+    stride, rows = V, 1
+    for d in range(z.dim() - 2, -1, -1):
+        if z.shape[d] == 1:                # (where one of these lies from the next is of no account)
+            continue
+        if rows == 1:
+            stride = z.stride(d)
+        ok = ok and z.stride(d) == stride * rows
+        rows *= z.shape[d]
+    ok = ok and stride >= V
     if not ok:
         raise ValueError("sv: logits must be device tensors whose rows are contiguous and equally far apart "
                          f"(got device={z.device}, shape={tuple(z.shape)}, strides={z.stride()})")
