@@ -601,7 +601,8 @@ int sv_accept_ratio_sparse(const int32_t* count_t, const int32_t* token_t, const
  *   top_token, top_logprob   the first n_top entries of that order
  *   z       dense [B, P, V], or packed [n_rows, V] with t_offsets_or_null [B+1]: position
  *           (b, i) is row t_offsets[b] + i for i < t_offsets[b+1] - t_offsets[b] and not
- *           there otherwise; rows addressed outside [0, n_rows) are bad rows, never read.
+ *           there otherwise; rows addressed outside [0, n_rows) are bad rows, never read (n_rows = 0:
+ *           z may be NULL).
  *           Consecutive rows lie z_stride >= V elements apart (rows padded to a multiple)
  *   tokens_or_null [B, P] int32   -1: no token at this position.  NULL: no token is asked
  *           for, all rows are swept; logprob and rank must be NULL then

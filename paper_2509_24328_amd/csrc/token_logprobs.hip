@@ -876,7 +876,8 @@ extern "C" int sv_token_logprobs(const void* z, int64_t z_stride, const int32_t*
   SV_REQUIRE(scale_of(temperature, &a.sc), SV_ERR_INVALID_ARG);
   SV_REQUIRE(V <= (1 << 24) && n_top <= SV_TOP_MAX && (long long)B * P <= 0x7fffffffLL, SV_ERR_TOO_LARGE);
   if (B == 0) return SV_OK;
-  SV_REQUIRE(z && (tokens_or_null || (!logprob_or_null && !rank_or_null)), SV_ERR_NULL);
+  SV_REQUIRE(z || (t_offsets_or_null && n_rows == 0), SV_ERR_NULL);      // (no row: torch gives NULL as its address)
+  SV_REQUIRE(tokens_or_null || (!logprob_or_null && !rank_or_null), SV_ERR_NULL);
   SV_REQUIRE(n_top == 0 || (top_token_or_null && top_logprob_or_null), SV_ERR_NULL);
   SV_REQUIRE(is_aligned(z, elem_bytes(dtype)) && is_aligned(t_offsets_or_null, 4) && is_aligned(tokens_or_null, 4) &&
                  is_aligned(logprob_or_null, 4) && is_aligned(lse_or_null, 4) && is_aligned(entropy_or_null, 4) &&

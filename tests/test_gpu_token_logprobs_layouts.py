@@ -1,4 +1,6 @@
-"""Layouts of logits that the scoring calls take: positions picked out of a tensor, dimensions of one and wider rows."""
+"""Layouts of logits that the scoring calls take: positions picked out of a tensor, dimensions of one, wider rows, and packed
+logits without a row."""
+import numpy as np
 import pytest
 import torch
 
@@ -48,3 +50,17 @@ def test_layouts_refused():
         with pytest.raises(ValueError):
             n = bad.numel() // bad.shape[-1]
             P.sv_token_logprobs(bad, tok.new_zeros(n), f.new_zeros(n))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_packed_logits_without_a_row(dtype):
+    """No position is there (a step in which every sequence has ended); offsets that say otherwise point at bad rows."""
+    B, Pn, V = 3, 2, 50
+    z = torch.empty((0, V), dtype=dtype, device="cuda")
+    tok = torch.ones((B, Pn), dtype=torch.int32, device="cuda")
+    got = score(z, tok, 2, offsets=torch.zeros(B + 1, dtype=torch.int32, device="cuda"))
+    for k in ("logprob", "lse", "entropy", "rank", "flags"):
+        assert not got[k].any(), k
+    assert (got["top_token"] == -1).all() and (got["top_logprob"] == -np.inf).all()
+    got = score(z, tok, 2, offsets=torch.tensor([0, 1, 1, 1], dtype=torch.int32, device="cuda"))
+    assert got["flags"].tolist() == [[1, 0], [0, 0], [0, 0]] and np.isnan(got["logprob"][0, 0])
