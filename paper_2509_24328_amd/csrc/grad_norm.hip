@@ -190,13 +190,14 @@ __global__ __launch_bounds__(kNormThreads) void grad_scale_kernel(const TensorBa
   }
 }
 
-inline int batches(int n) { return n == 0 ? 1 : (n + kTensors - 1) / kTensors; }
+inline int batches(int n) { return n == 0 ? 1 : (n - 1) / kTensors + 1; }
 
-// Tensors i0 .. of the lists, as one launch's arguments.
-inline TensorBatch batch_of(int i0, int n, const void* const* grads, const int64_t* numel, const int* dtype,
+// Batch k of the lists' tensors, as one launch's arguments.
+inline TensorBatch batch_of(int k, int n, const void* const* grads, const int64_t* numel, const int* dtype,
                             void* const* out, const int* out_dtype) {
   TensorBatch b = {};
-  for (int i = i0; i < n && i < i0 + kTensors; ++i) {
+  const int first = k * kTensors, here = n - first < kTensors ? n - first : kTensors;
+  for (int i = first; i - first < here; ++i) {
     if (numel[i] == 0) continue;
     b.t[b.n++] = {grads[i], out ? out[i] : nullptr, numel[i], b.granules, (uint16_t)dtype[i],
                   (uint16_t)(out ? out_dtype[i] : 0)};
@@ -236,8 +237,8 @@ int norm_and_scale(int n, const void* const* grads, const int64_t* numel, const 
   double* part = reinterpret_cast<double*>(static_cast<char*>(ws) + kWsAlign);
   hipStream_t st = as_stream(stream);
   int parts = 0;
-  for (int i = 0; i < n; i += kTensors) {
-    const TensorBatch b = batch_of(i, n, grads, numel, dtype, out, out_dtype);
+  for (int k = 0; k < batches(n); ++k) {
+    const TensorBatch b = batch_of(k, n, grads, numel, dtype, out, out_dtype);
     if (b.granules == 0) continue;
     const unsigned groups = b.granules < (uint32_t)kNormGroups ? b.granules : kNormGroups;
     hipLaunchKernelGGL(grad_norm_kernel, dim3(groups), dim3(kNormThreads), 0, st, b, part + parts);
@@ -246,8 +247,8 @@ int norm_and_scale(int n, const void* const* grads, const int64_t* numel, const 
   const bool apart = !out || parts == 0 || n > kTensors;
   if (apart)
     hipLaunchKernelGGL(grad_norm_finish_kernel, dim3(1), dim3(kNormThreads), 0, st, part, parts, max_norm, norm, flag, factor);
-  for (int i = (batches(n) - 1) * kTensors; out && i >= 0; i -= kTensors) {
-    const TensorBatch b = batch_of(i, n, grads, numel, dtype, out, out_dtype);
+  for (int k = batches(n) - 1; out && k >= 0; --k) {
+    const TensorBatch b = batch_of(k, n, grads, numel, dtype, out, out_dtype);
     if (b.granules == 0) continue;
     const unsigned groups = b.granules < 2u * kNormGroups ? b.granules : 2u * kNormGroups;
     const Finish f = {apart ? nullptr : part, parts, max_norm, norm, flag, factor};
