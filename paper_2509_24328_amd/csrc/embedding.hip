@@ -631,7 +631,6 @@ void launch_sums(const GradRows& a, const int32_t* ids, hipStream_t st) {
     hipLaunchKernelGGL((embedding_grad_pieces_kernel<DTG, DTW, true>), grid, dim3(kEmbThreads), 0, st, a);
   else
     hipLaunchKernelGGL((embedding_grad_pieces_kernel<DTG, DTW, false>), grid, dim3(kEmbThreads), 0, st, a);
-  if (a.n <= a.piece) return;
   const int lanes = a.lanes < kJoinLanes ? a.lanes : kJoinLanes, chunks = (a.D + kChunkCols - 1) / kChunkCols;
   const int join_per = kJoinPieces * a.piece;
   const dim3 join((unsigned)(((long long)a.n + join_per - 1) / join_per), (unsigned)((chunks + lanes - 1) / lanes));
