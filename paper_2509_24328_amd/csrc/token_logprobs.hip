@@ -526,8 +526,9 @@ __global__ __launch_bounds__(NT, 8) void token_logprobs_kernel(const ScoreArgs a
 }
 
 // Several workgroups to a row: first its parts, then one workgroup a row for the results.  A compute unit needs 10 us for the
-// instructions of 152064 entries, so one row takes 13 us this way (5 of them the parts) and 20 with a workgroup; 316 rows
-// 28 and 38 us, bound by the start and the end of each launch and the rest by HBM.
+// instructions of 152064 bf16 entries and longer for their loads one round after the other, so one row takes 14 us this way and 31 with a
+// workgroup (entropy, rank, 20 alternatives; 9 and 26 without these); 316 rows 40 and 48 us, bound by the start and the end of each launch
+// and the rest by HBM.
 template <int DT, bool ENT, bool TOP>
 __global__ __launch_bounds__(kPartThreads, 8) void token_logprobs_part_kernel(const ScoreArgs a) {
   __shared__ RowScratch sm;
@@ -576,9 +577,20 @@ __global__ __launch_bounds__(kPartThreads) void token_logprobs_join_kernel(const
 
 inline int round_up(int n, int to) { return (n + to - 1) / to * to; }
 
-// A row is divided where there are fewer rows than the chip has places for workgroups, into parts of whole rounds of
-// loads; one of few rounds is not, since the second launch costs what is saved.
-constexpr int kPlaces = 4096, kFewRounds = 10;
+// A call with few rows of many rounds of loads divides each into parts of whole rounds, as many as give the chip its places for
+// workgroups.  One workgroup to a row / divided, us, with entropy and rank:
+//  by rounds: without alternatives 6, 10 and 16 rounds of bf16, 1 row 10.7/8.6, 15.0/8.8, 23.2/8.5; 144 rows 12.3/12.2, 17.9/14.2, 26.4/17.6;
+//    f32, 1 row 7.3/8.6, 9.9/8.5, 14.9/8.2; 144 rows 9.9/10.5, 13.5/12.1, 19.6/14.4.  With 20, whose join is longer, bf16, 1 row 14.1/13.5,
+//    18.6/13.7, 26.8/13.9; 144 rows 16.7/18.5, 21.5/21.4, 30.9/25.7; f32, 1 row 10.9/12.2, 13.4/12.5, 18.9/12.5; 144 rows 13.1/16.5, 17.1/18.6,
+//    23.4/21.9.  Ten rounds is where calls with alternatives meet; those without meet at six to eight, and lose up to 6 us by one line for both.
+//  by rows, without / with 20 alternatives: bf16 x 152064, 256 rows 31.2/27.1, 36.1/34.5; 682 rows 51.4/50.8, 63.9/63.0; 1024 rows 66.8/69.4,
+//    79.7/87.4.  f32 x 152064, 256 rows 40.2/31.7, 50.1/41.0; 682 rows 68.7/74.9, 83.2/91.1.  bf16 x 80000, 256 rows 19.1/19.0, 23.3/26.1; 682
+//    rows 31.1/34.4, 37.6/41.5.  f32 x 40000, 144 rows 13.8/12.2, 17.4/18.7; 256 rows 14.7/15.6, 18.7/22.4; 682 rows 24.3/28.4, 29.6/36.3.
+//    682 is where long bf16 rows meet; shorter and f32 ones meet at 150 to 400 and lose up to a quarter between there and the line.
+//  gradient, by rows (divided, it reads the logits twice): bf16 x 152064, 64 rows 25.7/18.2, 96 rows 26.3/24.1, 128 rows 26.8/28.6, 192 rows
+//    28.4/40.2.  f32 x 152064, 96 rows 37.3/34.9, 128 rows 42.6/46.0.  bf16 x 80000, 96 rows 17.6/17.1, 128 rows 17.7/19.2.  f32 x 40000, 64 rows
+//    12.6/12.2, 96 rows 12.9/14.5, 192 rows 14.7/21.6.
+constexpr int kPlaces = 4096, kFewRounds = 10, kScoreRows = 682, kGradRows = 96;
 inline Split whole_row(int V, int dtype) {
   const int per_vec = 16 / elem_bytes(dtype);
   return {1, (V + per_vec - 1) / per_vec};
@@ -592,7 +604,6 @@ inline Split split_of(long long rows, int V, int dtype, int max_rows) {
   const int vecs = (rounds + n - 1) / n * kRound;
   return {(whole.vecs + vecs - 1) / vecs, vecs};
 }
-constexpr int kScoreRows = 682, kGradRows = 192;
 
 template <int DT, bool ENT>
 void launch_score(ScoreArgs a, long long rows, hipStream_t st) {

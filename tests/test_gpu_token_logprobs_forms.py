@@ -36,7 +36,7 @@ def blank(got, rows, n_top=0):
 
 
 # ---------------------------------------------------------------------------
-# gradient: one workgroup to a row (more than 192 rows)
+# gradient: one workgroup to a row (more than 96 rows)
 # ---------------------------------------------------------------------------
 # vectors of a row: up to 2048, 4096 and 8192 have 8, 8 and 12 registers of 256, 512 and 512 lanes (6144 vectors of the last), longer ones 19
 # of 1024 (19456): below, at and above each of these, with and without entries past the last whole vector
@@ -58,7 +58,7 @@ def test_gradient_by_one_workgroup(vectors, dtype, entropy, in_place, over):
 
 
 # ---------------------------------------------------------------------------
-# rows that several workgroups share: from ten rounds of 1024 vectors on, up to 192 rows (gradient) and 682
+# rows that several workgroups share: from ten rounds of 1024 vectors on, up to 96 rows (gradient) and 682
 # ---------------------------------------------------------------------------
 def conditions(N, V, dtype, seed):
     """Rows with NaN, +inf, nothing left, the lowest number alone, a masked token, one entry left, and what is wrong in one part only."""
