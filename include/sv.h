@@ -16,7 +16,9 @@
  * produces the table, the sampling warps (temperature, top-k, top-p,
  * repetition penalty) with dense and compacted forms of the step, what is done
  * with the emitted tokens and with the models that drafted them (log-probabilities
- * of tokens and their gradient, embedding rows and theirs, gradient norm), and helpers.
+ * of tokens and their gradient, embedding rows and theirs, gradient norm), the model
+ * side of a step (rotary positions, a paged cache and the attention of new tokens over
+ * it, drawing tokens), and helpers.
  *
  * Conventions common to all calls
  *   - Every data pointer is a DEVICE pointer owned by the caller.  The library
@@ -58,6 +60,8 @@ extern "C" {
 typedef void* sv_stream_t;
 
 enum { SV_F32 = 0, SV_BF16 = 1 };
+/* Storage type of a cache alone: float8 e4m3 (no infinities), with a float32 scale for each token and head. */
+enum { SV_F8 = 2 };
 enum { SV_BATCH_GREEDY = 0, SV_PER_SEQUENCE = 1 };
 
 enum {
@@ -87,7 +91,8 @@ enum {
                                      draft normalisers of these arguments (no sv_row_stats call
                                      on it, or one with another z_d, x, shape, dtype, draft
                                      temperature or draft cutoffs): the draft rows count as bad   */
-  SV_FLAG_NONFINITE = 128         /* sv_grad_norm, sv_clip_grad_norm: the norm is not finite      */
+  SV_FLAG_NONFINITE = 128,        /* sv_grad_norm, sv_clip_grad_norm: the norm is not finite      */
+  SV_FLAG_BAD_PAGE = 256          /* a position that is written, read or seen lies in no page of the cache */
 };
 
 /* Largest B*k accepted by sv_select_length (keys are sorted in one workgroup). */
@@ -105,6 +110,17 @@ enum {
 #define SV_TOP_MAX 32
 /* Largest number of tokens one sv_embedding_grad call takes. */
 #define SV_EMBEDDING_MAX_TOKENS (1 << 24)
+
+/* Largest width of a head of the calls on positions and caches, and of sv_chunk_attention. */
+#define SV_HEAD_MAX 1024
+#define SV_ATTENTION_HEAD_MAX 256
+/* Largest number of heads, and of tokens a page. */
+#define SV_HEADS_MAX 1024
+#define SV_PAGE_MAX 65536
+
+/* What of a head's columns turns together (sv_rope), and how frequencies are stretched (sv_rope_frequencies). */
+enum { SV_ROPE_HALVES = 0, SV_ROPE_PAIRS = 1 };
+enum { SV_ROPE_PLAIN = 0, SV_ROPE_LINEAR = 1, SV_ROPE_NTK = 2, SV_ROPE_PARTS = 3 };
 
 /* Device scratch that sv_verify_sample_static holds on every GPU it runs on. */
 #define SV_STATIC_SCRATCH_BYTES (1 << 20)
@@ -705,6 +721,130 @@ int sv_grad_norm(int n, const void* const* grads, const int64_t* numel, const in
 int sv_clip_grad_norm(int n, const void* const* grads, const int64_t* numel, const int* dtype, float max_norm,
                       void* const* out, const int* out_dtype, float* norm, uint32_t* flag_or_null,
                       void* ws, size_t ws_bytes, sv_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The model side of a step: a draft draws its tokens, and the target looks at
+ * the gamma[b] + 1 selected positions of every sequence, whose number only the
+ * device knows (t_offsets of sv_select_length).  Queries and keys turn by their
+ * position, keys and values go into the pages of a cache, and the new tokens
+ * attend over them.  A step that accepts n of the drafted tokens goes on from
+ * lengths[b] + n + 1: the cache's rows behind that are written again.
+ *
+ * New tokens.  Sequence b has new tokens i = 0 .. n_b - 1, at positions
+ * lengths[b] + i, in rows of [n_rows, ...] tensors:
+ *   t_offsets_or_null [B+1]  rows t_offsets[b] .. t_offsets[b+1]-1 are sequence b's (ascending; at most P of
+ *                            them, others are not touched); rows that are no sequence's are not touched.
+ *                            NULL: row b * P + i, n_b = P (n_rows is ignored)
+ *   lengths [B] int32        tokens of each sequence before its new ones
+ * Rows lie *_stride elements apart, the heads of a row one after the other.
+ *
+ * The cache.  k_cache, v_cache [n_pages, heads, page, D] of cache_dtype: the dtype of the call, or SV_F8 with
+ * k_scale, v_scale [n_pages, heads, page] float (NULL otherwise): a column is code * scale,
+ *   scale = max(amax / 448, 2^-126) over the columns of the token's head (1 if all are 0),  code = e4m3(x / scale)
+ * in float32, each rounded to nearest-even; a head with a NaN or an infinity gets the scale NaN.
+ *   pages [B, max_pages] int32   physical page of positions page * j .. page * j + page - 1 of the sequence.  Entries that
+ *                            no position of the call needs are not read
+ * A position whose entry is outside [0, n_pages), or that lies behind the last entry, is in no page
+ * (SV_FLAG_BAD_PAGE): it is not written, and what is read from or computed with it is NaN.  A length below 0 counts
+ * as one behind the last entry.  Two new tokens must not share a place of the cache.
+ * Limits: D <= SV_HEAD_MAX, heads <= SV_HEADS_MAX, page <= SV_PAGE_MAX.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * Angle per position of every pair of the rot turned columns, pairs j = 0 .. rot / 2 - 1:
+ *   SV_ROPE_PLAIN   f_j = base^(-2 j / rot)
+ *   SV_ROPE_LINEAR  f_j / factor
+ *   SV_ROPE_NTK     base * factor^(rot / (rot - 2)) for base (base itself where rot = 2)
+ *   SV_ROPE_PARTS   f_j / factor (1 - r) + f_j r  with r = (turns - low) / (high - low) in [0, 1], turns = length f_j / (2 pi):
+ *                   pairs that turn at least `high` times over the `length` tokens trained on stay, those below `low` are stretched
+ *   freq [rot / 2] double   out.   rot even, base > 1, factor > 0, 0 <= low < high (each where it is used).
+ */
+int sv_rope_frequencies(int rot, double base, int scaling, double factor, double low, double high, int length,
+                        double* freq, sv_stream_t stream);
+
+/*
+ * Rotary positions: of each head's leading rot columns, pairs (a, b) turn by t = positions[i] * freq[j],
+ *   a' = amplitude (a cos t - b sin t),  b' = amplitude (b cos t + a sin t)
+ * (columns j and j + rot / 2 with SV_ROPE_HALVES, 2 j and 2 j + 1 with SV_ROPE_PAIRS); the others are copied.
+ * Angles, sines and products in float64, rounded once.  inverse != 0: by -t, the gradient of x from that of out.
+ *   x, out [n, H, D] dtype     out may be x itself (same address and stride), and must not overlap it otherwise
+ *   positions [n] int32        rows of a negative one are left as they are
+ *   freq [rot / 2] double      of sv_rope_frequencies, or any
+ * amplitude > 0; rot even, 2 <= rot <= D.
+ */
+int sv_rope(const void* x, int64_t x_stride, const int32_t* positions, int n, int H, int D, int dtype,
+            const double* freq, int rot, int layout, float amplitude, int inverse, void* out,
+            int64_t out_stride, sv_stream_t stream);
+
+/*
+ * Keys and values of the new tokens into the cache, in one launch with the rotation of keys and queries:
+ *   k, v  [n_rows, heads, D] dtype   in   k turns by lengths[b] + i before it is stored (freq_or_null NULL: it does not)
+ *   q_or_null, q_out_or_null [n_rows, Hq, D] dtype   in, out   turned (or copied); q_out may be q itself (same stride).
+ *                                    Both or neither
+ *   flags_or_null [n_rows] uint32    out  SV_FLAG_BAD_PAGE; q_out of such a row is still written
+ * The rest as above; rot, layout and amplitude as for sv_rope (ignored without freq).
+ */
+int sv_cache_write(const void* k, int64_t k_stride, const void* v, int64_t v_stride, const void* q_or_null,
+                   int64_t q_stride, int Hq, void* q_out_or_null, int64_t q_out_stride,
+                   const int32_t* t_offsets_or_null, int n_rows, const int32_t* lengths, const int32_t* pages,
+                   int max_pages, int B, int P, int heads, int D, int dtype, const double* freq_or_null, int rot,
+                   int layout, float amplitude, void* k_cache, void* v_cache, int cache_dtype,
+                   float* k_scale_or_null, float* v_scale_or_null, int n_pages, int page, uint32_t* flags_or_null,
+                   sv_stream_t stream);
+
+/*
+ * Rows of a cache as dense tensors: k, v [n_rows, heads, D] dtype (out) of positions start[b] + i, rounded once.
+ *   flags_or_null [n_rows] uint32    out  SV_FLAG_BAD_PAGE: the row is NaN
+ */
+int sv_cache_read(const void* k_cache, const void* v_cache, int cache_dtype, const float* k_scale_or_null,
+                  const float* v_scale_or_null, int n_pages, int page, const int32_t* t_offsets_or_null, int n_rows,
+                  const int32_t* start, const int32_t* pages, int max_pages, int B, int P, int heads, int D, int dtype,
+                  void* k, int64_t k_stride, void* v, int64_t v_stride, uint32_t* flags_or_null, sv_stream_t stream);
+
+/* Bytes of device scratch with which sv_chunk_attention divides the keys of a row among workgroups where there are few rows (0: it
+ * never does, or the shape is invalid). */
+size_t sv_chunk_attention_workspace_bytes(int B, int P, int Hq, int heads, int D, int dtype, int max_pages, int page);
+
+/*
+ * Attention of the new tokens over the cache, which holds their own keys and values already (sv_cache_write):
+ *   out[i, h] = sum_j w_j v_j,  w = soft-max over j of  scale <q[i, h], k_j>   (head h of the queries reads head h / (Hq / heads))
+ *   lse[i, h] = log sum_j exp(scale <q[i, h], k_j>)
+ * over the positions j with  max(first[b], p - window + 1) <= j <= p,  p = lengths[b] + i  (window 0: no such bound).
+ *   q, out [n_rows, Hq, D] dtype      in, out  (no overlap)
+ *   first_or_null [B] int32           in   first position that may be seen (padding on the left, pages given back); below 0: 0
+ *   lse_or_null [n_rows, Hq] float    out
+ *   flags_or_null [n_rows] uint32     out  SV_FLAG_BAD_PAGE: a position that the row sees is in no page; out and lse are NaN
+ *   ws_or_null                        256-byte aligned, of sv_chunk_attention_workspace_bytes.  Without it one workgroup goes through
+ *                                     all keys of its rows: the same results, but for the order of the sums, in more time
+ * A row that sees no position, or only scores of -inf: out 0, lse -inf.  What the cache holds at positions that a row does not see
+ * does not matter to it, NaN and infinities included.  Scores, weights and sums are float32, weights rounded to bfloat16 before they
+ * multiply bfloat16 (or 8-bit) values for bfloat16 queries; out is rounded once.
+ * Hq a multiple of heads, D a multiple of 8 and <= SV_ATTENTION_HEAD_MAX, B * P * Hq <= 2^28, window >= 0.
+ */
+int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t* t_offsets_or_null, int n_rows,
+                       const int32_t* lengths, const int32_t* first_or_null, const int32_t* pages, int max_pages, int B,
+                       int P, int Hq, int heads, int D, int dtype, const void* k_cache, const void* v_cache,
+                       int cache_dtype, const float* k_scale_or_null, const float* v_scale_or_null, int n_pages,
+                       int page, float scale, int window, void* out, int64_t out_stride, float* lse_or_null,
+                       uint32_t* flags_or_null, void* ws_or_null, size_t ws_bytes, sv_stream_t stream);
+
+/*
+ * A token of every row, drawn with a given random number under temperature, top-k, top-p and min-p, in that order:
+ *   w_v = exp((z_v - max z) / temperature);  top_k > 0: entries below the K-th largest value are dropped;  top_p < 1: of the entries left,
+ *   groups of equal value are kept from the top until their mass reaches top_p of the mass left;  then entries with
+ *   w_v < min_p are dropped (min_p times the most probable entry's probability; 0: none)
+ *   token   = the smallest v whose inclusive cumulative weight over ascending token ids exceeds u W, W = sum of all kept
+ *   logprob = log(w_token / W)
+ *   z  [rows, V] dtype, rows z_stride >= V elements apart    in
+ *   u  [rows] double in [0, 1)      in   (outside: the nearest number inside; sv_uniforms makes such numbers)
+ *   token [rows] int32, logprob_or_null [rows] float         out
+ *   flags_or_null [rows] uint32     out  SV_FLAG_BAD_ROW (also where u is NaN): token -1, logprob NaN
+ * Weights and sums are float64, in an order that the sizes fix: the same call gives the same tokens.
+ * 0 < top_p, 0 <= min_p <= 1, temperature in [1e-3, 1e3], V <= 16777216.
+ */
+int sv_sample(const void* z, int64_t z_stride, int rows, int V, int dtype, float temperature, int top_k, float top_p,
+              float min_p, const double* u, int32_t* token, float* logprob_or_null, uint32_t* flags_or_null,
+              sv_stream_t stream);
 
 /*
  * The uniforms sv_verify_sample draws (for tests and for callers that want to

@@ -15,7 +15,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsv.so")
 
-SV_F32, SV_BF16 = 0, 1
+SV_F32, SV_BF16, SV_F8 = 0, 1, 2
 SV_BATCH_GREEDY, SV_PER_SEQUENCE = 0, 1
 SV_OK = 0
 SV_ERR_INVALID_ARG, SV_ERR_NULL, SV_ERR_DTYPE, SV_ERR_ALIGN = -1, -2, -3, -4
@@ -24,6 +24,7 @@ FLAG_BAD_ROW, FLAG_NEAR_TIE, FLAG_RESIDUAL_FALLBACK, FLAG_NEAR_CDF_EDGE, FLAG_BA
 FLAG_NOT_COMPACT = 32
 FLAG_NO_CHAIN = 64
 FLAG_NONFINITE = 128
+FLAG_BAD_PAGE = 256
 SV_SUPPORT_MAX_CAP = 1024
 SV_SELECT_MAX_KEYS = 8192
 SV_MAX_K = 64
@@ -39,11 +40,15 @@ EXPORTS = ("sv_strerror", "sv_workspace_bytes", "sv_row_stats", "sv_accept_estim
            "sv_repetition_penalty_multi", "sv_token_logprobs", "sv_token_logprobs_grad",
            "sv_token_logprobs_workspace_bytes", "sv_embedding",
            "sv_embedding_grad_workspace_bytes", "sv_embedding_grad", "sv_grad_norm_workspace_bytes", "sv_grad_norm",
-           "sv_clip_grad_norm")
+           "sv_clip_grad_norm", "sv_rope_frequencies", "sv_rope", "sv_cache_write", "sv_cache_read",
+           "sv_chunk_attention", "sv_chunk_attention_workspace_bytes", "sv_sample")
 SV_WARP_MAX_TENSORS = 8
 SV_STATIC_SCRATCH_BYTES = 1 << 20
 SV_TOP_MAX = 32
 SV_EMBEDDING_MAX_TOKENS = 1 << 24
+SV_HEAD_MAX, SV_ATTENTION_HEAD_MAX, SV_HEADS_MAX, SV_PAGE_MAX = 1024, 256, 1024, 65536
+SV_ROPE_HALVES, SV_ROPE_PAIRS = 0, 1
+SV_ROPE_PLAIN, SV_ROPE_LINEAR, SV_ROPE_NTK, SV_ROPE_PARTS = 0, 1, 2, 3
 (SV_KERNEL_ROW_STATS, SV_KERNEL_ACCEPT_ESTIMATE, SV_KERNEL_SELECT_LENGTH, SV_KERNEL_VERIFY_ROWS,
  SV_KERNEL_VERIFY_MASS, SV_KERNEL_VERIFY_PICK, SV_KERNEL_COUNT) = range(7)
 
@@ -136,6 +141,23 @@ lib.sv_grad_norm.restype = _i
 lib.sv_grad_norm.argtypes = [_i, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 lib.sv_clip_grad_norm.restype = _i
 lib.sv_clip_grad_norm.argtypes = [_i, _vp, _vp, _vp, _f, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_d = ctypes.c_double
+lib.sv_rope_frequencies.restype = _i
+lib.sv_rope_frequencies.argtypes = [_i, _d, _i, _d, _d, _d, _i, _vp, _vp]
+lib.sv_rope.restype = _i
+lib.sv_rope.argtypes = [_vp, _ll, _vp, _i, _i, _i, _i, _vp, _i, _i, _f, _i, _vp, _ll, _vp]
+lib.sv_cache_write.restype = _i
+lib.sv_cache_write.argtypes = [_vp, _ll, _vp, _ll, _vp, _ll, _i, _vp, _ll, _vp, _i, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _i, _i,
+                               _f, _vp, _vp, _i, _vp, _vp, _i, _i, _vp, _vp]
+lib.sv_cache_read.restype = _i
+lib.sv_cache_read.argtypes = [_vp, _vp, _i, _vp, _vp, _i, _i, _vp, _i, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _ll, _vp, _ll, _vp, _vp]
+lib.sv_chunk_attention_workspace_bytes.restype = _sz
+lib.sv_chunk_attention_workspace_bytes.argtypes = [_i, _i, _i, _i, _i, _i, _i, _i]
+lib.sv_chunk_attention.restype = _i
+lib.sv_chunk_attention.argtypes = [_vp, _ll, _vp, _i, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _vp, _vp, _i, _vp, _vp, _i, _i, _f, _i,
+                                   _vp, _ll, _vp, _vp, _vp, _sz, _vp]
+lib.sv_sample.restype = _i
+lib.sv_sample.argtypes = [_vp, _ll, _i, _i, _i, _f, _i, _f, _f, _vp, _vp, _vp, _vp, _vp]
 lib.sv_set_timing_events.restype = _i
 lib.sv_set_timing_events.argtypes = [_i, _vp, _vp]
 
@@ -656,3 +678,218 @@ def sv_clip_grad_norm(grads, max_norm, norm, out=None, flag=None, ws=None, strea
     _check(lib.sv_clip_grad_norm(len(tags), _host(ptrs), _host(numel), _host(tags), max_norm, _host(o_ptrs),
                                  _host(o_tags), _ptr(norm), _ptr(flag), _ptr(ws), 0 if ws is None else ws.numel(),
                                  _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# the model side of a step
+# ---------------------------------------------------------------------------
+def _device_of(t, *others):
+    """Refuses tensors of another device than the first one's, and a first one of another than the current device, whose
+    streams the calls run on."""
+    here = t.device
+    if here.type != "cuda" or (here.index is not None and here.index != torch.cuda.current_device()):
+        raise ValueError(f"sv: tensors must lie on the current device (got {here})")
+    for o in others:
+        if o is not None and o.device != here:
+            raise ValueError(f"sv: tensors of several devices ({here}, {o.device})")
+
+
+def _heads(t):
+    """(address, elements from row to row) of [..., H, D] whose heads follow each other and whose rows lie at one distance, as
+    columns of a wider projection do."""
+    if not t.is_cuda or t.dim() < 3 or t.dtype not in _TAGS:
+        raise ValueError("sv: rows of heads must be device tensors [..., heads, D] in float32 or bfloat16 "
+                         f"(got device={t.device}, shape={tuple(t.shape)}, dtype={t.dtype})")
+    H, D = t.shape[-2:]
+    if t.is_contiguous():
+        return t.data_ptr(), H * D
+    ok = (t.stride(-1) == 1 or D == 1) and (t.stride(-2) == D or H == 1)
+    stride, rows = H * D, 1
+    for d in range(t.dim() - 3, -1, -1):
+        if t.shape[d] == 1:
+            continue
+        if rows == 1:
+            stride = t.stride(d)
+        ok = ok and t.stride(d) == stride * rows
+        rows *= t.shape[d]
+    if not ok or stride < H * D:
+        raise ValueError("sv: the heads of a row must follow each other and rows lie equally far apart "
+                         f"(got shape={tuple(t.shape)}, strides={t.stride()})")
+    return t.data_ptr(), stride
+
+
+class Cache:
+    """Keys and values of a model's layer in pages: k, v [n_pages, heads, page, D] in float32, bfloat16 or float8_e4m3fn, the last
+    one with float32 scales [n_pages, heads, page].  Takes tensors, or makes them (Cache.empty)."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        f8 = k.dtype == torch.float8_e4m3fn
+        if k.dim() != 4 or v.shape != k.shape:
+            raise SvError(SV_ERR_INVALID_ARG)
+        if v.dtype != k.dtype or not (f8 or k.dtype in _TAGS):
+            raise SvError(SV_ERR_DTYPE)
+        if f8 and (k_scale is None or v_scale is None):
+            raise SvError(SV_ERR_NULL)
+        if not f8 and (k_scale is not None or v_scale is not None):
+            raise SvError(SV_ERR_INVALID_ARG)
+        if f8:
+            _f32(k_scale, v_scale)
+            if k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3]:
+                raise SvError(SV_ERR_INVALID_ARG)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.heads, self.page, self.D = k.shape
+        self.dtype = SV_F8 if f8 else _TAGS[k.dtype]
+
+    @classmethod
+    def empty(cls, n_pages, heads, page, D, dtype=torch.bfloat16, device="cuda"):
+        k, v = (torch.empty((n_pages, heads, page, D), dtype=dtype, device=device) for _ in range(2))
+        if dtype != torch.float8_e4m3fn:
+            return cls(k, v)
+        return cls(k, v, *(torch.empty((n_pages, heads, page), dtype=torch.float32, device=device) for _ in range(2)))
+
+    def _ptrs(self):
+        return _ptr(self.k), _ptr(self.v), self.dtype, _ptr(self.k_scale), _ptr(self.v_scale), self.n_pages, self.page
+
+
+def _new_rows(rows, t_offsets, start, pages, P):
+    """(n_rows, B, P) of new tokens whose rows have the leading shape `rows`: [B, P], or [n_rows] with t_offsets [B+1] and P."""
+    _i32(t_offsets, start, pages)
+    if pages.dim() != 2 or start.numel() != pages.shape[0]:
+        raise SvError(SV_ERR_INVALID_ARG)
+    B = pages.shape[0]
+    if t_offsets is None:
+        if len(rows) != 2 or rows[0] != B or (P is not None and P != rows[1]):
+            raise SvError(SV_ERR_INVALID_ARG)
+        return rows[0] * rows[1], B, rows[1]
+    if len(rows) != 1 or P is None or t_offsets.numel() != B + 1:
+        raise SvError(SV_ERR_INVALID_ARG)
+    return rows[0], B, P
+
+
+def sv_rope_frequencies(freq, base=10000.0, scaling=SV_ROPE_PLAIN, factor=1.0, low=1.0, high=32.0, length=0, stream=None):
+    """freq: [rot / 2] float64."""
+    if freq.dtype != torch.float64:
+        raise SvError(SV_ERR_DTYPE)
+    _device_of(freq)
+    _check(lib.sv_rope_frequencies(2 * freq.numel(), base, scaling, factor, low, high, length, _ptr(freq), _stream(stream)))
+
+
+def _freq(freq):
+    if freq is None:
+        return None, 0
+    if freq.dtype != torch.float64:
+        raise SvError(SV_ERR_DTYPE)
+    return _ptr(freq), 2 * freq.numel()
+
+
+def sv_rope(x, positions, freq, out, layout=SV_ROPE_HALVES, amplitude=1.0, inverse=False, stream=None):
+    """x, out: [..., H, D], out may be x; positions: one int32 per row; freq: [rot / 2] float64."""
+    addr, stride = _heads(x)
+    o_addr, o_stride = _heads(out)
+    H, D = x.shape[-2:]
+    n = x.numel() // (H * D) if H * D else 0
+    if out.shape != x.shape or out.dtype != x.dtype or positions.numel() != n:
+        raise SvError(SV_ERR_INVALID_ARG)
+    _i32(positions)
+    _device_of(x, positions, freq, out)
+    f, rot = _freq(freq)
+    _check(lib.sv_rope(addr, stride, _ptr(positions), n, H, D, _dtype_tag(x), f, rot, layout, amplitude, int(inverse), o_addr,
+                       o_stride, _stream(stream)))
+
+
+def sv_cache_write(cache, k, v, lengths, pages, t_offsets=None, P=None, q=None, q_out=None, freq=None,
+                   layout=SV_ROPE_HALVES, amplitude=1.0, flags=None, stream=None):
+    """k, v: [B, P, heads, D]; or [n_rows, heads, D] with t_offsets [B+1] and P.  q, q_out: the same with the queries' heads.
+    pages: [B, max_pages].  freq None: nothing is turned."""
+    n_rows, B, P = _new_rows(k.shape[:-2], t_offsets, lengths, pages, P)
+    if v.shape != k.shape or v.dtype != k.dtype or tuple(k.shape[-2:]) != (cache.heads, cache.D):
+        raise SvError(SV_ERR_INVALID_ARG)
+    k_addr, k_stride = _heads(k)
+    v_addr, v_stride = _heads(v)
+    q_addr, q_stride, o_addr, o_stride, Hq = None, 0, None, 0, 0
+    if (q is None) != (q_out is None):
+        raise SvError(SV_ERR_NULL)
+    if q is not None:
+        if q.shape[:-2] != k.shape[:-2] or q.shape[-1] != cache.D or q_out.shape != q.shape:
+            raise SvError(SV_ERR_INVALID_ARG)
+        if q.dtype != k.dtype or q_out.dtype != k.dtype:
+            raise SvError(SV_ERR_DTYPE)
+        q_addr, q_stride = _heads(q)
+        o_addr, o_stride = _heads(q_out)
+        Hq = q.shape[-2]
+    if flags is not None:
+        _i32(flags)
+        _outputs((n_rows,), flags)
+    _device_of(k, v, cache.k, q, q_out, lengths, pages, t_offsets, freq, flags)
+    f, rot = _freq(freq)
+    kc, vc, tag, ks, vs, n_pages, page = cache._ptrs()
+    _check(lib.sv_cache_write(k_addr, k_stride, v_addr, v_stride, q_addr, q_stride, Hq, o_addr, o_stride, _ptr(t_offsets), n_rows,
+                              _ptr(lengths), _ptr(pages), pages.shape[1], B, P, cache.heads, cache.D, _dtype_tag(k), f, rot, layout,
+                              amplitude, kc, vc, tag, ks, vs, n_pages, page, _ptr(flags), _stream(stream)))
+
+
+def sv_cache_read(cache, k, v, start, pages, t_offsets=None, P=None, flags=None, stream=None):
+    """k, v (out): [B, P, heads, D]; or [n_rows, heads, D] with t_offsets [B+1] and P: positions start[b] + i."""
+    n_rows, B, P = _new_rows(k.shape[:-2], t_offsets, start, pages, P)
+    if v.shape != k.shape or v.dtype != k.dtype or tuple(k.shape[-2:]) != (cache.heads, cache.D):
+        raise SvError(SV_ERR_INVALID_ARG)
+    k_addr, k_stride = _heads(k)
+    v_addr, v_stride = _heads(v)
+    if flags is not None:
+        _i32(flags)
+        _outputs((n_rows,), flags)
+    _device_of(k, v, cache.k, start, pages, t_offsets, flags)
+    kc, vc, tag, ks, vs, n_pages, page = cache._ptrs()
+    _check(lib.sv_cache_read(kc, vc, tag, ks, vs, n_pages, page, _ptr(t_offsets), n_rows, _ptr(start), _ptr(pages), pages.shape[1], B,
+                             P, cache.heads, cache.D, _dtype_tag(k), k_addr, k_stride, v_addr, v_stride, _ptr(flags),
+                             _stream(stream)))
+
+
+def sv_chunk_attention_workspace_bytes(B, P, Hq, heads, D, dtype, max_pages, page):
+    return int(lib.sv_chunk_attention_workspace_bytes(B, P, Hq, heads, D, dtype, max_pages, page))
+
+
+def sv_chunk_attention(cache, q, out, lengths, pages, t_offsets=None, P=None, scale=None, window=0, first=None, lse=None,
+                       flags=None, ws=None, stream=None):
+    """q, out: [B, P, Hq, D]; or [n_rows, Hq, D] with t_offsets [B+1] and P.  scale None: 1 / sqrt(D).  ws None: scratch is torch's."""
+    n_rows, B, P = _new_rows(q.shape[:-2], t_offsets, lengths, pages, P)
+    Hq, D = q.shape[-2:]
+    if out.shape != q.shape or out.dtype != q.dtype or D != cache.D:
+        raise SvError(SV_ERR_INVALID_ARG)
+    q_addr, q_stride = _heads(q)
+    o_addr, o_stride = _heads(out)
+    _i32(first, flags)
+    _f32(lse)
+    if first is not None:
+        _outputs((B,), first)
+    _outputs((n_rows, Hq), lse)
+    _outputs((n_rows,), flags)
+    _device_of(q, out, cache.k, lengths, pages, t_offsets, first, lse, flags, ws)
+    tag = _dtype_tag(q)
+    if ws is None:
+        n = lib.sv_chunk_attention_workspace_bytes(B, P, Hq, cache.heads, D, tag, pages.shape[1], cache.page)
+        if n > 0 and stream is None:
+            ws = torch.empty(n, dtype=torch.uint8, device=q.device)
+        elif n > 0:
+            with torch.cuda.stream(stream):
+                ws = torch.empty(n, dtype=torch.uint8, device=q.device)
+    kc, vc, c_tag, ks, vs, n_pages, page = cache._ptrs()
+    _check(lib.sv_chunk_attention(q_addr, q_stride, _ptr(t_offsets), n_rows, _ptr(lengths), _ptr(first), _ptr(pages), pages.shape[1],
+                                  B, P, Hq, cache.heads, D, tag, kc, vc, c_tag, ks, vs, n_pages, page,
+                                  D ** -0.5 if scale is None else scale, window, o_addr, o_stride, _ptr(lse), _ptr(flags), _ptr(ws),
+                                  0 if ws is None else ws.numel(), _stream(stream)))
+
+
+def sv_sample(z, u, token, logprob=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, flags=None, stream=None):
+    """z: [..., V]; u (float64), token (int32), logprob, flags: one entry per row."""
+    V = z.shape[-1]
+    rows = z.numel() // V if V else 0
+    if u.dtype != torch.float64:
+        raise SvError(SV_ERR_DTYPE)
+    _i32(token, flags)
+    _f32(logprob)
+    _outputs((rows,), u, token, logprob, flags)
+    _device_of(z, u, token, logprob, flags)
+    addr, stride = _strided(z)
+    _check(lib.sv_sample(addr, stride, rows, V, _dtype_tag(z), temperature, top_k, top_p, min_p, _ptr(u), _ptr(token), _ptr(logprob),
+                         _ptr(flags), _stream(stream)))

@@ -1,0 +1,201 @@
+// sv_chunk_attention: what the rows and the scratch decide, the join of divided keys, the flags.
+#include "attention.hpp"
+
+namespace sv {
+
+// Joins the parts of a row: a wavefront for each (new token, head).
+template <int ET>
+__global__ void __launch_bounds__(256) attention_join_kernel(AttnArgs a) {
+  const int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int hq = (int)(at % a.Hq);
+  const int64_t bi = at / a.Hq;
+  const int i = (int)(bi % a.rows.P), b = (int)(bi / a.rows.P);
+  if (b >= a.rows.B) return;
+  const Sequence s = sequence_of(a, b);
+  if (i >= s.n) return;
+  const int h = hq / a.group, rho = i * a.group + hq - h * a.group, tile = rho / a.tile_rows;
+  const int item = (b * a.pages.heads + h) * a.tiles + tile;
+  const int parts = a.n_split[item];
+  if (parts <= 1) return;
+  const int64_t part0 = (int64_t)item * a.splits * a.tile_rows + (rho - tile * a.tile_rows);
+  float m = -INFINITY, l = 0.f;
+  if (lane < parts) {
+    const int64_t p = part0 + (int64_t)lane * a.tile_rows;
+    m = a.part_ml[2 * p];
+    l = a.part_ml[2 * p + 1];
+  }
+  const float top = wave_max_f32(m);
+  const float f = m == top ? 1.f : exp2_fast(m - top);
+  const double total = wave_sum_f64(lane < parts ? (double)l * f : 0.0);
+  const bool out_of_pages = s.start + i >= s.cap;
+  const bool any = top != -INFINITY || !(total == 0.0);
+  const float inv = out_of_pages ? NAN : (any ? (float)(1.0 / total) : 0.f);
+  if (a.lse && lane == 0)
+    a.lse[(int64_t)(s.row0 + i) * a.Hq + hq] = out_of_pages ? NAN : (any ? (float)((top + log2(total)) * kLn2) : -INFINITY);
+  char* to = a.out + (int64_t)(s.row0 + i) * a.out_stride;
+  for (int col = 4 * lane; col < a.D; col += 4 * kWave) {
+    f32x4 o{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < parts; ++k) {
+      typedef f32x4 vec __attribute__((aligned(4)));
+      o += *reinterpret_cast<const vec*>(a.part_o + (part0 + (int64_t)k * a.tile_rows) * a.D + col) * lane_f32(f, k);
+    }
+    o *= inv;
+    if constexpr (ET == SV_F32) {
+      typedef f32x4 vec __attribute__((aligned(4)));
+      *reinterpret_cast<vec*>(to + ((int64_t)hq * a.D + col) * 4) = o;
+    } else {
+      typedef uint32_t vec __attribute__((ext_vector_type(2), aligned(2)));
+      *reinterpret_cast<vec*>(to + ((int64_t)hq * a.D + col) * 2) = vec{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+    }
+  }
+}
+
+// SV_FLAG_BAD_PAGE of every row that sees a key in no page: a wavefront for each new token.
+__global__ void __launch_bounds__(256) attention_flags_kernel(AttnArgs a, uint32_t* flags) {
+  const int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+  const int lane = threadIdx.x & (kWave - 1), i = (int)(at % a.rows.P), b = (int)(at / a.rows.P);
+  if (b >= a.rows.B) return;
+  const Sequence s = sequence_of(a, b);
+  if (i >= s.n) return;
+  int lo, hi;
+  keys_of(a, s, i, i, &lo, &hi);
+  bool bad = s.start + i >= s.cap;
+  if (hi > lo)
+    for (int k = divide(lo, a.pages.page) + lane; k <= divide(hi - 1, a.pages.page); k += kWave) {
+      const int p = a.pages.table[(int64_t)b * a.pages.max_pages + k];
+      bad |= p < 0 || p >= a.pages.n_pages;
+    }
+  if (__ballot(bad) == 0) bad = false; else bad = true;
+  if (lane == 0) flags[s.row0 + i] = bad ? SV_FLAG_BAD_PAGE : 0;
+}
+
+struct AttnPlan {
+  int nt, wr, tile_rows, tiles, splits;
+  int64_t items;
+  size_t bytes;
+};
+
+// How the rows of a call are laid out over workgroups.  Up to 16 rows a head and sequence: one block of them, the keys interleaved over
+// the four wavefronts; up to 32: two blocks; up to 64: two wavefronts with rows of their own; beyond, four.
+inline AttnPlan attention_plan(int B, int P, int Hq, int heads, int D, int dtype, bool whole, int64_t max_tokens) {
+  AttnPlan p{};
+  const int64_t rows = (int64_t)P * (Hq / heads);
+  const bool wide = dtype == SV_F32 || D > 128;             // (one block of rows a wavefront)
+  p.nt = wide ? 1 : 2;
+  if (rows <= 16) { p.nt = 1; p.wr = 1; }
+  else if (!whole) p.wr = 4;
+  else if (rows <= 16 * p.nt) p.wr = 1;
+  else if (rows <= 32 * p.nt) p.wr = 2;
+  else p.wr = 4;
+  if (!whole && p.wr == 1) p.nt = 1;
+  p.tile_rows = 16 * p.nt * p.wr;
+  const int64_t tiles = (rows + p.tile_rows - 1) / p.tile_rows;
+  p.items = (int64_t)B * heads * tiles;
+  p.tiles = (int)tiles;
+  const int64_t most = (max_tokens + kMinSteps * kStep - 1) / (kMinSteps * kStep);
+  int64_t splits = 4 * kTargetGroups / (p.items > 0 ? p.items : 1) + 1;
+  splits = splits < most ? splits : most;
+  // (what the parts take: each is written and read once, and 128 MB of them stay in the last-level cache)
+  const int64_t room = kCacheBytes / (p.items * p.tile_rows * D * 4 > 0 ? p.items * p.tile_rows * D * 4 : 1);
+  splits = splits < room ? splits : room;
+  p.splits = (int)(splits < 1 ? 1 : (splits < kMaxSplits ? splits : kMaxSplits));
+  p.bytes = 0;
+  if (p.splits > 1)
+    p.bytes = ws_round((size_t)p.items * 4) + ws_round((size_t)p.items * p.splits * p.tile_rows * 8) +
+              ws_round((size_t)p.items * p.splits * p.tile_rows * D * 4);
+  return p;
+}
+
+inline bool whole_tiles(int D, int page) { return (D == 64 || D == 128 || D == 256) && page % 16 == 0; }
+
+}  // namespace sv
+
+extern "C" size_t sv_chunk_attention_workspace_bytes(int B, int P, int Hq, int heads, int D, int dtype, int max_pages, int page) {
+  using namespace sv;
+  if (B < 1 || P < 1 || heads < 1 || Hq < heads || Hq % heads != 0 || Hq > SV_HEADS_MAX || D < 8 || D > SV_ATTENTION_HEAD_MAX || D % 8 != 0 ||
+      elem_bytes(dtype) == 0 || max_pages < 1 || page < 1 || page > SV_PAGE_MAX || (long long)B * P > kMaxRows / Hq)
+    return 0;
+  return attention_plan(B, P, Hq, heads, D, dtype, whole_tiles(D, page), (int64_t)max_pages * page).bytes;
+}
+
+extern "C" int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t* t_offsets_or_null, int n_rows,
+                                  const int32_t* lengths, const int32_t* first_or_null, const int32_t* pages, int max_pages,
+                                  int B, int P, int Hq, int heads, int D, int dtype, const void* k_cache,
+                                  const void* v_cache, int cache_dtype, const float* k_scale_or_null,
+                                  const float* v_scale_or_null, int n_pages, int page, float scale, int window, void* out,
+                                  int64_t out_stride, float* lse_or_null, uint32_t* flags_or_null, void* ws_or_null,
+                                  size_t ws_bytes, sv_stream_t stream) {
+  using namespace sv;
+  const int e = elem_bytes(dtype);
+  SV_REQUIRE(e != 0 && (cache_dtype == dtype || cache_dtype == SV_F8), SV_ERR_DTYPE);
+  const int status = check_rows(t_offsets_or_null, n_rows, B, P, max_pages, n_pages, heads, page, D);
+  SV_REQUIRE(status == SV_OK, status);
+  SV_REQUIRE(Hq >= heads && Hq % heads == 0 && D % 8 == 0 && window >= 0, SV_ERR_INVALID_ARG);
+  SV_REQUIRE(scale > -INFINITY && scale < INFINITY, SV_ERR_INVALID_ARG);
+  SV_REQUIRE(D <= SV_ATTENTION_HEAD_MAX && Hq <= SV_HEADS_MAX && (long long)B * P <= kMaxRows / Hq, SV_ERR_TOO_LARGE);
+  if (!t_offsets_or_null) n_rows = B * P;
+  if (B == 0 || n_rows == 0) return SV_OK;
+  SV_REQUIRE(q_stride >= (int64_t)Hq * D && out_stride >= (int64_t)Hq * D, SV_ERR_INVALID_ARG);
+  SV_REQUIRE(q_stride < (1ll << 40) && out_stride < (1ll << 40), SV_ERR_TOO_LARGE);
+  SV_REQUIRE(n_pages >= 1 && q != out, SV_ERR_INVALID_ARG);
+  SV_REQUIRE(q && out && lengths && pages && k_cache && v_cache, SV_ERR_NULL);
+  const bool f8 = cache_dtype == SV_F8;
+  SV_REQUIRE(!f8 || (k_scale_or_null && v_scale_or_null), SV_ERR_NULL);
+  SV_REQUIRE(is_aligned(q, e) && is_aligned(out, e) && is_aligned(lengths, 4) && is_aligned(pages, 4) && is_aligned(t_offsets_or_null, 4) &&
+                 is_aligned(first_or_null, 4) && is_aligned(lse_or_null, 4) && is_aligned(flags_or_null, 4) &&
+                 is_aligned(k_cache, f8 ? 1 : e) && is_aligned(v_cache, f8 ? 1 : e) &&
+                 (!f8 || (is_aligned(k_scale_or_null, 4) && is_aligned(v_scale_or_null, 4))),
+             SV_ERR_ALIGN);
+  const bool whole = whole_tiles(D, page);
+  AttnPlan p = attention_plan(B, P, Hq, heads, D, dtype, whole, (int64_t)max_pages * page);
+  if (!ws_or_null) p.splits = 1;
+  else if (p.splits > 1) SV_REQUIRE(is_aligned(ws_or_null, kWsAlign) && ws_bytes >= p.bytes, SV_ERR_WORKSPACE);
+  SV_REQUIRE(p.items * p.splits <= 0xffffffffLL / (kAttnWaves * kWave), SV_ERR_TOO_LARGE);
+  AttnArgs a{};
+  a.q = static_cast<const char*>(q);
+  a.out = static_cast<char*>(out);
+  a.lse = lse_or_null;
+  a.q_stride = q_stride * e;
+  a.out_stride = out_stride * e;
+  a.rows = Rows{t_offsets_or_null, lengths, n_rows, B, P};
+  a.pages = Pages{pages, max_pages, n_pages, heads, fast_div(page)};
+  a.first = first_or_null;
+  a.Hq = Hq;
+  a.group = Hq / heads;
+  a.D = D;
+  a.window = window;
+  a.by_group = fast_div(a.group);
+  a.scale2 = (float)((double)scale * kLog2e);
+  a.k_cache = static_cast<const char*>(k_cache);
+  a.v_cache = static_cast<const char*>(v_cache);
+  a.k_scale = k_scale_or_null;
+  a.v_scale = v_scale_or_null;
+  a.tiles = p.tiles;
+  a.splits = p.splits;
+  a.tile_rows = p.tile_rows;
+  if (p.splits > 1) {
+    char* w = static_cast<char*>(ws_or_null);
+    a.n_split = reinterpret_cast<int*>(w);
+    w += ws_round((size_t)p.items * 4);
+    a.part_ml = reinterpret_cast<float*>(w);
+    w += ws_round((size_t)p.items * p.splits * p.tile_rows * 8);
+    a.part_o = reinterpret_cast<float*>(w);
+  }
+  const AttnLaunch t{p.nt, p.wr, whole, (unsigned)(p.items * p.splits), as_stream(stream)};
+  if (dtype == SV_F32) {
+    if (f8) launch_attention_f32_f8(a, t); else launch_attention_f32(a, t);
+  } else {
+    if (f8) launch_attention_bf16_f8(a, t); else launch_attention_bf16(a, t);
+  }
+  if (p.splits > 1) {
+    const int64_t all = (int64_t)B * P * Hq;
+    if (dtype == SV_F32)
+      hipLaunchKernelGGL((attention_join_kernel<SV_F32>), dim3((unsigned)((all + 3) / 4)), dim3(256), 0, t.stream, a);
+    else
+      hipLaunchKernelGGL((attention_join_kernel<SV_BF16>), dim3((unsigned)((all + 3) / 4)), dim3(256), 0, t.stream, a);
+  }
+  if (flags_or_null)
+    hipLaunchKernelGGL(attention_flags_kernel, dim3((unsigned)(((int64_t)B * P + 3) / 4)), dim3(256), 0, t.stream, a, flags_or_null);
+  return launch_status();
+}

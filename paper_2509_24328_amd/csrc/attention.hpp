@@ -1,0 +1,751 @@
+// sv_chunk_attention: attention of the new tokens of every sequence over the pages of its cache.
+//
+// For a head of the cache, the rows are the new tokens times the query heads that share it (group G): row rho is token rho / G, head
+// h G + rho % G.  Both products run transposed on the matrix cores, so that nothing of a tile is rearranged between lanes:
+//   S^T[key][row] = K Q^T      operand A: sixteen keys, a lane holds sixteen bytes of one key's row
+//   O^T[col][row] = V^T P^T    operand A: sixteen groups of W columns, a lane holds W columns of eight keys
+// The result of the first product has, in lane (g, m), keys 4 g .. 4 g + 3 of row m, which is operand B of the second one if its sum
+// over 32 keys takes them in the order (tile, key 4 g + r): the order of a sum is free as long as both operands follow it.
+// Likewise the columns of the first product: a lane's sixteen bytes are at 64 s + 16 g of the row, for keys and queries alike.
+// So keys and values go from the cache's pages into registers and from there into the matrix cores, without LDS.
+// The softmax is one pass: a running maximum (in units of log2, raised only when it is exceeded by more than 8: a weight is at most 2^8
+// then) and, in every lane, the sum of the weights of its keys.  Scores, weights, sums and outputs are float32; weights are rounded to
+// bfloat16 for the second product where the queries are bfloat16 (half a step, 2^-9 of a weight, at random).
+//
+// A workgroup has WR x WK wavefronts: WR blocks of 16 NT rows, WK interleaved parts of the keys, joined in LDS at the end.  Where there
+// are few rows, the keys of a row block are divided among up to `splits` workgroups, whose results a second kernel joins; each has
+// at least kMinSteps x 32 keys, and about as many as the average of kTargetGroups of them, from the lengths that the device knows.
+#pragma once
+
+#include "paged.hpp"
+
+namespace sv {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kStep = 32;              // keys of a step
+constexpr int kMinSteps = 8;           // steps of a workgroup that divides a row block's keys with others, at least
+constexpr int kTargetGroups = 1024;    // workgroups that the keys of a call are divided among
+constexpr int kMaxSplits = 64;
+constexpr int kAttnWaves = 4;
+constexpr long long kMaxRows = 1 << 28;   // B * P * Hq: positions and rows stay within 32 bits
+
+struct AttnArgs {
+  const char* q;
+  char* out;
+  float* lse;                          // [n_rows, Hq], or null
+  int64_t q_stride, out_stride;        // bytes from row to row
+  Rows rows;
+  Pages pages;
+  const int32_t* first;                // [B], or null
+  int Hq, group, D, window;
+  FastDiv by_group;
+  float scale2;                        // scale * log2 e
+  const char *k_cache, *v_cache;
+  const float *k_scale, *v_scale;
+  int tiles, splits, tile_rows;        // row blocks of a head of a sequence; most workgroups to one; rows of one
+  int* n_split;                        // [items]            scratch, null without it
+  float* part_ml;                      // [items, splits, tile_rows, 2]
+  float* part_o;                       // [items, splits, tile_rows, D]
+};
+
+// A sequence as all calls see it.
+struct Sequence {
+  int row0, n, start, first;           // its first row, new tokens, tokens before them, first token that may be seen
+  int cap;                             // positions from here on are in no page
+};
+
+__device__ __forceinline__ Sequence sequence_of(const AttnArgs& a, int b) {
+  Sequence s;
+  if (a.rows.offsets) {
+    s.row0 = a.rows.offsets[b];
+    s.n = min(a.rows.offsets[b + 1] - s.row0, a.rows.P);
+    if (s.row0 < 0 || s.row0 > a.rows.n_rows - s.n) s.n = 0;        // (rows outside the tensor are not touched)
+  } else {
+    s.row0 = b * a.rows.P;
+    s.n = a.rows.P;
+  }
+  s.start = a.rows.start[b];
+  s.first = a.first ? max(a.first[b], 0) : 0;
+  const int64_t cap = (int64_t)a.pages.max_pages * (int)a.pages.page.d;
+  s.cap = (int)(cap < 0x40000000 ? cap : 0x40000000);
+  if (s.start < 0 || s.start > s.cap) s.start = s.cap;              // every row is behind the last page
+  return s;
+}
+
+// Keys [lo, hi) that the rows of tokens i0 .. i1 see between them.
+__device__ __forceinline__ void keys_of(const AttnArgs& a, const Sequence& s, int i0, int i1, int* lo, int* hi) {
+  *lo = s.first;
+  if (a.window > 0) *lo = max(*lo, s.start + i0 - a.window + 1);
+  *hi = min(s.start + i1 + 1, s.cap);
+}
+
+// Steps of a workgroup that divides keys with others, from the lengths of all sequences (all lanes of the wavefront active).
+__device__ __forceinline__ int steps_per_group(const AttnArgs& a) {
+  int64_t sum = 0;
+  const int lane = threadIdx.x & (kWave - 1);
+  for (int k = lane; k < a.rows.B; k += kWave) {
+    const Sequence s = sequence_of(a, k);
+    if (s.n <= 0) continue;
+    int lo, hi;
+    keys_of(a, s, 0, s.n - 1, &lo, &hi);
+    const int rows = (s.n * a.group + a.tile_rows - 1) / a.tile_rows;
+    if (hi > lo) sum += (int64_t)((hi - lo + kStep - 1) / kStep) * rows;
+  }
+  const double total = wave_sum_f64((double)sum) * a.pages.heads;
+  const double steps = total * (1.0 / kTargetGroups);
+  return max(kMinSteps, (int)fmin(steps + 1.0, 1e9));
+}
+
+template <int ET, int CT, int DPAD>
+struct Shape {
+  static constexpr bool f8 = CT == SV_F8;
+  static constexpr bool f32 = ET == SV_F32;
+  static constexpr int cb = f8 ? 1 : (f32 ? 4 : 2);     // bytes of a column in the cache
+  static constexpr int eb = f32 ? 4 : 2;
+  static constexpr int NK = DPAD * cb / 64;             // sixteen-byte loads of a key
+  static constexpr int EK = 16 / cb;                    // columns of one
+  static constexpr int W = f32 || DPAD == 64 ? 4 : 8;   // columns of a value that a lane holds in one block
+  static constexpr int NB = DPAD / (16 * W);            // blocks of 16 W columns
+  static constexpr int WV = (W * cb + 3) / 4;           // words of one
+};
+
+template <int N>
+struct Words {
+  uint32_t w[N];
+};
+
+template <int N>
+__device__ __forceinline__ void load_words(const char* p, uint32_t (&w)[N]) {
+  typedef uint32_t vec __attribute__((ext_vector_type(N == 1 ? 2 : N), aligned(1)));
+  if constexpr (N == 1) {
+    typedef uint32_t one __attribute__((aligned(1)));
+    w[0] = *reinterpret_cast<const one*>(p);
+  } else {
+    const vec v = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = v[i];
+  }
+}
+
+__device__ __forceinline__ uint32_t f8_pair_bf16(uint32_t w, bool high) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 v = high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)
+                        : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+__device__ __forceinline__ bf16x8 as_bf16x8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_bit_cast(bf16x8, u32x4{a, b, c, d});
+}
+
+// max / sum over the four lanes that hold the same row (lanes m, m + 16, m + 32, m + 48)
+__device__ __forceinline__ float across_max(float v) {
+  Halves h = swap32(__float_as_uint(v), __float_as_uint(v));
+  v = fmaxf(__uint_as_float(h.a), __uint_as_float(h.b));
+  h = swap16(__float_as_uint(v), __float_as_uint(v));
+  return fmaxf(__uint_as_float(h.a), __uint_as_float(h.b));
+}
+__device__ __forceinline__ float across_sum(float v) {
+  Halves h = swap32(__float_as_uint(v), __float_as_uint(v));
+  v = __uint_as_float(h.a) + __uint_as_float(h.b);
+  h = swap16(__float_as_uint(v), __float_as_uint(v));
+  return __uint_as_float(h.a) + __uint_as_float(h.b);
+}
+
+// The part of a row block's keys that a wavefront goes through, and its rows.
+template <int ET, int CT, int DPAD, int NT, bool WHOLE>
+struct Wavefront {
+  using Sh = Shape<ET, CT, DPAD>;
+  static constexpr int NO = DPAD / 16;                  // output tiles of a block of sixteen rows
+
+  const AttnArgs& a;
+  const int g, m;                                       // lane = 16 g + m
+  const int32_t* table;                                 // the sequence's pages
+  int64_t head_off;                                     // rows of D from a page's first to this head's first
+  int pos[NT], low[NT];                                 // the row's position, and the first key that it sees
+  uint32_t qw[NT][Sh::NK * Sh::EK * Sh::eb / 4];        // queries, by the columns of the keys' loads
+  f32x4 o[NT][NO];
+  float mx[NT], l[NT];
+
+  __device__ __forceinline__ Wavefront(const AttnArgs& args) : a(args), g((threadIdx.x & 63) >> 4), m(threadIdx.x & 15) {}
+
+  // (-1: in no page)
+  __device__ __forceinline__ int64_t page_row(int key) const {
+    const int k = divide(key, a.pages.page);
+    const int at = k < a.pages.max_pages ? table[k] : -1;
+    if (at < 0 || at >= a.pages.n_pages) return -1;
+    return (int64_t)at * a.pages.heads * (int)a.pages.page.d + head_off + (key - k * (int)a.pages.page.d);
+  }
+
+  __device__ __forceinline__ void start(const Sequence& s, int rho0, int h) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int rho = rho0 + 16 * n + m, i = divide(rho, a.by_group), hq = h * a.group + rho - i * a.group;
+      const bool there = i < s.n;
+      // rows that are not there see everything: they never make a step a partial one, and are not written
+      pos[n] = there ? s.start + i : 0x7fffffff;
+      low[n] = there ? s.first : 0;
+      if (there && a.window > 0) low[n] = max(low[n], pos[n] - a.window + 1);
+      const char* row = a.q + (int64_t)(s.row0 + (there ? i : 0)) * a.q_stride + (int64_t)hq * a.D * Sh::eb;
+#pragma unroll
+      for (int k = 0; k < Sh::NK; ++k) {
+        constexpr int words = Sh::EK * Sh::eb / 4, per = Sh::eb == 4 ? 4 : 8;    // (columns in whole vectors of `per`)
+        const int col = (64 * k + 16 * g) / Sh::cb;
+#pragma unroll
+        for (int e = 0; e < Sh::EK; e += per) {
+          uint32_t w[4] = {};
+          if (there && (WHOLE || col + e < a.D)) load_words<4>(row + (int64_t)(col + e) * Sh::eb, w);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) qw[n][k * words + e * Sh::eb / 4 + j] = w[j];
+        }
+      }
+      mx[n] = -INFINITY;
+      l[n] = 0.f;
+#pragma unroll
+      for (int t = 0; t < NO; ++t) o[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // Keys and values of a step.  Addresses are those of keys within [lo, hi): a key outside it stands for one inside, and its weight is 0.
+  struct Keys {
+    Words<4> k[2][Sh::NK];
+    float scale[2][4];
+  };
+  struct Values {
+    Words<Sh::WV> v[8][Sh::NB];
+    float scale[8];
+  };
+  // The pages of the two tiles of a step, where a tile lies in one page: rows of the cache of their first keys.
+  struct Where {
+    int64_t row[2];
+  };
+
+  __device__ __forceinline__ void find(int key0, int lo, int hi, Where& w) const {
+    if constexpr (WHOLE) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        // (the tile's first key, or if the tile is outside, that of a tile that is not)
+        const int first = min(max(key0 + 16 * t, lo & ~15), (hi - 1) & ~15);
+        const int64_t row = page_row(__builtin_amdgcn_readfirstlane(first));
+        const uint32_t r0 = __builtin_amdgcn_readfirstlane((uint32_t)row), r1 = __builtin_amdgcn_readfirstlane((uint32_t)(row >> 32));
+        w.row[t] = (int64_t)(((uint64_t)r1 << 32) | r0);
+      }
+    }
+  }
+
+  // Row of the cache of key key0 + 16 t + k.
+  __device__ __forceinline__ int64_t row_of(int key0, int t, int k, int lo, int hi, const Where& w) const {
+    if constexpr (WHOLE) return w.row[t] < 0 ? 0 : w.row[t] + k;
+    const int64_t r = page_row(min(max(key0 + 16 * t + k, lo), hi - 1));
+    return r < 0 ? 0 : r;
+  }
+
+  __device__ __forceinline__ void load_keys(int key0, int lo, int hi, const Where& w, Keys& kk) const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const char* row = a.k_cache + row_of(key0, t, m, lo, hi, w) * (int64_t)(a.D * Sh::cb);
+#pragma unroll
+      for (int k = 0; k < Sh::NK; ++k) {
+        const int at = 64 * k + 16 * g, bytes = a.D * Sh::cb;
+        if constexpr (WHOLE) {
+          load_words<4>(row + at, kk.k[t][k].w);
+        } else {
+          kk.k[t][k] = Words<4>{{0u, 0u, 0u, 0u}};
+          if (at + 16 <= bytes) load_words<4>(row + at, kk.k[t][k].w);
+          else if (at + 8 <= bytes) {
+            uint32_t w2[2];
+            load_words<2>(row + at, w2);
+            kk.k[t][k].w[0] = w2[0];
+            kk.k[t][k].w[1] = w2[1];
+          }
+        }
+      }
+      if constexpr (Sh::f8) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) kk.scale[t][r] = a.k_scale[row_of(key0, t, 4 * g + r, lo, hi, w)];
+      }
+    }
+  }
+
+  __device__ __forceinline__ void load_values(int key0, int lo, int hi, const Where& w, Values& vv) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t at = row_of(key0, i / 4, 4 * g + i % 4, lo, hi, w);
+      const char* row = a.v_cache + at * (int64_t)(a.D * Sh::cb);
+#pragma unroll
+      for (int n = 0; n < Sh::NB; ++n) {
+        const int col = (16 * n + m) * Sh::W;
+        if (WHOLE || col < a.D) load_words<Sh::WV>(row + col * Sh::cb, vv.v[i][n].w);
+        else {
+#pragma unroll
+          for (int j = 0; j < Sh::WV; ++j) vv.v[i][n].w[j] = 0u;
+        }
+      }
+      if constexpr (Sh::f8) vv.scale[i] = a.v_scale[at];
+    }
+  }
+
+  __device__ __forceinline__ void scores(const Keys& kk, f32x4 (&s)[NT][2]) const {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int k = 0; k < Sh::NK; ++k) {
+        const uint32_t(&w)[4] = kk.k[t][k].w;
+        if constexpr (!Sh::f32 && !Sh::f8) {
+          const bf16x8 ka = as_bf16x8(w[0], w[1], w[2], w[3]);
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                ka, as_bf16x8(qw[n][4 * k], qw[n][4 * k + 1], qw[n][4 * k + 2], qw[n][4 * k + 3]), s[n][t], 0, 0, 0);
+        } else if constexpr (!Sh::f32) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const bf16x8 ka = as_bf16x8(f8_pair_bf16(w[2 * u], false), f8_pair_bf16(w[2 * u], true),
+                                        f8_pair_bf16(w[2 * u + 1], false), f8_pair_bf16(w[2 * u + 1], true));
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  ka, as_bf16x8(qw[n][8 * k + 4 * u], qw[n][8 * k + 4 * u + 1], qw[n][8 * k + 4 * u + 2], qw[n][8 * k + 4 * u + 3]),
+                  s[n][t], 0, 0, 0);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < Sh::EK; ++e) {
+            float ka;
+            if constexpr (Sh::f8) {
+              const auto p = (e & 2) ? __builtin_amdgcn_cvt_pk_f32_fp8(w[e / 4], true) : __builtin_amdgcn_cvt_pk_f32_fp8(w[e / 4], false);
+              ka = p[e & 1];
+            } else {
+              ka = __uint_as_float(w[e]);
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              s[n][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka, __uint_as_float(qw[n][Sh::EK * k + e]), s[n][t], 0, 0, 0);
+          }
+        }
+      }
+    }
+  }
+
+  // Scores to weights, in place (p: what multiplies the values), with the running maximum and sum.  PART: some key of the step is not
+  // seen by some row; bad: tiles without a page.
+  template <bool PART>
+  __device__ __forceinline__ void weigh(int key0, const Keys& kk, const Values& vv, const bool (&bad)[2], f32x4 (&s)[NT][2]) {
+    bool raise = false;
+    float top[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float t8 = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float x = s[n][t][r] * a.scale2;
+          if constexpr (Sh::f8) x *= kk.scale[t][r];
+          if (PART) {
+            const int key = key0 + 16 * t + 4 * g + r;
+            bool none = bad[t];
+            if constexpr (!WHOLE) none = page_row(min(key, 0x3fffffff)) < 0;
+            x = none ? NAN : x;
+            x = key >= low[n] && key <= pos[n] ? x : -INFINITY;
+          }
+          s[n][t][r] = x;
+          t8 = fmaxf(t8, x);
+        }
+      }
+      top[n] = across_max(t8);
+      raise |= top[n] > mx[n] + 8.f;
+    }
+    if (__ballot(raise)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const bool up = top[n] > mx[n] + 8.f;
+        const float f = up ? exp2_fast(mx[n] - top[n]) : 1.f;      // (from -inf: 0)
+        mx[n] = up ? top[n] : mx[n];
+        l[n] *= f;
+#pragma unroll
+        for (int t = 0; t < NO; ++t) o[n][t] *= f;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const float base = mx[n] == -INFINITY ? 0.f : mx[n];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float p = exp2_fast(s[n][t][r] - base);
+          l[n] += p;
+          if constexpr (Sh::f8) {
+            p *= vv.scale[4 * t + r];
+            if (PART) {
+              const int key = key0 + 16 * t + 4 * g + r;
+              p = key >= low[n] && key <= pos[n] ? p : 0.f;        // (whatever the scale of an unseen key is)
+            }
+          }
+          s[n][t][r] = p;
+        }
+      }
+    }
+  }
+
+  // Operand A of output tile (block n, column c of W): the eight keys of a lane.
+  __device__ __forceinline__ void value_words(const Values& vv, int nb, uint32_t (&w)[Sh::W][4]) const {
+    static_assert(!Sh::f32, "pairs of bfloat16");
+    uint32_t x[8][Sh::W / 2];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int j = 0; j < Sh::W / 2; ++j) {
+        if constexpr (Sh::f8) x[i][j] = f8_pair_bf16(vv.v[i][nb].w[j / 2], j & 1);
+        else x[i][j] = vv.v[i][nb].w[j];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < Sh::W / 2; ++j) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        w[2 * j][k] = __builtin_amdgcn_perm(x[2 * k + 1][j], x[2 * k][j], 0x05040100u);
+        w[2 * j + 1][k] = __builtin_amdgcn_perm(x[2 * k + 1][j], x[2 * k][j], 0x07060302u);
+      }
+    }
+  }
+  __device__ __forceinline__ float value_f32(const Values& vv, int i, int nb, int c) const {
+    if constexpr (Sh::f8) {
+      const auto p = (c & 2) ? __builtin_amdgcn_cvt_pk_f32_fp8(vv.v[i][nb].w[c / 4], true)
+                             : __builtin_amdgcn_cvt_pk_f32_fp8(vv.v[i][nb].w[c / 4], false);
+      return p[c & 1];
+    } else {
+      return __uint_as_float(vv.v[i][nb].w[c]);
+    }
+  }
+
+  __device__ __forceinline__ bf16x8 weights(const f32x4 (&s)[2]) const {
+    return as_bf16x8(pack_bf16(s[0][0], s[0][1]), pack_bf16(s[0][2], s[0][3]), pack_bf16(s[1][0], s[1][1]), pack_bf16(s[1][2], s[1][3]));
+  }
+
+  __device__ __forceinline__ void add_values(const Values& vv, const f32x4 (&s)[NT][2]) {
+    if constexpr (!Sh::f32) {
+      bf16x8 p[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) p[n] = weights(s[n]);
+#pragma unroll
+      for (int nb = 0; nb < Sh::NB; ++nb) {
+        uint32_t w[Sh::W][4];
+        value_words(vv, nb, w);
+#pragma unroll
+        for (int c = 0; c < Sh::W; ++c) {
+          const bf16x8 va = as_bf16x8(w[c][0], w[c][1], w[c][2], w[c][3]);
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            o[n][nb * Sh::W + c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, p[n], o[n][nb * Sh::W + c], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (int nb = 0; nb < Sh::NB; ++nb) {
+#pragma unroll
+          for (int c = 0; c < Sh::W; ++c) {
+            const float va = value_f32(vv, i, nb, c);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              o[n][nb * Sh::W + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(va, s[n][i / 4][i % 4], o[n][nb * Sh::W + c], 0, 0, 0);
+          }
+        }
+      }
+    }
+  }
+
+  // Values of a step some of whose keys are not seen by some row: 0 where no row of the block sees the key; returns whether one that a
+  // row does see is not finite.
+  __device__ __forceinline__ bool clean_values(int key0, int lo, int hi, Values& vv) const {
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int key = key0 + 16 * (i / 4) + 4 * g + i % 4;
+      const bool in = key >= lo && key < hi;
+#pragma unroll
+      for (int nb = 0; nb < Sh::NB; ++nb) {
+#pragma unroll
+        for (int j = 0; j < Sh::WV; ++j) {
+          uint32_t& w = vv.v[i][nb].w[j];
+          w = in ? w : 0u;
+          if constexpr (Sh::f8) {
+            // a byte 0x7f or 0xff is a NaN: adding 1 to the seven bits carries into the eighth
+            odd |= (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+          } else if constexpr (Sh::f32) {
+            odd |= (w & 0x7f800000u) == 0x7f800000u;
+          } else {
+            odd |= (w & 0x7f800000u) == 0x7f800000u || (w & 0x00007f80u) == 0x00007f80u;
+          }
+        }
+      }
+    }
+    return __ballot(odd) != 0;
+  }
+
+  // add_values where a value that some row must not see is not finite: key by key, each added to the rows that see it alone.
+  __device__ __forceinline__ void add_values_apart(int key0, const Values& vv, const f32x4 (&s)[NT][2]) {
+#pragma unroll 1
+    for (int j = 0; j < 32; ++j) {
+      const int i = j & 7, owner = j >> 3;                  // slot i of the lanes 16 owner .. 16 owner + 15
+      const int key = key0 + 16 * (i / 4) + 4 * owner + i % 4;
+#pragma unroll
+      for (int nb = 0; nb < Sh::NB; ++nb) {
+        if constexpr (!Sh::f32) {
+          uint32_t w[Sh::W][4];
+          value_words(vv, nb, w);
+#pragma unroll
+          for (int c = 0; c < Sh::W; ++c) {
+            uint32_t x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = g == owner && k == i / 2 ? w[c][k] & ((i & 1) ? 0xffff0000u : 0x0000ffffu) : 0u;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x[0], x[1], x[2], x[3]), weights(s[n]),
+                                                                    o[n][nb * Sh::W + c], 0, 0, 0);
+              if (key >= low[n] && key <= pos[n]) o[n][nb * Sh::W + c] = y;
+            }
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < Sh::W; ++c) {
+            float x = 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x = k == i && g == owner ? value_f32(vv, k, nb, c) : x;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              float p = 0.f;
+#pragma unroll
+              for (int k = 0; k < 8; ++k) p = k == i ? s[n][k / 4][k % 4] : p;
+              const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p, o[n][nb * Sh::W + c], 0, 0, 0);
+              if (key >= low[n] && key <= pos[n]) o[n][nb * Sh::W + c] = y;
+            }
+          }
+        }
+      }
+    }
+  }
+
+  // Steps s0, s0 + stride, ... below s1 of the keys [lo, hi); step s begins at key 32 s.
+  __device__ __forceinline__ void sweep(int s0, int s1, int stride, int lo, int hi) {
+    if (s0 >= s1) return;
+    // keys that every row of the wavefront sees
+    int all_lo = 0, all_hi = 0x7fffffff;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      all_lo = max(all_lo, low[n]);
+      all_hi = min(all_hi, pos[n]);
+    }
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) {
+      all_lo = max(all_lo, __shfl_xor(all_lo, d, kWave));
+      all_hi = min(all_hi, __shfl_xor(all_hi, d, kWave));
+    }
+    all_lo = __builtin_amdgcn_readfirstlane(max(all_lo, lo));
+    all_hi = __builtin_amdgcn_readfirstlane(min(all_hi, hi - 1));
+    Where at, next;
+    Keys kk;
+    find(kStep * s0, lo, hi, at);
+    load_keys(kStep * s0, lo, hi, at, kk);
+    for (int s = s0; s < s1; s += stride) {
+      const int key0 = kStep * s;
+      Values vv;
+      load_values(key0, lo, hi, at, vv);
+      f32x4 sc[NT][2];
+      scores(kk, sc);
+      Keys kept = kk;
+      const int after = min(s + stride, s1 - 1);
+      find(kStep * after, lo, hi, next);
+      if (s + stride < s1) load_keys(kStep * after, lo, hi, next, kk);
+      bool bad[2] = {false, false};
+      if constexpr (WHOLE) {
+        bad[0] = at.row[0] < 0;
+        bad[1] = at.row[1] < 0;
+      }
+      const bool part = !WHOLE || key0 < all_lo || key0 + kStep - 1 > all_hi || bad[0] || bad[1];
+      if (!part) {
+        weigh<false>(key0, kept, vv, bad, sc);
+        add_values(vv, sc);
+      } else {
+        weigh<true>(key0, kept, vv, bad, sc);
+        if (clean_values(key0, lo, hi, vv)) add_values_apart(key0, vv, sc);
+        else add_values(vv, sc);
+      }
+      at = next;
+    }
+  }
+};
+
+// One workgroup: a row block of a head of a sequence, a part of its keys.
+template <int ET, int CT, int DPAD, int NT, int WR, int WK, bool WHOLE>
+__global__ void __launch_bounds__(kAttnWaves* kWave, 1) attention_kernel(AttnArgs a) {
+  static_assert(WR * WK == kAttnWaves, "four wavefronts");
+  using Wf = Wavefront<ET, CT, DPAD, NT, WHOLE>;
+  using Sh = Shape<ET, CT, DPAD>;
+  constexpr int kRows = 16 * NT;
+  // joined in LDS: the outputs of the wavefronts with another part of the keys, column by column
+  __shared__ float sh_o[WK > 1 ? WR * (WK / 2) : 1][WK > 1 ? NT * Wf::NO * 4 : 1][WK > 1 ? kWave : 1];
+  __shared__ float sh_ml[WK > 1 ? WR * (WK / 2) : 1][2][WK > 1 ? NT : 1][WK > 1 ? kWave : 1];
+  const int split = blockIdx.x % a.splits, item = blockIdx.x / a.splits;
+  const int tile = item % a.tiles, bh = item / a.tiles, h = bh % a.pages.heads, b = bh / a.pages.heads;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wr = wave % WR, wk = wave / WR;
+  const Sequence s = sequence_of(a, b);
+  const int rho0 = tile * a.tile_rows, rows = s.n * a.group - rho0;
+  if (rows <= 0) return;
+  const int i0 = divide(rho0, a.by_group), i1 = divide(min(rho0 + a.tile_rows, s.n * a.group) - 1, a.by_group);
+  int lo, hi;
+  keys_of(a, s, i0, i1, &lo, &hi);
+  const int step_lo = lo / kStep, steps = hi > lo ? (hi + kStep - 1) / kStep - step_lo : 0;
+  int mine0 = 0, mine1 = steps, parts = 1;
+  if (a.splits > 1) {
+    const int unit = steps_per_group(a);
+    parts = max(1, min((steps + unit - 1) / unit, a.splits));
+    if (split >= parts) return;
+    const int each = (steps + parts - 1) / parts;
+    mine0 = min(split * each, steps);
+    mine1 = min(mine0 + each, steps);
+    if (split == 0 && threadIdx.x == 0) a.n_split[item] = parts;
+  }
+  Wf w(a);
+  w.table = a.pages.table + (int64_t)b * a.pages.max_pages;
+  w.head_off = (int64_t)h * (int)a.pages.page.d;
+  w.start(s, rho0 + wr * kRows, h);
+  w.sweep(step_lo + mine0 + wk, step_lo + mine1, WK, lo, hi);
+  float l[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) l[n] = across_sum(w.l[n]);
+  const int lane = threadIdx.x & (kWave - 1);
+  if constexpr (WK > 1) {
+    // halves: the upper wavefronts hand over, the lower ones add
+#pragma unroll
+    for (int half = WK / 2; half >= 1; half /= 2) {
+      if (wk >= half && wk < 2 * half) {
+        const int slot = (wk - half) * WR + wr;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          sh_ml[slot][0][n][lane] = w.mx[n];
+          sh_ml[slot][1][n][lane] = l[n];
+#pragma unroll
+          for (int t = 0; t < Wf::NO; ++t) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sh_o[slot][(n * Wf::NO + t) * 4 + r][lane] = w.o[n][t][r];
+          }
+        }
+      }
+      __syncthreads();
+      if (wk < half) {
+        const int slot = wk * WR + wr;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const float m2 = sh_ml[slot][0][n][lane], top = fmaxf(w.mx[n], m2);
+          const float f1 = w.mx[n] == top ? 1.f : exp2_fast(w.mx[n] - top), f2 = m2 == top ? 1.f : exp2_fast(m2 - top);
+          w.mx[n] = top;
+          l[n] = l[n] * f1 + sh_ml[slot][1][n][lane] * f2;
+#pragma unroll
+          for (int t = 0; t < Wf::NO; ++t) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) w.o[n][t][r] = w.o[n][t][r] * f1 + sh_o[slot][(n * Wf::NO + t) * 4 + r][lane] * f2;
+          }
+        }
+      }
+      __syncthreads();
+    }
+    if (wk > 0) return;
+  }
+  // lane (g, m): row m of the block, columns ((16 nb) + 4 g + r) W + c of output tile nb W + c
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int rho = rho0 + wr * kRows + 16 * n + w.m, i = divide(rho, a.by_group), hq = h * a.group + rho - i * a.group;
+    if (i >= s.n) continue;
+    const bool out_of_pages = w.pos[n] >= s.cap;
+    const bool any = w.mx[n] != -INFINITY || !(l[n] == 0.f);
+    if (parts == 1) {
+      const float inv = out_of_pages ? NAN : (any ? 1.f / l[n] : 0.f);
+      if (a.lse && w.g == 0)
+        a.lse[(int64_t)(s.row0 + i) * a.Hq + hq] = out_of_pages ? NAN : (any ? (float)((w.mx[n] + log2((double)l[n])) * kLn2) : -INFINITY);
+      char* to = a.out + (int64_t)(s.row0 + i) * a.out_stride + (int64_t)hq * a.D * Sh::eb;
+#pragma unroll
+      for (int nb = 0; nb < Sh::NB; ++nb) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int col = (16 * nb + 4 * w.g + r) * Sh::W;
+          if (!WHOLE && col >= a.D) continue;
+          if constexpr (Sh::f32) {
+            typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
+            *reinterpret_cast<vec*>(to + col * 4) = vec{w.o[n][nb * 4][r] * inv, w.o[n][nb * 4 + 1][r] * inv,
+                                                        w.o[n][nb * 4 + 2][r] * inv, w.o[n][nb * 4 + 3][r] * inv};
+          } else {
+            typedef uint32_t vec __attribute__((ext_vector_type(Sh::W / 2), aligned(2)));
+            vec v;
+#pragma unroll
+            for (int c = 0; c < Sh::W / 2; ++c)
+              v[c] = pack_bf16(w.o[n][nb * Sh::W + 2 * c][r] * inv, w.o[n][nb * Sh::W + 2 * c + 1][r] * inv);
+            *reinterpret_cast<vec*>(to + col * 2) = v;
+          }
+        }
+      }
+    } else {
+      const int64_t at = ((int64_t)item * a.splits + split) * a.tile_rows + (rho - rho0);
+      if (w.g == 0) {
+        a.part_ml[2 * at] = w.mx[n];
+        a.part_ml[2 * at + 1] = l[n];
+      }
+#pragma unroll
+      for (int nb = 0; nb < Sh::NB; ++nb) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int col = (16 * nb + 4 * w.g + r) * Sh::W;
+          if (!WHOLE && col >= a.D) continue;
+#pragma unroll
+          for (int c = 0; c < Sh::W; c += 4) {
+            typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
+            *reinterpret_cast<vec*>(a.part_o + at * a.D + col + c) =
+                vec{w.o[n][nb * Sh::W + c][r], w.o[n][nb * Sh::W + c + 1][r], w.o[n][nb * Sh::W + c + 2][r], w.o[n][nb * Sh::W + c + 3][r]};
+          }
+        }
+      }
+    }
+  }
+}
+
+// Launches the kernel of a shape; what the rows decide is chosen in sv_chunk_attention.
+struct AttnLaunch {
+  int nt, wr;          // row blocks of a wavefront, row wavefronts of a workgroup
+  bool whole;          // D is 64, 128 or 256 and no page ends inside a tile of sixteen keys
+  unsigned grid;
+  hipStream_t stream;
+};
+void launch_attention_f32(const AttnArgs&, const AttnLaunch&);
+void launch_attention_f32_f8(const AttnArgs&, const AttnLaunch&);
+void launch_attention_bf16(const AttnArgs&, const AttnLaunch&);
+void launch_attention_bf16_f8(const AttnArgs&, const AttnLaunch&);
+
+template <int ET, int CT, int DPAD>
+void launch_attention_of(const AttnArgs& a, const AttnLaunch& t) {
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(t.grid), dim3(kAttnWaves * kWave), 0, t.stream, a); };
+  constexpr int NT = ET == SV_F32 || DPAD == 256 ? 1 : 2;
+  if (t.whole) {
+    if (t.wr == 4) go(attention_kernel<ET, CT, DPAD, NT, 4, 1, true>);
+    else if (t.wr == 2) go(attention_kernel<ET, CT, DPAD, NT, 2, 2, true>);
+    else if (t.nt == 2 && NT == 2) go(attention_kernel<ET, CT, DPAD, NT, 1, 4, true>);
+    else go(attention_kernel<ET, CT, DPAD, 1, 1, 4, true>);
+  } else {
+    if (t.wr == 4) go(attention_kernel<ET, CT, DPAD, NT, 4, 1, false>);
+    else go(attention_kernel<ET, CT, DPAD, 1, 1, 4, false>);
+  }
+}
+template <int ET, int CT>
+void launch_attention(const AttnArgs& a, const AttnLaunch& t) {
+  if (a.D <= 64) launch_attention_of<ET, CT, 64>(a, t);
+  else if (a.D <= 128) launch_attention_of<ET, CT, 128>(a, t);
+  else launch_attention_of<ET, CT, 256>(a, t);
+}
+
+}  // namespace sv
