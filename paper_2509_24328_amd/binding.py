@@ -683,39 +683,58 @@ def sv_clip_grad_norm(grads, max_norm, norm, out=None, flag=None, ws=None, strea
 # ---------------------------------------------------------------------------
 # the model side of a step
 # ---------------------------------------------------------------------------
-def _device_of(t, *others):
-    """Refuses tensors of another device than the first one's, and a first one of another than the current device, whose
-    streams the calls run on."""
-    here = t.device
-    if here.type != "cuda" or (here.index is not None and here.index != torch.cuda.current_device()):
-        raise ValueError(f"sv: tensors must lie on the current device (got {here})")
-    for o in others:
-        if o is not None and o.device != here:
-            raise ValueError(f"sv: tensors of several devices ({here}, {o.device})")
+def _here(*tensors):
+    """Refuses tensors that do not lie on the current device, whose stream the calls run on.  (Numbers of devices, from torch's C layer:
+    torch.device objects take longer to make than a small call runs.)"""
+    try:
+        device = torch._C._cuda_getDevice()
+    except (AttributeError, RuntimeError):
+        device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"sv: tensors must lie on the current device (cuda:{device}, got {t.device})")
+
+
+def _dense(t):
+    """Address of a contiguous tensor whose device has been looked at (None -> NULL)."""
+    if t is None:
+        return None
+    if not t.is_contiguous():
+        raise ValueError(f"sv: tensors must be contiguous device tensors (got device={t.device}, contiguous=False)")
+    return t.data_ptr()
 
 
 def _heads(t):
     """(address, elements from row to row) of [..., H, D] whose heads follow each other and whose rows lie at one distance, as
     columns of a wider projection do."""
-    if not t.is_cuda or t.dim() < 3 or t.dtype not in _TAGS:
-        raise ValueError("sv: rows of heads must be device tensors [..., heads, D] in float32 or bfloat16 "
-                         f"(got device={t.device}, shape={tuple(t.shape)}, dtype={t.dtype})")
-    H, D = t.shape[-2:]
+    shape, strides = t.shape, t.stride()
+    if len(shape) == 3 and strides[2] == 1 and strides[1] == shape[2] and strides[0] >= shape[1] * shape[2]:
+        return t.data_ptr(), strides[0]
+    if len(shape) < 3:
+        raise ValueError(f"sv: rows of heads must be [..., heads, D] (got shape={tuple(shape)})")
+    H, D = shape[-2:]
     if t.is_contiguous():
         return t.data_ptr(), H * D
-    ok = (t.stride(-1) == 1 or D == 1) and (t.stride(-2) == D or H == 1)
+    ok = (strides[-1] == 1 or D == 1) and (strides[-2] == D or H == 1)
     stride, rows = H * D, 1
-    for d in range(t.dim() - 3, -1, -1):
-        if t.shape[d] == 1:
+    for d in range(len(shape) - 3, -1, -1):
+        if shape[d] == 1:
             continue
         if rows == 1:
-            stride = t.stride(d)
-        ok = ok and t.stride(d) == stride * rows
-        rows *= t.shape[d]
+            stride = strides[d]
+        ok = ok and strides[d] == stride * rows
+        rows *= shape[d]
     if not ok or stride < H * D:
         raise ValueError("sv: the heads of a row must follow each other and rows lie equally far apart "
-                         f"(got shape={tuple(t.shape)}, strides={t.stride()})")
+                         f"(got shape={tuple(shape)}, strides={strides})")
     return t.data_ptr(), stride
+
+
+def _tag(t):
+    try:
+        return _TAGS[t.dtype]
+    except KeyError:
+        raise SvError(SV_ERR_DTYPE) from None
 
 
 class Cache:
@@ -748,19 +767,22 @@ class Cache:
         return cls(k, v, *(torch.empty((n_pages, heads, page), dtype=torch.float32, device=device) for _ in range(2)))
 
     def _ptrs(self):
-        return _ptr(self.k), _ptr(self.v), self.dtype, _ptr(self.k_scale), _ptr(self.v_scale), self.n_pages, self.page
+        return (_dense(self.k), _dense(self.v), self.dtype, _dense(self.k_scale), _dense(self.v_scale), self.n_pages, self.page)
 
 
 def _new_rows(rows, t_offsets, start, pages, P):
     """(n_rows, B, P) of new tokens whose rows have the leading shape `rows`: [B, P], or [n_rows] with t_offsets [B+1] and P."""
-    _i32(t_offsets, start, pages)
-    if pages.dim() != 2 or start.numel() != pages.shape[0]:
+    if pages.dim() != 2:
         raise SvError(SV_ERR_INVALID_ARG)
     B = pages.shape[0]
+    if start.numel() != B:
+        raise SvError(SV_ERR_INVALID_ARG)
     if t_offsets is None:
+        _i32(start, pages)
         if len(rows) != 2 or rows[0] != B or (P is not None and P != rows[1]):
             raise SvError(SV_ERR_INVALID_ARG)
         return rows[0] * rows[1], B, rows[1]
+    _i32(t_offsets, start, pages)
     if len(rows) != 1 or P is None or t_offsets.numel() != B + 1:
         raise SvError(SV_ERR_INVALID_ARG)
     return rows[0], B, P
@@ -770,8 +792,8 @@ def sv_rope_frequencies(freq, base=10000.0, scaling=SV_ROPE_PLAIN, factor=1.0, l
     """freq: [rot / 2] float64."""
     if freq.dtype != torch.float64:
         raise SvError(SV_ERR_DTYPE)
-    _device_of(freq)
-    _check(lib.sv_rope_frequencies(2 * freq.numel(), base, scaling, factor, low, high, length, _ptr(freq), _stream(stream)))
+    _here(freq)
+    _check(lib.sv_rope_frequencies(2 * freq.numel(), base, scaling, factor, low, high, length, _dense(freq), _stream(stream)))
 
 
 def _freq(freq):
@@ -779,30 +801,32 @@ def _freq(freq):
         return None, 0
     if freq.dtype != torch.float64:
         raise SvError(SV_ERR_DTYPE)
-    return _ptr(freq), 2 * freq.numel()
+    return _dense(freq), 2 * freq.numel()
 
 
 def sv_rope(x, positions, freq, out, layout=SV_ROPE_HALVES, amplitude=1.0, inverse=False, stream=None):
     """x, out: [..., H, D], out may be x; positions: one int32 per row; freq: [rot / 2] float64."""
     addr, stride = _heads(x)
     o_addr, o_stride = _heads(out)
-    H, D = x.shape[-2:]
-    n = x.numel() // (H * D) if H * D else 0
-    if out.shape != x.shape or out.dtype != x.dtype or positions.numel() != n:
+    shape = x.shape
+    H, D = shape[-2:]
+    n = positions.numel()
+    if out.shape != shape or out.dtype != x.dtype or x.numel() != n * H * D:
         raise SvError(SV_ERR_INVALID_ARG)
     _i32(positions)
-    _device_of(x, positions, freq, out)
+    _here(x, positions, freq, out)
     f, rot = _freq(freq)
-    _check(lib.sv_rope(addr, stride, _ptr(positions), n, H, D, _dtype_tag(x), f, rot, layout, amplitude, int(inverse), o_addr,
-                       o_stride, _stream(stream)))
+    _check(lib.sv_rope(addr, stride, _dense(positions), n, H, D, _tag(x), f, rot, layout, amplitude, inverse, o_addr, o_stride,
+                       _stream(stream)))
 
 
 def sv_cache_write(cache, k, v, lengths, pages, t_offsets=None, P=None, q=None, q_out=None, freq=None,
                    layout=SV_ROPE_HALVES, amplitude=1.0, flags=None, stream=None):
     """k, v: [B, P, heads, D]; or [n_rows, heads, D] with t_offsets [B+1] and P.  q, q_out: the same with the queries' heads.
     pages: [B, max_pages].  freq None: nothing is turned."""
-    n_rows, B, P = _new_rows(k.shape[:-2], t_offsets, lengths, pages, P)
-    if v.shape != k.shape or v.dtype != k.dtype or tuple(k.shape[-2:]) != (cache.heads, cache.D):
+    shape = k.shape
+    n_rows, B, P = _new_rows(shape[:-2], t_offsets, lengths, pages, P)
+    if v.shape != shape or v.dtype != k.dtype or shape[-2] != cache.heads or shape[-1] != cache.D:
         raise SvError(SV_ERR_INVALID_ARG)
     k_addr, k_stride = _heads(k)
     v_addr, v_stride = _heads(v)
@@ -810,38 +834,40 @@ def sv_cache_write(cache, k, v, lengths, pages, t_offsets=None, P=None, q=None, 
     if (q is None) != (q_out is None):
         raise SvError(SV_ERR_NULL)
     if q is not None:
-        if q.shape[:-2] != k.shape[:-2] or q.shape[-1] != cache.D or q_out.shape != q.shape:
+        q_shape = q.shape
+        if q_shape[:-2] != shape[:-2] or q_shape[-1] != cache.D or q_out.shape != q_shape:
             raise SvError(SV_ERR_INVALID_ARG)
         if q.dtype != k.dtype or q_out.dtype != k.dtype:
             raise SvError(SV_ERR_DTYPE)
         q_addr, q_stride = _heads(q)
         o_addr, o_stride = _heads(q_out)
-        Hq = q.shape[-2]
+        Hq = q_shape[-2]
     if flags is not None:
         _i32(flags)
         _outputs((n_rows,), flags)
-    _device_of(k, v, cache.k, q, q_out, lengths, pages, t_offsets, freq, flags)
+    _here(k, v, cache.k, cache.v, cache.k_scale, cache.v_scale, q, q_out, lengths, pages, t_offsets, freq, flags)
     f, rot = _freq(freq)
     kc, vc, tag, ks, vs, n_pages, page = cache._ptrs()
-    _check(lib.sv_cache_write(k_addr, k_stride, v_addr, v_stride, q_addr, q_stride, Hq, o_addr, o_stride, _ptr(t_offsets), n_rows,
-                              _ptr(lengths), _ptr(pages), pages.shape[1], B, P, cache.heads, cache.D, _dtype_tag(k), f, rot, layout,
-                              amplitude, kc, vc, tag, ks, vs, n_pages, page, _ptr(flags), _stream(stream)))
+    _check(lib.sv_cache_write(k_addr, k_stride, v_addr, v_stride, q_addr, q_stride, Hq, o_addr, o_stride, _dense(t_offsets), n_rows,
+                              _dense(lengths), _dense(pages), pages.shape[1], B, P, cache.heads, cache.D, _tag(k), f, rot, layout,
+                              amplitude, kc, vc, tag, ks, vs, n_pages, page, _dense(flags), _stream(stream)))
 
 
 def sv_cache_read(cache, k, v, start, pages, t_offsets=None, P=None, flags=None, stream=None):
     """k, v (out): [B, P, heads, D]; or [n_rows, heads, D] with t_offsets [B+1] and P: positions start[b] + i."""
-    n_rows, B, P = _new_rows(k.shape[:-2], t_offsets, start, pages, P)
-    if v.shape != k.shape or v.dtype != k.dtype or tuple(k.shape[-2:]) != (cache.heads, cache.D):
+    shape = k.shape
+    n_rows, B, P = _new_rows(shape[:-2], t_offsets, start, pages, P)
+    if v.shape != shape or v.dtype != k.dtype or shape[-2] != cache.heads or shape[-1] != cache.D:
         raise SvError(SV_ERR_INVALID_ARG)
     k_addr, k_stride = _heads(k)
     v_addr, v_stride = _heads(v)
     if flags is not None:
         _i32(flags)
         _outputs((n_rows,), flags)
-    _device_of(k, v, cache.k, start, pages, t_offsets, flags)
+    _here(k, v, cache.k, cache.v, cache.k_scale, cache.v_scale, start, pages, t_offsets, flags)
     kc, vc, tag, ks, vs, n_pages, page = cache._ptrs()
-    _check(lib.sv_cache_read(kc, vc, tag, ks, vs, n_pages, page, _ptr(t_offsets), n_rows, _ptr(start), _ptr(pages), pages.shape[1], B,
-                             P, cache.heads, cache.D, _dtype_tag(k), k_addr, k_stride, v_addr, v_stride, _ptr(flags),
+    _check(lib.sv_cache_read(kc, vc, tag, ks, vs, n_pages, page, _dense(t_offsets), n_rows, _dense(start), _dense(pages),
+                             pages.shape[1], B, P, cache.heads, cache.D, _tag(k), k_addr, k_stride, v_addr, v_stride, _dense(flags),
                              _stream(stream)))
 
 
@@ -852,44 +878,54 @@ def sv_chunk_attention_workspace_bytes(B, P, Hq, heads, D, dtype, max_pages, pag
 def sv_chunk_attention(cache, q, out, lengths, pages, t_offsets=None, P=None, scale=None, window=0, first=None, lse=None,
                        flags=None, ws=None, stream=None):
     """q, out: [B, P, Hq, D]; or [n_rows, Hq, D] with t_offsets [B+1] and P.  scale None: 1 / sqrt(D).  ws None: scratch is torch's."""
-    n_rows, B, P = _new_rows(q.shape[:-2], t_offsets, lengths, pages, P)
-    Hq, D = q.shape[-2:]
-    if out.shape != q.shape or out.dtype != q.dtype or D != cache.D:
+    shape = q.shape
+    n_rows, B, P = _new_rows(shape[:-2], t_offsets, lengths, pages, P)
+    Hq, D = shape[-2:]
+    if out.shape != shape or out.dtype != q.dtype or D != cache.D:
         raise SvError(SV_ERR_INVALID_ARG)
     q_addr, q_stride = _heads(q)
     o_addr, o_stride = _heads(out)
-    _i32(first, flags)
-    _f32(lse)
     if first is not None:
+        _i32(first)
         _outputs((B,), first)
-    _outputs((n_rows, Hq), lse)
-    _outputs((n_rows,), flags)
-    _device_of(q, out, cache.k, lengths, pages, t_offsets, first, lse, flags, ws)
-    tag = _dtype_tag(q)
+    if lse is not None:
+        _f32(lse)
+        _outputs((n_rows, Hq), lse)
+    if flags is not None:
+        _i32(flags)
+        _outputs((n_rows,), flags)
+    _here(q, out, cache.k, cache.v, cache.k_scale, cache.v_scale, lengths, pages, t_offsets, first, lse, flags, ws)
+    tag, max_pages = _tag(q), pages.shape[1]
     if ws is None:
-        n = lib.sv_chunk_attention_workspace_bytes(B, P, Hq, cache.heads, D, tag, pages.shape[1], cache.page)
+        n = lib.sv_chunk_attention_workspace_bytes(B, P, Hq, cache.heads, D, tag, max_pages, cache.page)
         if n > 0 and stream is None:
-            ws = torch.empty(n, dtype=torch.uint8, device=q.device)
+            ws = torch.empty(n, dtype=torch.uint8, device="cuda")
         elif n > 0:
             with torch.cuda.stream(stream):
-                ws = torch.empty(n, dtype=torch.uint8, device=q.device)
+                ws = torch.empty(n, dtype=torch.uint8, device="cuda")
     kc, vc, c_tag, ks, vs, n_pages, page = cache._ptrs()
-    _check(lib.sv_chunk_attention(q_addr, q_stride, _ptr(t_offsets), n_rows, _ptr(lengths), _ptr(first), _ptr(pages), pages.shape[1],
-                                  B, P, Hq, cache.heads, D, tag, kc, vc, c_tag, ks, vs, n_pages, page,
-                                  D ** -0.5 if scale is None else scale, window, o_addr, o_stride, _ptr(lse), _ptr(flags), _ptr(ws),
-                                  0 if ws is None else ws.numel(), _stream(stream)))
+    _check(lib.sv_chunk_attention(q_addr, q_stride, _dense(t_offsets), n_rows, _dense(lengths), _dense(first), _dense(pages),
+                                  max_pages, B, P, Hq, cache.heads, D, tag, kc, vc, c_tag, ks, vs, n_pages, page,
+                                  D ** -0.5 if scale is None else scale, window, o_addr, o_stride, _dense(lse), _dense(flags),
+                                  _dense(ws), 0 if ws is None else ws.numel(), _stream(stream)))
 
 
 def sv_sample(z, u, token, logprob=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, flags=None, stream=None):
     """z: [..., V]; u (float64), token (int32), logprob, flags: one entry per row."""
     V = z.shape[-1]
-    rows = z.numel() // V if V else 0
+    rows = u.numel()
     if u.dtype != torch.float64:
         raise SvError(SV_ERR_DTYPE)
-    _i32(token, flags)
-    _f32(logprob)
-    _outputs((rows,), u, token, logprob, flags)
-    _device_of(z, u, token, logprob, flags)
+    if z.numel() != rows * V or token.numel() != rows:
+        raise SvError(SV_ERR_INVALID_ARG)
+    _i32(token)
+    if logprob is not None:
+        _f32(logprob)
+        _outputs((rows,), logprob)
+    if flags is not None:
+        _i32(flags)
+        _outputs((rows,), flags)
+    _here(z, u, token, logprob, flags)
     addr, stride = _strided(z)
-    _check(lib.sv_sample(addr, stride, rows, V, _dtype_tag(z), temperature, top_k, top_p, min_p, _ptr(u), _ptr(token), _ptr(logprob),
-                         _ptr(flags), _stream(stream)))
+    _check(lib.sv_sample(addr, stride, rows, V, _tag(z), temperature, top_k, top_p, min_p, _dense(u), _dense(token), _dense(logprob),
+                         _dense(flags), _stream(stream)))

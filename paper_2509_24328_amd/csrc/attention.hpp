@@ -171,13 +171,15 @@ struct Wavefront {
 
   __device__ __forceinline__ Wavefront(const AttnArgs& args) : a(args), g((threadIdx.x & 63) >> 4), m(threadIdx.x & 15) {}
 
-  // (-1: in no page)
+  // Row of the cache, in units of D columns, of a position and this head; -1: in no page.
   __device__ __forceinline__ int64_t page_row(int key) const {
     const int k = divide(key, a.pages.page);
     const int at = k < a.pages.max_pages ? table[k] : -1;
     if (at < 0 || at >= a.pages.n_pages) return -1;
     return (int64_t)at * a.pages.heads * (int)a.pages.page.d + head_off + (key - k * (int)a.pages.page.d);
   }
+
+  __device__ __forceinline__ int row_bytes() const { return (WHOLE ? DPAD : a.D) * Sh::cb; }
 
   __device__ __forceinline__ void start(const Sequence& s, int rho0, int h) {
 #pragma unroll
@@ -208,7 +210,6 @@ struct Wavefront {
     }
   }
 
-  // Keys and values of a step.  Addresses are those of keys within [lo, hi): a key outside it stands for one inside, and its weight is 0.
   struct Keys {
     Words<4> k[2][Sh::NK];
     float scale[2][4];
@@ -217,73 +218,108 @@ struct Wavefront {
     Words<Sh::WV> v[8][Sh::NB];
     float scale[8];
   };
-  // The pages of the two tiles of a step, where a tile lies in one page: rows of the cache of their first keys.
+  // Where the keys of a step are.  WHOLE: rows of the first keys of its two tiles, the same in all lanes (a tile lies in one page);
+  // otherwise the row of key `lane % 32`, which the lanes that need it take from there.  -1: in no page.
   struct Where {
-    int64_t row[2];
+    int64_t row[WHOLE ? 2 : 1];
   };
 
+  // Keys outside [lo, hi) stand for one inside: they are read, and have no weight.
   __device__ __forceinline__ void find(int key0, int lo, int hi, Where& w) const {
     if constexpr (WHOLE) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        // (the tile's first key, or if the tile is outside, that of a tile that is not)
         const int first = min(max(key0 + 16 * t, lo & ~15), (hi - 1) & ~15);
-        const int64_t row = page_row(__builtin_amdgcn_readfirstlane(first));
-        const uint32_t r0 = __builtin_amdgcn_readfirstlane((uint32_t)row), r1 = __builtin_amdgcn_readfirstlane((uint32_t)(row >> 32));
+        w.row[t] = page_row(__builtin_amdgcn_readfirstlane(first));
+      }
+    } else {
+      w.row[0] = page_row(min(max(key0 + (int)(threadIdx.x & 31), lo), hi - 1));
+    }
+  }
+  // (after a wait for the table's entries)
+  __device__ __forceinline__ void settle(Where& w) const {
+    if constexpr (WHOLE) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const uint32_t r0 = __builtin_amdgcn_readfirstlane((uint32_t)w.row[t]), r1 = __builtin_amdgcn_readfirstlane((uint32_t)(w.row[t] >> 32));
         w.row[t] = (int64_t)(((uint64_t)r1 << 32) | r0);
       }
     }
   }
-
-  // Row of the cache of key key0 + 16 t + k.
-  __device__ __forceinline__ int64_t row_of(int key0, int t, int k, int lo, int hi, const Where& w) const {
-    if constexpr (WHOLE) return w.row[t] < 0 ? 0 : w.row[t] + k;
-    const int64_t r = page_row(min(max(key0 + 16 * t + k, lo), hi - 1));
-    return r < 0 ? 0 : r;
+  __device__ __forceinline__ int64_t found(const Where& w, int t, int k) const {         // (unclamped: -1 where there is none)
+    if constexpr (WHOLE) return w.row[t] < 0 ? -1 : w.row[t] + k;
+    const int from = 16 * t + k;
+    const uint32_t r0 = __shfl((int)(uint32_t)w.row[0], from, kWave), r1 = __shfl((int)(w.row[0] >> 32), from, kWave);
+    return (int64_t)(((uint64_t)r1 << 32) | r0);
   }
 
-  __device__ __forceinline__ void load_keys(int key0, int lo, int hi, const Where& w, Keys& kk) const {
+  __device__ __forceinline__ void load_keys(const Where& w, Keys& kk) const {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const char* row = a.k_cache + row_of(key0, t, m, lo, hi, w) * (int64_t)(a.D * Sh::cb);
+      const char* row;
+      if constexpr (WHOLE) row = a.k_cache + (w.row[t] < 0 ? 0 : w.row[t]) * row_bytes() + (uint32_t)(m * row_bytes() + 16 * g);
+      else row = a.k_cache + max(found(w, t, m), (int64_t)0) * row_bytes() + 16 * g;
 #pragma unroll
       for (int k = 0; k < Sh::NK; ++k) {
-        const int at = 64 * k + 16 * g, bytes = a.D * Sh::cb;
+        const int at = 64 * k + 16 * g, bytes = row_bytes();
         if constexpr (WHOLE) {
-          load_words<4>(row + at, kk.k[t][k].w);
+          load_words<4>(row + 64 * k, kk.k[t][k].w);
         } else {
           kk.k[t][k] = Words<4>{{0u, 0u, 0u, 0u}};
-          if (at + 16 <= bytes) load_words<4>(row + at, kk.k[t][k].w);
+          if (at + 16 <= bytes) load_words<4>(row + 64 * k, kk.k[t][k].w);
           else if (at + 8 <= bytes) {
             uint32_t w2[2];
-            load_words<2>(row + at, w2);
+            load_words<2>(row + 64 * k, w2);
             kk.k[t][k].w[0] = w2[0];
             kk.k[t][k].w[1] = w2[1];
           }
         }
       }
       if constexpr (Sh::f8) {
+        if constexpr (WHOLE) {
+          uint32_t x[4];
+          load_words<4>(reinterpret_cast<const char*>(a.k_scale + (w.row[t] < 0 ? 0 : w.row[t]) + 4 * g), x);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) kk.scale[t][r] = a.k_scale[row_of(key0, t, 4 * g + r, lo, hi, w)];
+          for (int r = 0; r < 4; ++r) kk.scale[t][r] = __uint_as_float(x[r]);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) kk.scale[t][r] = a.k_scale[max(found(w, t, 4 * g + r), (int64_t)0)];
+        }
       }
     }
   }
 
-  __device__ __forceinline__ void load_values(int key0, int lo, int hi, const Where& w, Values& vv) const {
+  __device__ __forceinline__ void load_values(const Where& w, Values& vv) const {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int64_t at = row_of(key0, i / 4, 4 * g + i % 4, lo, hi, w);
-      const char* row = a.v_cache + at * (int64_t)(a.D * Sh::cb);
+      const int t = i / 4, r = i % 4;
+      const char* row;
+      int64_t at = 0;
+      if constexpr (WHOLE) {
+        row = a.v_cache + (w.row[t] < 0 ? 0 : w.row[t]) * row_bytes() + (uint32_t)(4 * g * row_bytes() + m * Sh::W * Sh::cb) + r * row_bytes();
+      } else {
+        at = max(found(w, t, 4 * g + r), (int64_t)0);
+        row = a.v_cache + at * row_bytes() + m * Sh::W * Sh::cb;
+      }
 #pragma unroll
       for (int n = 0; n < Sh::NB; ++n) {
         const int col = (16 * n + m) * Sh::W;
-        if (WHOLE || col < a.D) load_words<Sh::WV>(row + col * Sh::cb, vv.v[i][n].w);
+        if (WHOLE || col < a.D) load_words<Sh::WV>(row + 16 * n * Sh::W * Sh::cb, vv.v[i][n].w);
         else {
 #pragma unroll
           for (int j = 0; j < Sh::WV; ++j) vv.v[i][n].w[j] = 0u;
         }
       }
-      if constexpr (Sh::f8) vv.scale[i] = a.v_scale[at];
+      if constexpr (Sh::f8 && !WHOLE) vv.scale[i] = a.v_scale[at];
+    }
+    if constexpr (Sh::f8 && WHOLE) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        uint32_t x[4];
+        load_words<4>(reinterpret_cast<const char*>(a.v_scale + (w.row[t] < 0 ? 0 : w.row[t]) + 4 * g), x);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) vv.scale[4 * t + r] = __uint_as_float(x[r]);
+      }
     }
   }
 
@@ -332,9 +368,17 @@ struct Wavefront {
   }
 
   // Scores to weights, in place (p: what multiplies the values), with the running maximum and sum.  PART: some key of the step is not
-  // seen by some row; bad: tiles without a page.
+  // seen by some row, or in no page.  ks: scales of the keys (8 bits).
   template <bool PART>
-  __device__ __forceinline__ void weigh(int key0, const Keys& kk, const Values& vv, const bool (&bad)[2], f32x4 (&s)[NT][2]) {
+  __device__ __forceinline__ void weigh(int key0, const float (&ks)[2][4], const Values& vv, const Where& w, f32x4 (&s)[NT][2]) {
+    bool none[2][4];
+    if (PART) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) none[t][r] = found(w, t, 4 * g + r) < 0;
+      }
+    }
     bool raise = false;
     float top[NT];
 #pragma unroll
@@ -344,13 +388,10 @@ struct Wavefront {
       for (int t = 0; t < 2; ++t) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float x = s[n][t][r] * a.scale2;
-          if constexpr (Sh::f8) x *= kk.scale[t][r];
+          float x = s[n][t][r] * (Sh::f8 ? ks[t][r] : a.scale2);
           if (PART) {
             const int key = key0 + 16 * t + 4 * g + r;
-            bool none = bad[t];
-            if constexpr (!WHOLE) none = page_row(min(key, 0x3fffffff)) < 0;
-            x = none ? NAN : x;
+            x = none[t][r] ? NAN : x;
             x = key >= low[n] && key <= pos[n] ? x : -INFINITY;
           }
           s[n][t][r] = x;
@@ -462,10 +503,21 @@ struct Wavefront {
     }
   }
 
-  // Values of a step some of whose keys are not seen by some row: 0 where no row of the block sees the key; returns whether one that a
-  // row does see is not finite.
+  // Values of a step some of whose keys are not seen by some row: 0 where no row of the block sees the key, and where one is not finite, which
+  // the matrix cores would spread to every row (0 times it is NaN); returns whether there is one.
   __device__ __forceinline__ bool clean_values(int key0, int lo, int hi, Values& vv) const {
-    bool odd = false;
+    auto odd_in = [](uint32_t w) -> uint32_t {             // bits of w that belong to numbers that are not finite
+      if constexpr (Sh::f8) {
+        // a byte 0x7f or 0xff is a NaN: adding 1 to the seven bits carries into the eighth
+        const uint32_t top = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+        return (top >> 7) * 0xffu;
+      } else if constexpr (Sh::f32) {
+        return (w & 0x7f800000u) == 0x7f800000u ? 0xffffffffu : 0u;
+      } else {
+        return ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u) | ((w & 0x00007f80u) == 0x00007f80u ? 0x0000ffffu : 0u);
+      }
+    };
+    uint32_t odd = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int key = key0 + 16 * (i / 4) + 4 * g + i % 4;
@@ -476,60 +528,104 @@ struct Wavefront {
         for (int j = 0; j < Sh::WV; ++j) {
           uint32_t& w = vv.v[i][nb].w[j];
           w = in ? w : 0u;
-          if constexpr (Sh::f8) {
-            // a byte 0x7f or 0xff is a NaN: adding 1 to the seven bits carries into the eighth
-            odd |= (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
-          } else if constexpr (Sh::f32) {
-            odd |= (w & 0x7f800000u) == 0x7f800000u;
-          } else {
-            odd |= (w & 0x7f800000u) == 0x7f800000u || (w & 0x00007f80u) == 0x00007f80u;
-          }
+          const uint32_t bits = odd_in(w);
+          odd |= bits;
+          w &= ~bits;
         }
       }
     }
-    return __ballot(odd) != 0;
+    return __ballot(odd != 0) != 0;
   }
 
-  // add_values where a value that some row must not see is not finite: key by key, each added to the rows that see it alone.
-  __device__ __forceinline__ void add_values_apart(int key0, const Values& vv, const f32x4 (&s)[NT][2]) {
+  // What clean_values took out, added to the rows that see it: weights are positive, so a sum with such a term is that of the values
+  // themselves.  Read again from the cache, key by key.
+  __device__ __forceinline__ void add_odd_values(int key0, int lo, int hi, const Where& w) {
 #pragma unroll 1
-    for (int j = 0; j < 32; ++j) {
-      const int i = j & 7, owner = j >> 3;                  // slot i of the lanes 16 owner .. 16 owner + 15
-      const int key = key0 + 16 * (i / 4) + 4 * owner + i % 4;
+    for (int j = 0; j < kStep; ++j) {
+      const int key = key0 + j;
+      const int64_t at = found(w, 0, j & 15), at1 = found(w, 1, j & 15), row = j < 16 ? at : at1;
+      if (key < lo || key >= hi || row < 0) continue;
+      const char* from = a.v_cache + row * row_bytes();
 #pragma unroll
-      for (int nb = 0; nb < Sh::NB; ++nb) {
-        if constexpr (!Sh::f32) {
-          uint32_t w[Sh::W][4];
-          value_words(vv, nb, w);
+      for (int t = 0; t < NO; ++t) {
 #pragma unroll
-          for (int c = 0; c < Sh::W; ++c) {
-            uint32_t x[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = g == owner && k == i / 2 ? w[c][k] & ((i & 1) ? 0xffff0000u : 0x0000ffffu) : 0u;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x[0], x[1], x[2], x[3]), weights(s[n]),
-                                                                    o[n][nb * Sh::W + c], 0, 0, 0);
-              if (key >= low[n] && key <= pos[n]) o[n][nb * Sh::W + c] = y;
+        for (int r = 0; r < 4; ++r) {
+          const int col = (16 * (t / Sh::W) + 4 * g + r) * Sh::W + t % Sh::W;
+          float v = 0.f;
+          if (WHOLE || col < a.D) {
+            if constexpr (Sh::f8) {
+              const uint8_t c = static_cast<uint8_t>(from[col]);
+              v = (c & 0x7f) == 0x7f ? NAN : 0.f;
+            } else if constexpr (Sh::f32) {
+              v = reinterpret_cast<const float*>(from)[col];
+            } else {
+              v = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(from)[col] << 16);
             }
           }
-        } else {
+          const bool odd = !(fabsf(v) < INFINITY);
 #pragma unroll
-          for (int c = 0; c < Sh::W; ++c) {
-            float x = 0.f;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) x = k == i && g == owner ? value_f32(vv, k, nb, c) : x;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              float p = 0.f;
-#pragma unroll
-              for (int k = 0; k < 8; ++k) p = k == i ? s[n][k / 4][k % 4] : p;
-              const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p, o[n][nb * Sh::W + c], 0, 0, 0);
-              if (key >= low[n] && key <= pos[n]) o[n][nb * Sh::W + c] = y;
-            }
-          }
+          for (int n = 0; n < NT; ++n)
+            if (odd && key >= low[n] && key <= pos[n]) o[n][t][r] += v;
         }
       }
+    }
+  }
+
+  __device__ __forceinline__ void scaled(const Keys& kk, float (&ks)[2][4]) const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) ks[t][r] = Sh::f8 ? kk.scale[t][r] * a.scale2 : 0.f;
+    }
+  }
+
+  // Steps whose keys some row does not see, or are in no page.
+  __device__ __forceinline__ void sweep_part(int s0, int s1, int stride, int lo, int hi) {
+#pragma unroll 1
+    for (int s = s0; s < s1; s += stride) {
+      const int key0 = kStep * s;
+      Where at;
+      find(key0, lo, hi, at);
+      settle(at);
+      Keys kk;
+      Values vv;
+      load_keys(at, kk);
+      load_values(at, vv);
+      f32x4 sc[NT][2];
+      scores(kk, sc);
+      float ks[2][4];
+      scaled(kk, ks);
+      weigh<true>(key0, ks, vv, at, sc);
+      const bool odd = clean_values(key0, lo, hi, vv);
+      add_values(vv, sc);
+      if (odd) add_odd_values(key0, lo, hi, at);
+    }
+  }
+
+  // Steps whose keys all rows see.  The keys of the next step are asked for before the weights of this one are formed, its values
+  // before the scores are.
+  __device__ __forceinline__ void sweep_all(int s0, int s1, int stride, int lo, int hi) {
+    if (s0 >= s1) return;
+    Where at;
+    Keys kk;
+    find(kStep * s0, lo, hi, at);
+    settle(at);
+    load_keys(at, kk);
+#pragma unroll 1
+    for (int s = s0; s < s1; s += stride) {
+      Where next;
+      find(kStep * min(s + stride, s1 - 1), lo, hi, next);
+      Values vv;
+      load_values(at, vv);
+      f32x4 sc[NT][2];
+      scores(kk, sc);
+      float ks[2][4];
+      scaled(kk, ks);
+      settle(next);
+      if (s + stride < s1) load_keys(next, kk);
+      weigh<false>(kStep * s, ks, vv, at, sc);
+      add_values(vv, sc);
+      at = next;
     }
   }
 
@@ -550,42 +646,30 @@ struct Wavefront {
     }
     all_lo = __builtin_amdgcn_readfirstlane(max(all_lo, lo));
     all_hi = __builtin_amdgcn_readfirstlane(min(all_hi, hi - 1));
-    Where at, next;
-    Keys kk;
-    find(kStep * s0, lo, hi, at);
-    load_keys(kStep * s0, lo, hi, at, kk);
-    for (int s = s0; s < s1; s += stride) {
-      const int key0 = kStep * s;
-      Values vv;
-      load_values(key0, lo, hi, at, vv);
-      f32x4 sc[NT][2];
-      scores(kk, sc);
-      Keys kept = kk;
-      const int after = min(s + stride, s1 - 1);
-      find(kStep * after, lo, hi, next);
-      if (s + stride < s1) load_keys(kStep * after, lo, hi, next, kk);
-      bool bad[2] = {false, false};
-      if constexpr (WHOLE) {
-        bad[0] = at.row[0] < 0;
-        bad[1] = at.row[1] < 0;
-      }
-      const bool part = !WHOLE || key0 < all_lo || key0 + kStep - 1 > all_hi || bad[0] || bad[1];
-      if (!part) {
-        weigh<false>(key0, kept, vv, bad, sc);
-        add_values(vv, sc);
-      } else {
-        weigh<true>(key0, kept, vv, bad, sc);
-        if (clean_values(key0, lo, hi, vv)) add_values_apart(key0, vv, sc);
-        else add_values(vv, sc);
-      }
-      at = next;
+    if (all_hi == 0x7fffffff) return;                    // no row is there
+    // whether a page is missing
+    bool gone = false;
+    const int last = divide(min(kStep * s1, hi) - 1, a.pages.page);
+    for (int k = divide(max(kStep * s0, lo), a.pages.page) + (int)(threadIdx.x & (kWave - 1)); k <= last; k += kWave) {
+      const int p = table[k];
+      gone |= p < 0 || p >= a.pages.n_pages;
     }
+    // steps [f0, f1) are seen whole
+    int f0 = (all_lo + kStep - 1) / kStep, f1 = (all_hi + 1) / kStep;
+    if (__ballot(gone)) f1 = f0;
+    f0 = min(max(f0, s0), s1);
+    f0 = s0 + (f0 - s0 + stride - 1) / stride * stride;
+    f1 = min(max(f1, f0), s1);
+    sweep_part(s0, min(f0, s1), stride, lo, hi);
+    sweep_all(f0, f1, stride, lo, hi);
+    const int from = f1 > f0 ? f0 + (f1 - f0 + stride - 1) / stride * stride : f0;
+    sweep_part(from, s1, stride, lo, hi);
   }
 };
 
 // One workgroup: a row block of a head of a sequence, a part of its keys.
 template <int ET, int CT, int DPAD, int NT, int WR, int WK, bool WHOLE>
-__global__ void __launch_bounds__(kAttnWaves* kWave, 1) attention_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kAttnWaves* kWave, (DPAD == 256 || (ET == SV_F32 && DPAD == 128) ? 1 : 2)) attention_kernel(AttnArgs a) {
   static_assert(WR * WK == kAttnWaves, "four wavefronts");
   using Wf = Wavefront<ET, CT, DPAD, NT, WHOLE>;
   using Sh = Shape<ET, CT, DPAD>;
