@@ -27,6 +27,8 @@ OWN_FLAGS = {
     "row_stats.hip": ["-mllvm", "-disable-machine-licm"],
     # likewise: the logits of a row stay in registers from its sums to its gradient
     "token_logprobs.hip": ["-mllvm", "-disable-machine-licm"],
+    # and the constants of an fp64 exponential again
+    "sample.hip": ["-mllvm", "-disable-machine-licm"],
 }
 
 

@@ -5,14 +5,14 @@
 //   sweep     the row's maximum m, and of every sixteen bytes the largest entry (its upper sixteen bits, in LDS); for a nucleus without
 //             a K, the row's mass, in float32 and good to 4e-6
 //   tau       a value that K entries reach: the K-th largest of the lanes' maxima, or of the vectors' (distinct entries of the
-//             row); for a nucleus a guess, and what min-p says
+//             row), or a little less; for a nucleus a guess, and what min-p says
 //   list      the entries that reach tau, by ascending token, from the few vectors that hold one
-//   settle    counts and masses above each entry of the list; what is kept; its masses by token, and the one that holds u W
+//   settle    counts and masses above the entries of the list; what is kept; its masses by token, and the one that holds u W
 // up to 64 entries by one wavefront without a barrier.  A list that does not reach as far as the warps do (a deep nucleus, a K of thousands)
-// is narrowed instead: sweeps count and weigh what lies above a value, until the stretch that holds the cutoff fits a list or is one
-// value.  Where a decision lies within the float32 mass's error of its target, the mass is summed again in fp64.
-// Weights are fp64 (2^x as a polynomial: an error of 1e-15, where float32 exponentials would make 1 row in 300 of a flat 152064-entry
-// distribution draw another token), and every sum has an order that the sizes fix.
+// is narrowed from both sides instead: a sweep counts and weighs, in float32, what lies above three values, until the stretch that holds the
+// cutoff fits a list or is one value.  Where a decision lies within the float32 masses' error of its target, it is taken in fp64.
+// Weights of what is drawn are fp64 (2^x as a polynomial: an error of 1e-15, where float32 exponentials would make 1 row in 300 of a flat
+// 152064-entry distribution draw another token), and every sum has an order that the sizes fix, or terms that add exactly.
 #include "sv_device.hpp"
 #include "sv_host.hpp"
 
@@ -26,7 +26,7 @@ constexpr int kOwn = kList / kDrawThreads;   // entries of the list that a threa
 constexpr int kNucleusRank = 40;         // first guess of a nucleus: the entries above this many lane maxima
 constexpr int kDeepRank = 1200;          // second guess: above this many vectors' maxima
 constexpr int kMaxKeys = 40960;          // vectors' maxima in LDS (80 KB); longer rows share one among several vectors
-// Error of the float32 mass, relative: the exponent k of a weight is off by 2^-23 |k| (difference and product), which is 8.3e-8 |k| of the
+// Error of a float32 mass, relative: the exponent k of a weight is off by 2^-23 |k| (difference and product), which is 8.3e-8 |k| of the
 // weight; an average over the mass has |k| <= 24 (2^24 entries that far down weigh as much as the first).  Up to six factors of v_exp_f32
 // (a lane's maximum is raised a few times), 2^-23 each, and 2^-21 for sums of eight terms: 3.3e-6.
 constexpr double kMassError = 4e-6;
@@ -68,62 +68,119 @@ __device__ __forceinline__ double exp2_series(double k) {
   return k < -1000.0 ? 0.0 : __builtin_ldexp(p, (int)n);
 }
 
-struct DrawShared {
-  uint32_t vec[kList];                   // vectors of the list
-  int count[2][kDrawWaves];
-  uint64_t key[kList];                   // order key above, ~token below: sorted descending
-  double cum[kList];                     // masses down the list, or of the kept entries up to a token
-  double wave_d[kDrawWaves], out_d[2];
-  int wave_i[kDrawWaves], out_i[2];
-  uint32_t wave_u[kDrawWaves];
-  int n, hit;
+// Weight in float32 of an entry `below` (<= 0) the largest one: hi + lo is the scale.
+struct FastScale {
+  float hi, lo;
+  __device__ __forceinline__ float weight(float below) const {
+    const float b = fmaxf(below, -1e30f);                // (-inf times lo is no -inf)
+    return exp2_fast(__builtin_fmaf(b, hi, b * lo));
+  }
 };
 
-// Sum over the workgroup of a double and an int, in every thread.
-__device__ __forceinline__ void block_sums(double& d, int& c, DrawShared& sh) {
-  const int wave = threadIdx.x / kWave;
-  const double dw = wave_sum_f64(d);
-  const int cw = __builtin_amdgcn_readlane(wave_scan_i32(c), kWave - 1);
-  if ((threadIdx.x & (kWave - 1)) == 0) { sh.wave_d[wave] = dw; sh.wave_i[wave] = cw; }
-  __syncthreads();
-  double ds = 0.0;
-  int cs = 0;
-#pragma unroll
-  for (int w = 0; w < kDrawWaves; ++w) { ds += sh.wave_d[w]; cs += sh.wave_i[w]; }
-  __syncthreads();
-  d = ds;
-  c = cs;
-}
+struct alignas(16) DrawShared {
+  uint64_t key[kList];                   // order key of a value above, token below
+  double piece[kList];                   // masses of pieces of the row
+  uint32_t vec[kList];                   // vectors of the list
+  uint16_t lane_key[kDrawThreads];
+  double d[2][kDrawWaves][4];            // sums of the wavefronts; slots alternate, so that a reduction takes one barrier
+  int i[2][kDrawWaves][4];
+  float wave_top[kDrawWaves];
+  uint32_t wave_low[kDrawWaves];
+  int n, hit, state, token;
+  uint32_t found;
+  double mass, value;
+};
 
-// Inclusive scan of the workgroup's values in the order of the threads; total in every thread.
-__device__ __forceinline__ double block_scan(double v, double* total, DrawShared& sh) {
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  const double incl = wave_scan_f64(v);
-  if (lane == kWave - 1) sh.wave_d[wave] = incl;
-  __syncthreads();
-  double before = 0.0, all = 0.0;
-#pragma unroll
-  for (int w = 0; w < kDrawWaves; ++w) {
-    if (w == wave) before = all;
-    all += sh.wave_d[w];
+// Reductions over the workgroup.  Each writes one of two slots, so the readers of the last one are past it when it is written again.
+struct Team {
+  DrawShared& sh;
+  int turn = 0;
+  __device__ __forceinline__ int lane() const { return threadIdx.x & (kWave - 1); }
+  __device__ __forceinline__ int wave() const { return threadIdx.x / kWave; }
+
+  // The sum over eight lanes, the same in all of them.
+  static_assert(kDrawWaves == 8, "eight lanes hold the wavefronts' sums");
+  template <class T>
+  static __device__ __forceinline__ T of_eight(T v) {
+    v += lane_xor<1>(v);
+    v += lane_xor<2>(v);
+    return v + lane_xor<4>(v);
   }
-  __syncthreads();
-  *total = all;
-  return before + incl;
-}
+
+  // Sums of up to three doubles and counts; a count is the wavefront's own already, the same in its lanes.
+  template <int N, bool MASS>
+  __device__ __forceinline__ void sums(double (&s)[N], int (&c)[N]) {
+    turn ^= 1;
+    if constexpr (MASS) {
+      double w;
+      if constexpr (N == 1) w = wave_scan_f64(s[0]);     // (lane 63)
+      else w = wave_sum4_f64(s[0], N > 1 ? s[1 % N] : 0.0, N > 2 ? s[2 % N] : 0.0, 0.0);   // lanes 15, 31, 47
+      if (N == 1 ? lane() == 63 : (lane() & 15) == 15) sh.d[turn][wave()][N == 1 ? 0 : lane() >> 4] = w;
+    }
+    if (lane() == 0) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) sh.i[turn][wave()][k] = c[k];
+    }
+    __syncthreads();
+    const int w = threadIdx.x & 7;                       // (a lane reads one wavefront's, and eight of them add up)
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      if (MASS) s[k] = of_eight(sh.d[turn][w][k]);
+      c[k] = of_eight(sh.i[turn][w][k]);
+    }
+  }
+  __device__ __forceinline__ double sum(double v) {
+    double s[1] = {v};
+    int c[1] = {0};
+    sums<1, true>(s, c);
+    return s[0];
+  }
+  __device__ __forceinline__ int count(int of_wave) {
+    double s[1];
+    int c[1] = {of_wave};
+    sums<1, false>(s, c);
+    return c[0];
+  }
+  // Exclusive place of a thread's c items, or mass before its own, in the order of the threads; the total in every thread.
+  __device__ __forceinline__ int place(int c, int* total) {
+    const int incl = wave_scan_i32(c);
+    turn ^= 1;
+    if (lane() == kWave - 1) sh.i[turn][wave()][0] = incl;
+    __syncthreads();
+    const int w = threadIdx.x & 7, v = sh.i[turn][w][0];
+    *total = of_eight(v);
+    return of_eight(w < wave() ? v : 0) + incl - c;
+  }
+  __device__ __forceinline__ double place(double v, double* total) {
+    const double incl = wave_scan_f64(v);
+    turn ^= 1;
+    if (lane() == kWave - 1) sh.d[turn][wave()][0] = incl;
+    __syncthreads();
+    const int w = threadIdx.x & 7;
+    const double t = sh.d[turn][w][0];
+    *total = of_eight(t);
+    return of_eight(w < wave() ? t : 0.0) + (incl - v);
+  }
+};
+
+__device__ __forceinline__ int wave_sum_i32(int c) { return __builtin_amdgcn_readlane(wave_scan_i32(c), kWave - 1); }
 
 template <int DT>
 struct Draw {
   static constexpr int EPV = Elem<DT>::per_vec;
+  // the lower half of the order key of a bfloat16 value says nothing
+  static constexpr uint32_t kQuantum = DT == DT_BF16 ? 1u << 16 : 1u;
   const SampleArgs& a;
   const char* row;
   DrawShared& sh;
+  Team& team;
   double m;
+  FastScale fast;
 
   __device__ __forceinline__ double weight_log2(float z) const { return ((double)z - m) * a.scale; }
   __device__ __forceinline__ double weight(float z) const { return exp2_series(weight_log2(z)); }
 
-  // f(value, token) for every entry, in no order.
+  // f(values, first token, entries) for every vector, in no order.
   template <class F>
   __device__ __forceinline__ void each(F&& f) const {
     const int nvec = a.V / EPV;
@@ -138,6 +195,7 @@ struct Draw {
         float x[EPV];
         unpack<DT>(q[u], x);
         f(x, (i + u * kDrawThreads) * EPV, EPV);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     for (; i < nvec; i += kDrawThreads) {
@@ -154,31 +212,63 @@ struct Draw {
     }
   }
 
-  // Entries with keys >= at: their number and, if asked for, their mass.
-  __device__ __forceinline__ void above(uint32_t at, bool masses, int& count, double& mass) {
+  // Mass of the entries with keys >= at, in fp64.
+  __device__ __forceinline__ double mass_above(uint32_t at) {
     const float least = key_float(at);
-    int c = 0;
     double s = 0.0;
     each([&](const float (&x)[EPV], int, int n) {
       bool any = false;
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) {
-        const bool in = x[e] >= least && e < n;
-        c += in;
-        any |= in;
-      }
-      if (masses && any) {
+      for (int e = 0; e < EPV; ++e) any |= x[e] >= least;
+      if (!any) return;
 #pragma unroll
-        for (int e = 0; e < EPV; ++e) s += x[e] >= least && e < n ? weight(x[e]) : 0.0;
+      for (int e = 0; e < EPV; ++e) {
+        s += x[e] >= least && e < n ? weight(x[e]) : 0.0;
+        if (e % 2 == 1) __builtin_amdgcn_sched_barrier(0);
       }
     });
-    block_sums(s, c, sh);
-    count = c;
-    mass = s;
+    return team.sum(s);
   }
 
-  // Lists the entries with keys in [lo, hi) (hi 0: no upper bound), sorted descending; their number.  (More than kList: not all.)
-  __device__ __forceinline__ int list(uint32_t lo, uint32_t hi) {
+  // Entries with keys >= each of three, and their masses in float32 terms.
+  template <bool MASS>
+  __device__ __forceinline__ void above(const uint32_t (&at)[3], int (&count)[3], double (&mass)[3]) {
+    const float l0 = key_float(at[0]), l1 = key_float(at[1]), l2 = key_float(at[2]), top = (float)m;
+    int c[3] = {0, 0, 0};
+    double s[3] = {0.0, 0.0, 0.0};
+    each([&](const float (&x)[EPV], int, int n) {
+      bool any = false;
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) any |= x[e] >= l0;
+      if (!any) return;
+      float t[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) {
+        const bool in = e < n, b0 = in && x[e] >= l0, b1 = in && x[e] >= l1, b2 = in && x[e] >= l2;
+        c[0] += b0;
+        c[1] += b1;
+        c[2] += b2;
+        if (MASS) {
+          const float w = fast.weight(x[e] - top);
+          t[0] += b0 ? w : 0.f;
+          t[1] += b1 ? w : 0.f;
+          t[2] += b2 ? w : 0.f;
+        }
+      }
+      if (MASS) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) s[k] += (double)t[k];
+      }
+    });
+#pragma unroll
+    for (int k = 0; k < 3; ++k) count[k] = wave_sum_i32(c[k]);
+    team.template sums<3, MASS>(s, count);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) mass[k] = s[k];
+  }
+
+  // The entries with keys in [lo, hi) into sh.key, in no order; at most kList of them are there.
+  __device__ __forceinline__ void collect(uint32_t lo, uint32_t hi) {
     const float least = key_float(lo);
     if (threadIdx.x == 0) sh.n = 0;
     __syncthreads();
@@ -186,121 +276,128 @@ struct Draw {
       bool any = false;
 #pragma unroll
       for (int e = 0; e < EPV; ++e) any |= x[e] >= least;
-      if (!any || __hip_atomic_load(&sh.n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) > kList) return;
+      if (!any) return;
 #pragma unroll
       for (int e = 0; e < EPV; ++e) {
         const uint32_t k = order_key(x[e]);
-        if (e < n && k >= lo && (hi == 0 || k < hi)) {
+        if (e < n && k >= lo && k < hi) {
           const int at = atomicAdd(&sh.n, 1);
-          if (at < kList) sh.key[at] = ((uint64_t)k << 32) | (uint32_t)~(uint32_t)(v0 + e);
+          if (at < kList) sh.key[at] = ((uint64_t)k << 32) | (uint32_t)(v0 + e);
         }
       }
     });
     __syncthreads();
-    const int n = sh.n;
-    if (n <= kList) sort(n);
-    return n;
   }
 
-  // sh.key[0 .. n) descending.
-  __device__ __forceinline__ void sort(int n) {
-    const int tid = threadIdx.x;
-    if (n <= 256) {                                     // every key counts those above it (keys differ)
-      const uint64_t mine = tid < n ? sh.key[tid] : 0;
-      int rank = 0;
-      for (int j = 0; j < n; ++j) rank += sh.key[j] > mine;
-      __syncthreads();
-      if (tid < n) sh.key[rank] = mine;
-      __syncthreads();
-      return;
-    }
-    int n2 = 512;
-    while (n2 < n) n2 <<= 1;
-    for (int i = n + tid; i < n2; i += kDrawThreads) sh.key[i] = 0;
-    __syncthreads();
-    for (int k2 = 2; k2 <= n2; k2 <<= 1)
-      for (int j = k2 >> 1; j > 0; j >>= 1) {
-        const int pairs = n2 / 2;
-        for (int p = tid; p < pairs; p += kDrawThreads) {
-          const int i = 2 * p - (p & (j - 1)), o = i + j;
-          const uint64_t x = sh.key[i], y = sh.key[o];
-          if (((i & k2) == 0) == (x < y)) { sh.key[i] = y; sh.key[o] = x; }
-        }
-        __syncthreads();
-      }
-  }
-
-  __device__ __forceinline__ float list_value(int i) const { return key_float((uint32_t)(sh.key[i] >> 32)); }
-
-  // Masses down the list: sh.cum[i] = before + the weights of entries 0 .. i.
-  __device__ __forceinline__ void masses(int n, double before) {
-    const int i0 = threadIdx.x * kOwn;
-    double w[kOwn], mine = 0.0, total;
+  // Entries of a list that the threads own: keys (0: none) and weights.  The largest key c in [lo, hi) such that the entries >= c, with n_hi
+  // and mass_hi above hi, are at least K (BY_COUNT) or weigh at least `target`; lo is such a key, hi is not.
+  template <bool BY_COUNT>
+  __device__ __forceinline__ uint32_t search(const uint32_t (&vk)[kOwn], const double (&w)[kOwn], uint32_t lo, uint32_t hi, int n_hi,
+                                             double mass_hi, int K, double target) {
+    int c_lo = 0x7fffffff, c_hi = 0;                     // entries of the list >= lo, >= hi
+    while (hi - lo > kQuantum && c_lo - c_hi > 1) {
+      const uint32_t quanta = (hi - lo + kQuantum - 1) / kQuantum, step = max(quanta / 4, 1u) * kQuantum;
+      const uint32_t base = lo / kQuantum * kQuantum;    // (a bfloat16 key is told by its upper half)
+      uint32_t p[3];
+      double s[3] = {0.0, 0.0, 0.0};
+      int c[3];
 #pragma unroll
-    for (int j = 0; j < kOwn; ++j) mine += w[j] = i0 + j < n ? weight(list_value(i0 + j)) : 0.0;
-    double run = before + (block_scan(mine, &total, sh) - mine);
+      for (int k = 0; k < 3; ++k) {
+        p[k] = base + (k + 1) * step;
+        int n = 0;
 #pragma unroll
-    for (int j = 0; j < kOwn; ++j) {
-      run += w[j];
-      if (i0 + j < n) sh.cum[i0 + j] = run;
-    }
-    __syncthreads();
-  }
-
-  // First index whose mass reaches `target`, or n.
-  __device__ __forceinline__ int reach(int n, double target) {
-    if (threadIdx.x == 0) sh.hit = n;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kDrawThreads)
-      if (sh.cum[i] >= target && (i == 0 || !(sh.cum[i - 1] >= target))) atomicMin(&sh.hit, i);
-    __syncthreads();
-    return sh.hit;
-  }
-
-  // The largest key c such that the entries >= c are at least K (by_count) or weigh at least `target`; lo is such a key, hi (0: none) is
-  // not, with n_hi entries and a mass of mass_hi not below it.
-  __device__ __forceinline__ uint32_t narrow(bool by_count, int K, double target, uint32_t lo, int n_lo, uint32_t hi, int n_hi,
-                                             double mass_hi) {
-    const uint32_t top = order_key((float)m) + 1;        // above every entry
-    if (hi == 0) hi = top;
-    for (int round = 0; hi - lo > 1; ++round) {
-      if (n_lo - n_hi <= kList) {
-        const int n = list(lo, hi);
-        int i = 0;
-        if (by_count) {
-          i = K - n_hi - 1;
-        } else {
-          masses(n, mass_hi);
-          i = reach(n, target);
+        for (int j = 0; j < kOwn; ++j) {
+          const bool in = vk[j] >= p[k];
+          n += (int)__popcll(__ballot(in));
+          if (!BY_COUNT) s[k] += in ? w[j] : 0.0;
         }
-        // (not reached by rounding: the lowest)
-        const uint32_t c = (uint32_t)(sh.key[max(min(i, n - 1), 0)] >> 32);
-        __syncthreads();
-        return c;
+        c[k] = n;
       }
-      uint32_t mid = lo + (hi - lo) / 2;
-      if (round < 12) {                                  // halves of the values first, which are nearer to halves of the row
-        const float v = 0.5f * key_float(lo) + 0.5f * key_float(hi);
-        const uint32_t k = order_key(v);
-        if (v > -INFINITY && k > lo && k < hi) mid = k;
+      team.template sums<3, !BY_COUNT>(s, c);
+#pragma unroll
+      for (int k = 2; k >= 0; --k) {                     // (probes at or above hi do not count: it is not such a key)
+        if (p[k] >= hi) continue;
+        if (BY_COUNT ? n_hi + c[k] >= K : mass_hi + s[k] >= target) { lo = p[k]; c_lo = c[k]; break; }
+        hi = p[k];
+        c_hi = c[k];
       }
-      int c;
-      double s;
-      above(mid, !by_count, c, s);
-      if (by_count ? c >= K : s >= target) { lo = mid; n_lo = c; }
-      else { hi = mid; n_hi = c; mass_hi = s; }
+    }
+    if (c_lo - c_hi == 1) {                              // one entry is left
+#pragma unroll
+      for (int j = 0; j < kOwn; ++j)
+        if (vk[j] >= lo && vk[j] < hi) sh.found = vk[j];
+      __syncthreads();
+      lo = sh.found;
+      __syncthreads();
     }
     return lo;
   }
 
-  // Index of the place that holds u W among n places whose weights the threads own in order, w[j] that of place kOwn t + j; W; the mass before.
-  __device__ __forceinline__ int place_of(const double (&w)[kOwn], int n, double u, double* total, double* before) {
+  // The largest key c of the row such that the entries >= c are at least K, or weigh at least `target` (which is `top_p * all`, `all`
+  // known in fp64); lo is such a key.
+  template <bool BY_COUNT>
+  __device__ __forceinline__ uint32_t narrow(int K, double target, double all, uint32_t lo, int n_lo) {
+    uint32_t hi = order_key((float)m) + 1;               // above every entry
+    int n_hi = 0;
+    for (int round = 0; hi - lo > kQuantum; ++round) {
+      if (n_lo - n_hi <= kList) {
+        collect(lo, hi);
+        const int n = min(sh.n, kList);
+        const double over = BY_COUNT || n_hi == 0 ? 0.0 : mass_above(hi);
+        // weights in units of 2^-41 of the largest of them: sums of 2^11 are exact, in any order
+        const double unit = BY_COUNT ? 1.0 : __builtin_ldexp(1.0, max((int)__builtin_ceil(fmax(weight_log2(key_float(hi - 1)), -900.0)), -900) - 41);
+        uint32_t vk[kOwn];
+        double w[kOwn];
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) {
+          const int i = threadIdx.x + j * kDrawThreads;
+          vk[j] = i < n ? (uint32_t)(sh.key[i] >> 32) : 0u;
+          w[j] = i < n && !BY_COUNT ? __builtin_rint(weight(key_float(vk[j])) / unit) * unit : 0.0;
+        }
+        return search<BY_COUNT>(vk, w, lo, hi, n_hi, over, K, target);
+      }
+      uint32_t p[3];
+      const uint32_t quarter = max((hi - lo) / 4, 1u);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) p[k] = lo + min((k + 1) * quarter, hi - lo - 1);
+      const float f0 = key_float(lo), f1 = key_float(hi - 1);
+      if (round < 8 && f0 > -INFINITY) {                 // quarters of the values, which are nearer to quarters of the row
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          const float t = 0.25f * (k + 1);
+          const uint32_t q = order_key(f0 * (1.f - t) + f1 * t);
+          if (q > lo && q < hi) p[k] = q;
+        }
+        p[1] = max(p[1], p[0]);
+        p[2] = max(p[2], p[1]);
+      }
+      int c[3];
+      double s[3];
+      above<!BY_COUNT>(p, c, s);
+      for (int k = 2; k >= 0; --k) {
+        bool yes;
+        if (BY_COUNT) {
+          yes = c[k] >= K;
+        } else {
+          if (fabs(s[k] - target) <= kMassError * all) s[k] = mass_above(p[k]);
+          yes = s[k] >= target;
+        }
+        if (yes) { lo = p[k]; n_lo = c[k]; break; }
+        hi = p[k];
+        n_hi = c[k];
+      }
+    }
+    return lo;
+  }
+
+  // Index of the place that holds u W among places whose weights the threads own in order, w[j] that of place kOwn t + j; W; the mass before.
+  __device__ __forceinline__ int place_of(const double (&w)[kOwn], double u, double* total, double* before) {
     const int i0 = threadIdx.x * kOwn;
     double mine = 0.0, W;
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) mine += w[j];
     if (threadIdx.x == 0) { sh.hit = 0x7fffffff; sh.n = 0; }
-    const double start = block_scan(mine, &W, sh) - mine, at = u * W;
+    const double start = team.place(mine, &W), at = u * W;
     double run = start;
     int first = -1, last = -1;
 #pragma unroll
@@ -314,16 +411,16 @@ struct Draw {
     if (first >= 0) atomicMin(&sh.hit, first);
     if (last >= 0) atomicMax(&sh.n, last);
     __syncthreads();
-    const int i = sh.hit < n ? sh.hit : sh.n;            // (u W rounded up to W: the last one)
+    const int i = sh.hit < kList ? sh.hit : sh.n;        // (u W rounded up to W: the last one)
     run = start;
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
-      if (i0 + j == i) sh.out_d[0] = run;
+      if (i0 + j == i) sh.mass = run;
       run += w[j];
     }
     __syncthreads();
     *total = W;
-    *before = sh.out_d[0];
+    *before = sh.mass;
     return i;
   }
 
@@ -333,16 +430,14 @@ struct Draw {
     return k >= a.min_log2 ? exp2_series(k) : 0.0;
   }
 
-  // Weights of a piece, entry e of vector j of this lane: entries (piece * 8 + j) * 64 + lane, EPV of them.  sums[j]: of a vector.
+  // Mass of what is kept of a piece: vectors (8 piece + j) 64 + lane.
   __device__ __forceinline__ double piece_sum(int piece, float least) const {
     const int lane = threadIdx.x & (kWave - 1), nvec = a.V / EPV;
     const int64_t base = (int64_t)piece * kPieceVecs * kWave + lane;
     u32x4 q[kPieceVecs];
 #pragma unroll
-    for (int j = 0; j < kPieceVecs; ++j) {
-      const int64_t i = base + j * kWave;
-      if (i < nvec) q[j] = load_vec(row, (int)i);
-    }
+    for (int j = 0; j < kPieceVecs; ++j)
+      if (base + j * kWave < nvec) q[j] = load_vec(row, (int)(base + j * kWave));
     double s = 0.0;
 #pragma unroll
     for (int j = 0; j < kPieceVecs; ++j) {
@@ -355,7 +450,10 @@ struct Draw {
         for (int e = 0; e < EPV; ++e) any |= x[e] >= least;
         if (any) {
 #pragma unroll
-          for (int e = 0; e < EPV; ++e) s += kept_weight(x[e], least);
+          for (int e = 0; e < EPV; ++e) {
+            s += kept_weight(x[e], least);
+            if (e % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+          }
         }
       } else if (i == nvec) {                            // the entries past the last vector
         for (int v = nvec * EPV; v < a.V; ++v) s += kept_weight(load_elem<DT>(row, v), least);
@@ -366,28 +464,27 @@ struct Draw {
 
   // From all entries not below `least` (and above min-p): masses of pieces, then the entries of one.
   __device__ __forceinline__ float draw_swept(float least, double u, int* token, double* total) {
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int wave = threadIdx.x / kWave;
     const int pieces = a.V / EPV / (kPieceVecs * kWave) + 1;
-    double* mass = sh.cum;                               // (the list's places: pieces are gathered so that there are at most kList of them)
     const int group = (pieces + kList - 1) / kList;      // pieces that share a mass
     const int groups = (pieces + group - 1) / group;
-    for (int gI = wave; gI < groups; gI += kDrawWaves) {
+    for (int g = wave; g < groups; g += kDrawWaves) {
       double s = 0.0;
-      for (int p = gI * group; p < min((gI + 1) * group, pieces); ++p) s += piece_sum(p, least);
-      if (lane == 0) mass[gI] = s;
+      for (int p = g * group; p < min((g + 1) * group, pieces); ++p) s += piece_sum(p, least);
+      if ((threadIdx.x & (kWave - 1)) == 0) sh.piece[g] = s;
     }
     __syncthreads();
     double w[kOwn], W, begin;
 #pragma unroll
-    for (int j = 0; j < kOwn; ++j) w[j] = (int)threadIdx.x * kOwn + j < groups ? mass[threadIdx.x * kOwn + j] : 0.0;
-    const int gI = place_of(w, groups, u, &W, &begin);
-    *token = in_pieces(gI * group, min((gI + 1) * group, pieces), begin, u * W, least);
+    for (int j = 0; j < kOwn; ++j) w[j] = (int)threadIdx.x * kOwn + j < groups ? sh.piece[threadIdx.x * kOwn + j] : 0.0;
+    const int g = place_of(w, u, &W, &begin);
+    *token = in_pieces(g * group, min((g + 1) * group, pieces), begin, u * W, least);
     *total = W;
     return load_elem<DT>(row, *token);
   }
 
   // The token at which the running mass, `before` ahead of piece p0, passes `at`, among pieces p0 .. p1 - 1; if it does not, the last kept one.
-  // A wavefront for each vector of 64 lanes, eight of them at a time.
+  // A wavefront for each of a piece's eight vectors of 64 lanes.
   __device__ __forceinline__ int in_pieces(int p0, int p1, double before, double at, float least) {
     static_assert(kPieceVecs == kDrawWaves, "a wavefront for each vector of a piece");
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, nvec = a.V / EPV;
@@ -406,18 +503,13 @@ struct Draw {
           if (i * EPV + e < a.V) x[e] = load_elem<DT>(row, (int)(i * EPV + e));
       }
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) s += w[e] = kept_weight(x[e], least);
-      const double incl = wave_scan_f64(s);
-      if (lane == kWave - 1) sh.wave_d[wave] = incl;
-      if (threadIdx.x == 0) { sh.hit = 0x7fffffff; sh.n = -1; }
-      __syncthreads();
-      double run = before, all = before;
-#pragma unroll
-      for (int k = 0; k < kDrawWaves; ++k) {
-        if (k == wave) run = all;
-        all += sh.wave_d[k];
+      for (int e = 0; e < EPV; ++e) {
+        s += w[e] = kept_weight(x[e], least);
+        if (e % 2 == 1) __builtin_amdgcn_sched_barrier(0);
       }
-      run += incl - s;
+      if (threadIdx.x == 0) { sh.hit = 0x7fffffff; sh.n = -1; }
+      double all;
+      double run = before + team.place(s, &all);
       int first = -1, last = -1;
 #pragma unroll
       for (int e = 0; e < EPV; ++e) {
@@ -432,40 +524,12 @@ struct Draw {
       __syncthreads();
       if (sh.hit != 0x7fffffff) return sh.hit;
       if (sh.n >= 0) last_seen = sh.n;
-      before = all;
+      before += all;
       __syncthreads();
     }
     return last_seen;
   }
 };
-// Sum over the workgroup of a small count (at most 2^16 a wavefront); slots alternate, so that one barrier is enough.
-__device__ __forceinline__ int block_count(int c, int& turn, DrawShared& sh) {
-  // c: the wavefront's own, the same in its lanes
-  if ((threadIdx.x & (kWave - 1)) == 0) sh.count[turn][threadIdx.x / kWave] = c;
-  __syncthreads();
-  int all = 0;
-#pragma unroll
-  for (int w = 0; w < kDrawWaves; ++w) all += sh.count[turn][w];
-  turn ^= 1;
-  return all;
-}
-__device__ __forceinline__ int wave_sum_i32(int c) { return __builtin_amdgcn_readlane(wave_scan_i32(c), kWave - 1); }
-
-// Exclusive place of a thread's c items in the order of the threads; their number in every thread.
-__device__ __forceinline__ int block_place(int c, int* total, DrawShared& sh) {
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, incl = wave_scan_i32(c);
-  if (lane == kWave - 1) sh.wave_i[wave] = incl;
-  __syncthreads();
-  int before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kDrawWaves; ++w) {
-    if (w == wave) before = all;
-    all += sh.wave_i[w];
-  }
-  __syncthreads();
-  *total = all;
-  return before + incl - c;
-}
 
 template <int DT>
 __device__ __forceinline__ void bad_row_out(const SampleArgs& a, int64_t r) {
@@ -477,22 +541,23 @@ __device__ __forceinline__ void bad_row_out(const SampleArgs& a, int64_t r) {
 
 // No warps: a piece of the row for each wavefront in turn, weights relative to the piece's largest entry; one pass over the row.
 template <int DT>
-__global__ void __launch_bounds__(kDrawThreads) sample_plain_kernel(SampleArgs a) {
+__global__ void __launch_bounds__(kDrawThreads, 4) sample_plain_kernel(SampleArgs a) {
   constexpr int EPV = Elem<DT>::per_vec;
   __shared__ DrawShared sh;
   __shared__ float piece_top[kList];
   const int64_t r = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-  Draw<DT> d{a, a.z + r * a.z_stride, sh, 0.0};
+  Team team{sh};
+  Draw<DT> d{a, a.z + r * a.z_stride, sh, team, 0.0, {0.f, 0.f}};
   double u = a.u[r];
   const int nvec = a.V / EPV, pieces = nvec / (kPieceVecs * kWave) + 1;
   const int group = (pieces + kList - 1) / kList, groups = (pieces + group - 1) / group;
   bool nan = false;
   float row_top = -INFINITY;
-  for (int gI = wave; gI < groups; gI += kDrawWaves) {
+  for (int g = wave; g < groups; g += kDrawWaves) {
     float ref = -INFINITY;
     double sum = 0.0;
-    for (int p = gI * group; p < min((gI + 1) * group, pieces); ++p) {
+    for (int p = g * group; p < min((g + 1) * group, pieces); ++p) {
       const int64_t base = (int64_t)p * kPieceVecs * kWave + lane;
       u32x4 q[kPieceVecs];
 #pragma unroll
@@ -518,6 +583,7 @@ __global__ void __launch_bounds__(kDrawThreads) sample_plain_kernel(SampleArgs a
           nan |= v != v;
           top = fmaxf(top, v);
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
       top = wave_max_f32(top);
       if (top == -INFINITY) continue;
@@ -534,7 +600,10 @@ __global__ void __launch_bounds__(kDrawThreads) sample_plain_kernel(SampleArgs a
         float x[EPV];
         unpack<DT>(q[j], x);
 #pragma unroll
-        for (int e = 0; e < EPV; ++e) s += d.weight(x[e]);
+        for (int e = 0; e < EPV; ++e) {
+          s += d.weight(x[e]);
+          if (e % 2 == 1) __builtin_amdgcn_sched_barrier(0);   // (two weights side by side)
+        }
       }
       if (base <= nvec && nvec < base + kPieceVecs * kWave && (nvec - base) % kWave == 0) {
 #pragma unroll
@@ -542,15 +611,15 @@ __global__ void __launch_bounds__(kDrawThreads) sample_plain_kernel(SampleArgs a
       }
       sum += wave_sum_f64(s);
     }
-    if (lane == 0) { sh.cum[gI] = sum; piece_top[gI] = ref; }
+    if (lane == 0) { sh.piece[g] = sum; piece_top[g] = ref; }
     row_top = fmaxf(row_top, ref);
   }
   if (__ballot(nan)) row_top = INFINITY;
-  if (lane == 0) sh.wave_u[wave] = __float_as_uint(row_top);
+  if (lane == 0) sh.wave_top[wave] = row_top;
   __syncthreads();
   float top = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < kDrawWaves; ++w) top = fmaxf(top, __uint_as_float(sh.wave_u[w]));
+  for (int w = 0; w < kDrawWaves; ++w) top = fmaxf(top, sh.wave_top[w]);
   const double y = (double)top * a.scale;
   if (!(y >= (double)kRefFloor && y <= (double)kRefCeil) || u != u) return bad_row_out<DT>(a, r);
   u = fmin(fmax(u, 0.0), 1.0 - 0x1p-53);
@@ -559,10 +628,10 @@ __global__ void __launch_bounds__(kDrawThreads) sample_plain_kernel(SampleArgs a
 #pragma unroll
   for (int j = 0; j < kOwn; ++j) {
     const int i = tid * kOwn + j;
-    w[j] = i < groups && sh.cum[i] > 0.0 ? sh.cum[i] * d.weight(piece_top[i]) : 0.0;
+    w[j] = i < groups && sh.piece[i] > 0.0 ? sh.piece[i] * d.weight(piece_top[i]) : 0.0;
   }
-  const int gI = d.place_of(w, groups, u, &W, &begin);
-  const int token = d.in_pieces(gI * group, min((gI + 1) * group, pieces), begin, u * W, -INFINITY);
+  const int g = d.place_of(w, u, &W, &begin);
+  const int token = d.in_pieces(g * group, min((g + 1) * group, pieces), begin, u * W, -INFINITY);
   if (tid == 0) {
     a.token[r] = token;
     if (a.logprob) a.logprob[r] = (float)(((double)load_elem<DT>(d.row, token) - d.m) * a.inv_t - log(W));
@@ -570,29 +639,19 @@ __global__ void __launch_bounds__(kDrawThreads) sample_plain_kernel(SampleArgs a
   }
 }
 
-// Weight in float32 of an entry `below` (<= 0) the largest one: L_hi + L_lo is the scale.
-struct FastScale {
-  float hi, lo;
-  __device__ __forceinline__ float weight(float below) const {
-    const float b = fmaxf(below, -1e30f);                // (-inf times lo is no -inf)
-    return exp2_fast(__builtin_fmaf(b, hi, b * lo));
-  }
-};
-
 template <int DT>
-__global__ void __launch_bounds__(kDrawThreads) sample_kernel(SampleArgs a) {
+__global__ void __launch_bounds__(kDrawThreads, 4) sample_kernel(SampleArgs a) {
   constexpr int EPV = Elem<DT>::per_vec;
   __shared__ DrawShared sh;
-  extern __shared__ uint16_t vec_key[];                  // [n_keys rounded up to 8]
+  extern __shared__ __align__(16) uint16_t vec_key[];                // [n_keys rounded up to 8]
   const int64_t r = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-  Draw<DT> d{a, a.z + r * a.z_stride, sh, 0.0};
+  Team team{sh};
+  Draw<DT> d{a, a.z + r * a.z_stride, sh, team, 0.0, {(float)a.scale, (float)(a.scale - (double)(float)a.scale)}};
   const bool use_k = a.top_k > 0, use_p = a.top_p < 1.0, use_min = a.min_log2 > -INFINITY;
   const int nvec = a.V / EPV, n_all = nvec + (a.V > nvec * EPV);   // the last one may be a part of a vector
   const int n_keys = (n_all + a.share - 1) / a.share;
-  int turn = 0;
   double u = a.u[r];
-  const FastScale fast{(float)a.scale, (float)(a.scale - (double)(float)a.scale)};
 
   // sweep: maxima of vectors, of the lane and the row; the row's mass relative to the lane's maximum
   float mine = -INFINITY;
@@ -607,56 +666,51 @@ __global__ void __launch_bounds__(kDrawThreads) sample_kernel(SampleArgs a) {
       for (int e = 0; e < EPV; ++e) x[e] = i * EPV + e < a.V ? load_elem<DT>(d.row, i * EPV + e) : -INFINITY;
     }
   };
-  auto take = [&](const float (&x)[EPV], float top) {    // (top: of these entries)
-    if (!weigh) return;
-    const float m = fmaxf(mine, top);
-    if (m == -INFINITY) return;
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < EPV; e += 2) s += fast.weight(x[e] - m) + fast.weight(x[e + 1] - m);
-    if (m > mine) mass *= mine == -INFINITY ? 0.0 : (double)fast.weight(mine - m);
-    mass += (double)s;
-  };
-  auto top_in = [&](const float (&x)[EPV]) {
+  auto take = [&](const float (&x)[EPV]) {               // the largest of a vector's entries
     float t = x[0];
 #pragma unroll
     for (int e = 1; e < EPV; ++e) t = fmaxf(t, x[e]);
 #pragma unroll
     for (int e = 0; e < EPV; ++e) nan |= x[e] != x[e];
+    const float m = fmaxf(mine, t);
+    if (weigh && m > -INFINITY) {
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < EPV; e += 2) s += d.fast.weight(x[e] - m) + d.fast.weight(x[e + 1] - m);
+      if (m > mine) mass *= mine == -INFINITY ? 0.0 : (double)d.fast.weight(mine - m);
+      mass += (double)s;
+    }
+    mine = m;
     return t;
   };
   if (a.share == 1) {
-    constexpr int U = 8;
-    int i = tid;
-    for (; i + (U - 1) * kDrawThreads < nvec; i += U * kDrawThreads) {
-      u32x4 q[U];
+    // five vectors under way while the five before them are looked at
+    constexpr int U = 5, kRound = U * kDrawThreads;
+    auto load = [&](int i, u32x4 (&q)[U]) {
 #pragma unroll
-      for (int k = 0; k < U; ++k) q[k] = load_vec(d.row, i + k * kDrawThreads);
+      for (int k = 0; k < U; ++k)
+        if (i + k * kDrawThreads < nvec) q[k] = load_vec(d.row, i + k * kDrawThreads);
+    };
+    auto look = [&](int i, const u32x4 (&q)[U]) {
 #pragma unroll
       for (int k = 0; k < U; ++k) {
+        const int at = i + k * kDrawThreads;
+        if (at >= n_all) continue;
         float x[EPV];
-        unpack<DT>(q[k], x);
-        const float t = top_in(x);
-        take(x, t);
-        mine = fmaxf(mine, t);
-        vec_key[i + k * kDrawThreads] = (uint16_t)(order_key(t) >> 16);
+        if (at < nvec) unpack<DT>(q[k], x);
+        else vector_at(at, x);
+        vec_key[at] = (uint16_t)(order_key(take(x)) >> 16);
+        __builtin_amdgcn_sched_barrier(0);               // (one at a time: their weights side by side take the registers of two more rows)
       }
-    }
-    u32x4 q[U];                                          // what is left, all of it under way together
-#pragma unroll
-    for (int k = 0; k < U; ++k)
-      if (i + k * kDrawThreads < nvec) q[k] = load_vec(d.row, i + k * kDrawThreads);
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-      const int at = i + k * kDrawThreads;
-      if (at >= n_all) continue;
-      float x[EPV];
-      if (at < nvec) unpack<DT>(q[k], x);
-      else vector_at(at, x);
-      const float t = top_in(x);
-      take(x, t);
-      mine = fmaxf(mine, t);
-      vec_key[at] = (uint16_t)(order_key(t) >> 16);
+    };
+    u32x4 q0[U], q1[U];
+    load(tid, q0);
+    for (int i = tid; i < n_all; i += 2 * kRound) {
+      load(i + kRound, q1);
+      look(i, q0);
+      if (i + kRound >= n_all) break;
+      load(i + 2 * kRound, q0);
+      look(i + kRound, q1);
     }
   } else {
     for (int k = tid; k < n_keys; k += kDrawThreads) {
@@ -664,21 +718,18 @@ __global__ void __launch_bounds__(kDrawThreads) sample_kernel(SampleArgs a) {
       for (int i = k * a.share; i < min((k + 1) * a.share, n_all); ++i) {
         float x[EPV];
         vector_at(i, x);
-        const float t = top_in(x);
-        take(x, t);
-        mine = fmaxf(mine, t);
-        all = fmaxf(all, t);
+        all = fmaxf(all, take(x));
       }
       vec_key[k] = (uint16_t)(order_key(all) >> 16);
     }
   }
   for (int k = n_keys + tid; k < ((n_keys + 7) & ~7); k += kDrawThreads) vec_key[k] = 0;
-  const uint32_t lane_key = order_key(mine) >> 16;
+  sh.lane_key[tid] = (uint16_t)(order_key(mine) >> 16);
   {
     const float hi = wave_max_f32(nan ? INFINITY : mine), lo = -wave_max_f32(-mine);
     if (lane == 0) {
-      sh.wave_u[wave] = __float_as_uint(hi);
-      sh.count[0][wave] = (int)(order_key(lo) >> 16);
+      sh.wave_top[wave] = __ballot(nan) ? INFINITY : hi;
+      sh.wave_low[wave] = order_key(lo) >> 16;
     }
   }
   __syncthreads();
@@ -686,10 +737,9 @@ __global__ void __launch_bounds__(kDrawThreads) sample_kernel(SampleArgs a) {
   uint32_t low_key = 0xffffu;
 #pragma unroll
   for (int w = 0; w < kDrawWaves; ++w) {
-    top = fmaxf(top, __uint_as_float(sh.wave_u[w]));
-    low_key = min(low_key, (uint32_t)sh.count[0][w]);
+    top = fmaxf(top, sh.wave_top[w]);
+    low_key = min(low_key, sh.wave_low[w]);
   }
-  turn = 1;                                              // (slot 0 may still be read)
   const double y = (double)top * a.scale;
   if (!(y >= (double)kRefFloor && y <= (double)kRefCeil) || u != u) return bad_row_out<DT>(a, r);
   u = fmin(fmax(u, 0.0), 1.0 - 0x1p-53);
@@ -698,19 +748,16 @@ __global__ void __launch_bounds__(kDrawThreads) sample_kernel(SampleArgs a) {
   double all = 0.0;                                      // the row's mass
   bool exact = true;
   if (weigh) {
-    all = mine == -INFINITY ? 0.0 : mass * (double)fast.weight(mine - top);
-    int zero = 0;
-    block_sums(all, zero, sh);
+    all = team.sum(mine == -INFINITY ? 0.0 : mass * (double)d.fast.weight(mine - top));
     exact = false;
   }
   auto make_exact = [&]() {
-    if (exact) return;
-    int count;
-    d.above(none, true, count, all);
+    if (!exact) all = d.mass_above(none);
     exact = true;
   };
 
-  // The largest sixteen-bit key that at least `want` of the keys counted by count(probe) reach; `from` to `to` hold it.
+  // A sixteen-bit key that at least `want` of the keys counted by count(probe) reach, and few more than that if there is such a one; the keys
+  // lie between `from`, which `want` of them reach, and `to`.
   auto select = [&](uint32_t from, uint32_t to, int want, auto&& count) {
     const uint32_t differ = from ^ to;
     if (differ == 0) return from;
@@ -718,11 +765,12 @@ __global__ void __launch_bounds__(kDrawThreads) sample_kernel(SampleArgs a) {
     uint32_t t = from & ~((2u << bit) - 1u);
     for (; bit >= 0; --bit) {
       const uint32_t probe = t | (1u << bit);
-      if (block_count(count(probe), turn, sh) >= want) t = probe;
+      const int c = count(probe);
+      if (c >= want) t = probe;
+      if (c >= want && c <= want + want / 4) break;
     }
     return t;
   };
-  auto lanes_at = [&](uint32_t probe) { return (int)__popcll(__ballot(lane_key >= probe)); };
   const int own = ((n_keys + kDrawThreads * 8 - 1) / (kDrawThreads * 8)) * 8;    // keys of a thread, in order
   auto each_key = [&](auto&& f) {                        // f(key, index) of the thread's keys, eight of them loaded at a time
     for (int k = tid * own; k < min((tid + 1) * own, n_keys); k += 8) {
@@ -730,11 +778,6 @@ __global__ void __launch_bounds__(kDrawThreads) sample_kernel(SampleArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) f((q[e / 2] >> (16 * (e % 2))) & 0xffffu, k + e);
     }
-  };
-  auto vectors_at = [&](uint32_t probe) {
-    int c = 0;
-    each_key([&](uint32_t key, int) { c += key >= probe; });
-    return wave_sum_i32(c);
   };
   uint32_t min_key = none;
   if (use_min) {
@@ -753,27 +796,48 @@ __global__ void __launch_bounds__(kDrawThreads) sample_kernel(SampleArgs a) {
     if (attempt > 0) want = a.V <= kList ? 0 : min(kDeepRank, (n_keys * 2 + 2) / 3);
     uint32_t tau = none;
     if (want > 0 && want <= kDrawThreads && attempt == 0) {
-      tau = select(low_key, top_key, want, lanes_at) << 16;
+      // every wavefront by itself, eight of the lanes' maxima in a lane
+      const u32x4 q = *reinterpret_cast<const u32x4*>(sh.lane_key + 8 * lane);
+      tau = select(low_key, top_key, want, [&](uint32_t probe) {
+        int c = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) c += (int)__popcll(__ballot(((q[e / 2] >> (16 * (e % 2))) & 0xffffu) >= probe));
+        return c;
+      }) << 16;
+      if (weigh && tau > min_key) {
+        // a nucleus that the lanes' maxima above tau are far from filling is deeper than their list
+        const double reached = team.sum((uint32_t)sh.lane_key[tid] >= (tau >> 16) ? (double)d.fast.weight(mine - top) : 0.0);
+        if (reached < 0.7 * a.top_p * all) continue;
+      }
     } else if (want > 0 && want <= n_keys) {
-      tau = select(0, top_key, want, vectors_at) << 16;
+      tau = select(0, top_key, want, [&](uint32_t probe) {
+        int c = 0;
+        each_key([&](uint32_t key, int) { c += key >= probe; });
+        return team.count(wave_sum_i32(c));
+      }) << 16;
     }
     tau = max(tau, none);
     if (!use_k) tau = max(tau, min_key);                 // (the K-th value may lie below what min-p keeps)
     if (use_k && want > n_keys) break;
     // the vectors that reach it, in order
     int c = 0, n_vec, n;
-    each_key([&](uint32_t key, int k) {
-      if (key >= (tau >> 16) && k < n_keys) c += min(a.share, n_all - k * a.share);
-    });
-    int at = block_place(c, &n_vec, sh);
+    each_key([&](uint32_t key, int k) { c += key >= (tau >> 16) && k < n_keys; });
+    if (a.share > 1) {
+      c = 0;
+      each_key([&](uint32_t key, int k) {
+        if (key >= (tau >> 16) && k < n_keys) c += min(a.share, n_all - k * a.share);
+      });
+    }
+    int at = team.place(c, &n_vec);
     if (n_vec > kList) break;
-    each_key([&](uint32_t key, int k) {
-      if (key >= (tau >> 16) && k < n_keys)
-        for (int i = k * a.share; i < min((k + 1) * a.share, n_all); ++i) sh.vec[at++] = (uint32_t)i;
-    });
+    if (c > 0)
+      each_key([&](uint32_t key, int k) {
+        if (key >= (tau >> 16) && k < n_keys)
+          for (int i = k * a.share; i < min((k + 1) * a.share, n_all); ++i) sh.vec[at++] = (uint32_t)i;
+      });
     __syncthreads();
     // their entries
-    float x[kOwn][EPV];
+    u32x4 q[kOwn];
     int v0[kOwn];
     const float least = key_float(tau);
     const int per = (n_vec + kDrawThreads - 1) / kDrawThreads;   // vectors of a thread
@@ -784,31 +848,38 @@ __global__ void __launch_bounds__(kDrawThreads) sample_kernel(SampleArgs a) {
       v0[j] = j < per && i < n_vec ? (int)sh.vec[i] : -1;
     }
 #pragma unroll
-    for (int j = 0; j < kOwn; ++j) {
-      if (v0[j] < 0) continue;
-      vector_at(v0[j], x[j]);
-    }
+    for (int j = 0; j < kOwn; ++j)
+      if (v0[j] >= 0 && v0[j] < nvec) q[j] = load_vec(d.row, v0[j]);
+    auto entries = [&](int j, float (&x)[EPV]) {
+      if (v0[j] < nvec) unpack<DT>(q[j], x);
+      else vector_at(v0[j], x);
+    };
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) {
       if (v0[j] < 0) continue;
+      float x[EPV];
+      entries(j, x);
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) c += x[j][e] >= least && v0[j] * EPV + e < a.V;
+      for (int e = 0; e < EPV; ++e) c += x[e] >= least && v0[j] * EPV + e < a.V;
     }
-    at = block_place(c, &n, sh);
+    at = team.place(c, &n);
     if (n > kList) break;
+    if (c > 0) {
 #pragma unroll
-    for (int j = 0; j < kOwn; ++j) {
-      if (v0[j] < 0) continue;
+      for (int j = 0; j < kOwn; ++j) {
+        if (v0[j] < 0) continue;
+        float x[EPV];
+        entries(j, x);
 #pragma unroll
-      for (int e = 0; e < EPV; ++e)
-        if (x[j][e] >= least && v0[j] * EPV + e < a.V)
-          sh.key[at++] = ((uint64_t)order_key(x[j][e]) << 32) | (uint32_t)(v0[j] * EPV + e);
+        for (int e = 0; e < EPV; ++e)
+          if (x[e] >= least && v0[j] * EPV + e < a.V) sh.key[at++] = ((uint64_t)order_key(x[e]) << 32) | (uint32_t)(v0[j] * EPV + e);
+      }
     }
     __syncthreads();
     if (use_k && n < a.top_k) break;
     const bool whole_min = use_min && tau <= min_key;    // the list holds all that min-p keeps
     if (n <= kWave) {
-      // one wavefront, a lane for each entry, by ascending token.  out_i[0]: 0 settled, 1 does not reach, 2 too near a decision
+      // one wavefront, a lane for each entry, by ascending token.  state: 0 settled, 1 does not reach, 2 too near a decision
       for (int pass = 0; pass < 2; ++pass) {
         if (wave == 0) {
           const uint64_t key = lane < n ? sh.key[lane] : 0;
@@ -818,24 +889,29 @@ __global__ void __launch_bounds__(kDrawThreads) sample_kernel(SampleArgs a) {
           double w = lane < n ? exp2_series(k2) : 0.0;
           bool keep = lane < n;
           int state = 0;
+          const int n4 = (n + 3) & ~3;                   // (lanes without an entry have key and weight 0)
           if (use_k) {
             int above = 0;                               // entries of a larger value
-            for (int j = 0; j < n; ++j) above += (uint32_t)__builtin_amdgcn_readlane(vk, j) > vk;
+            for (int j = 0; j < n4; j += 4) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) above += (uint32_t)__builtin_amdgcn_readlane(vk, j + e) > vk;
+            }
             keep = keep && above < a.top_k;
           }
           if (use_p) {
             if (!keep) w = 0.0;
-            double above = 0.0, sum = 0.0;               // masses of larger values, of all
-            for (int j = 0; j < n; ++j) {
-              const double wj = lane_f64(w, j);
-              sum += wj;
-              above += (uint32_t)__builtin_amdgcn_readlane(vk, j) > vk ? wj : 0.0;
+            double above[2] = {0.0, 0.0};                // masses of larger values
+            const double sum = wave_sum_f64(w);
+            for (int j = 0; j < n4; j += 4) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) above[e & 1] += (uint32_t)__builtin_amdgcn_readlane(vk, j + e) > vk ? lane_f64(w, j + e) : 0.0;
             }
+            above[0] += above[1];
             const double target = a.top_p * (use_k ? sum : all);
             const double band = use_k || exact ? 0.0 : kMassError * all;
-            if (__ballot(keep && fabs(above - target) < band) || fabs(sum - target) < band) state = 2;
+            if (__ballot(keep && fabs(above[0] - target) < band) || fabs(sum - target) < band) state = 2;
             else if (!(sum >= target) && !use_k && !whole_min) state = 1;
-            keep = keep && above < target;
+            keep = keep && above[0] < target;
           } else if (!use_k && !whole_min) {
             state = 1;
           }
@@ -845,25 +921,24 @@ __global__ void __launch_bounds__(kDrawThreads) sample_kernel(SampleArgs a) {
           const uint64_t hits = __ballot(w > 0.0 && incl > u * total), any = __ballot(w > 0.0);
           const int i = hits ? __builtin_ctzll(hits) : 63 - __builtin_clzll(any);
           if (lane == i) {
-            sh.out_i[1] = (int)(uint32_t)key;
-            sh.out_d[1] = (double)v;
+            sh.token = (int)(uint32_t)key;
+            sh.value = (double)v;
           }
-          if (lane == 0) { sh.out_i[0] = state; sh.out_d[0] = total; }
+          if (lane == 0) { sh.state = state; sh.mass = total; }
         }
         __syncthreads();
-        const int state = sh.out_i[0];
+        const int state = sh.state;
         if (state == 0) {
-          token = sh.out_i[1];
-          z = (float)sh.out_d[1];
-          W = sh.out_d[0];
+          token = sh.token;
+          z = (float)sh.value;
+          W = sh.mass;
           done = true;
         }
-        __syncthreads();
         if (state != 2) break;
-        make_exact();
+        make_exact();                                    // (its barrier lets all read the state first)
       }
     } else {
-      // the workgroup, kOwn entries a thread, by ascending token
+      // the workgroup, up to kOwn entries a thread, by ascending token
       uint32_t vk[kOwn];
       double w[kOwn];
       const int per_n = (n + kDrawThreads - 1) / kDrawThreads;
@@ -874,50 +949,28 @@ __global__ void __launch_bounds__(kDrawThreads) sample_kernel(SampleArgs a) {
         vk[j] = in ? (uint32_t)(sh.key[i] >> 32) : 0u;
         w[j] = in ? d.weight(key_float(vk[j])) : 0.0;
       }
-      const uint32_t top32 = order_key(top);
-      // the largest key that satisfies f; the lower half of a bfloat16 key says nothing
-      constexpr int stop = DT == DT_BF16 ? 16 : 0;
-      auto search = [&](uint32_t from, auto&& f) {
-        const uint32_t differ = from ^ top32;
-        if (differ == 0) return from;
-        int bit = 31 - __builtin_clz(differ);
-        uint32_t t = from & ~((2u << bit) - 1u);
-        for (; bit >= stop; --bit) {
-          const uint32_t probe = t | (1u << bit);
-          if (f(probe)) t = probe;
-        }
-        return t;
-      };
+      const uint32_t past = order_key(top) + 1;
       auto mass_at = [&](uint32_t probe) {
         double s = 0.0;
-        int c2 = 0;
 #pragma unroll
         for (int j = 0; j < kOwn; ++j) s += vk[j] >= probe ? w[j] : 0.0;
-        block_sums(s, c2, sh);
-        return s;
+        return team.sum(s);
       };
       uint32_t cut = tau;
-      if (use_k)
-        cut = search(tau, [&](uint32_t probe) {
-          int c2 = 0;
-#pragma unroll
-          for (int j = 0; j < kOwn; ++j) c2 += (int)__popcll(__ballot(vk[j] >= probe));
-          return block_count(c2, turn, sh) >= a.top_k;
-        });
+      if (use_k) cut = d.template search<true>(vk, w, tau, past, 0, 0.0, a.top_k, 0.0);
       bool settled = use_k || use_p || whole_min;
       if (use_p) {
-        const double listed = mass_at(use_k ? cut : 1u);
+        const double listed = mass_at(cut);
         if (use_k) all = listed;
-        if (!use_k && !exact && fabs(listed - a.top_p * all) < kMassError * all) make_exact();
+        if (!exact && fabs(listed - a.top_p * all) < kMassError * all) make_exact();
         if (listed >= a.top_p * all) {
           const uint32_t kth = cut;
-          auto nearest = [&](double target) { return search(kth, [&](uint32_t probe) { return mass_at(probe) >= target; }); };
-          cut = max(nearest(a.top_p * all), kth);
-          if (!use_k && !exact) {
-            const double at_cut = mass_at(cut), over = mass_at(cut + (1u << stop)), target = a.top_p * all;
+          cut = d.template search<false>(vk, w, kth, past, 0, 0.0, 0, a.top_p * all);
+          if (!exact) {
+            const double at_cut = mass_at(cut), over = mass_at(cut / Draw<DT>::kQuantum * Draw<DT>::kQuantum + Draw<DT>::kQuantum), target = a.top_p * all;
             if (at_cut - target < kMassError * all || target - over < kMassError * all) {
               make_exact();
-              cut = max(nearest(a.top_p * all), kth);
+              cut = d.template search<false>(vk, w, kth, past, 0, 0.0, 0, a.top_p * all);
             }
           }
         } else {
@@ -928,27 +981,26 @@ __global__ void __launch_bounds__(kDrawThreads) sample_kernel(SampleArgs a) {
         double kept[kOwn], before;
 #pragma unroll
         for (int j = 0; j < kOwn; ++j) kept[j] = vk[j] >= cut && w[j] > 0.0 && d.weight_log2(key_float(vk[j])) >= a.min_log2 ? w[j] : 0.0;
-        // (place_of counts places of kOwn a thread; threads own per_n of them)
-        const int i = d.place_of(kept, kList, u, &W, &before);
+        // (place_of counts kOwn places a thread; threads own per_n entries)
+        const int i = d.place_of(kept, u, &W, &before);
         const uint64_t key = sh.key[(i / kOwn) * per_n + i % kOwn];
         token = (int)(uint32_t)key;
         z = key_float((uint32_t)(key >> 32));
         done = true;
-        __syncthreads();
       }
     }
     if (use_k || !use_p) break;
   }
   if (!done) {
+    __syncthreads();
     uint32_t least = none;                               // keys below it are dropped
-    int count = a.V;
     if (use_k) {
-      least = d.narrow(true, a.top_k, 0.0, none, a.V, 0, 0, 0.0);
-      if (use_p) d.above(least, true, count, all);
+      least = d.template narrow<true>(a.top_k, 0.0, 0.0, none, a.V);
+      if (use_p) all = d.mass_above(least);
     } else if (use_p) {
       make_exact();
     }
-    if (use_p) least = d.narrow(false, 0, a.top_p * all, least, count, 0, 0, 0.0);
+    if (use_p) least = d.template narrow<false>(0, a.top_p * all, all, least, a.V);
     z = d.draw_swept(key_float(least), u, &token, &W);
   }
   if (tid == 0) {
