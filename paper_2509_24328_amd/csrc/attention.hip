@@ -71,25 +71,18 @@ __global__ void __launch_bounds__(256) attention_flags_kernel(AttnArgs a, uint32
 }
 
 struct AttnPlan {
-  int nt, wr, tile_rows, tiles, splits;
+  int nt, tile_rows, tiles, splits;
   int64_t items;
   size_t bytes;
 };
 
-// How the rows of a call are laid out over workgroups.  Up to 16 rows a head and sequence: one block of them, the keys interleaved over
-// the four wavefronts; up to 32: two blocks; up to 64: two wavefronts with rows of their own; beyond, four.
-inline AttnPlan attention_plan(int B, int P, int Hq, int heads, int D, int dtype, bool whole, int64_t max_tokens) {
+// How the rows of a call are laid out over workgroups: one block of up to 16 or 32 rows to a wavefront, up to four of them.
+inline AttnPlan attention_plan(int B, int P, int Hq, int heads, int D, int dtype, int64_t max_tokens) {
   AttnPlan p{};
   const int64_t rows = (int64_t)P * (Hq / heads);
-  const bool wide = dtype == SV_F32 || D > 128;             // (one block of rows a wavefront)
-  p.nt = wide ? 1 : 2;
-  if (rows <= 16) { p.nt = 1; p.wr = 1; }
-  else if (!whole) p.wr = 4;
-  else if (rows <= 16 * p.nt) p.wr = 1;
-  else if (rows <= 32 * p.nt) p.wr = 2;
-  else p.wr = 4;
-  if (!whole && p.wr == 1) p.nt = 1;
-  p.tile_rows = 16 * p.nt * p.wr;
+  const bool wide = dtype == SV_F32 || D > 128;             // (outputs of one block of rows fill a wavefront's registers)
+  p.nt = wide || rows <= 16 ? 1 : 2;
+  p.tile_rows = 16 * p.nt * (rows <= 16 * p.nt ? 1 : (rows <= 32 * p.nt ? 2 : 4));
   const int64_t tiles = (rows + p.tile_rows - 1) / p.tile_rows;
   p.items = (int64_t)B * heads * tiles;
   p.tiles = (int)tiles;
@@ -116,7 +109,7 @@ extern "C" size_t sv_chunk_attention_workspace_bytes(int B, int P, int Hq, int h
   if (B < 1 || P < 1 || heads < 1 || Hq < heads || Hq % heads != 0 || Hq > SV_HEADS_MAX || D < 8 || D > SV_ATTENTION_HEAD_MAX || D % 8 != 0 ||
       elem_bytes(dtype) == 0 || max_pages < 1 || page < 1 || page > SV_PAGE_MAX || (long long)B * P > kMaxRows / Hq)
     return 0;
-  return attention_plan(B, P, Hq, heads, D, dtype, whole_tiles(D, page), (int64_t)max_pages * page).bytes;
+  return attention_plan(B, P, Hq, heads, D, dtype, (int64_t)max_pages * page).bytes;
 }
 
 extern "C" int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t* t_offsets_or_null, int n_rows,
@@ -148,7 +141,7 @@ extern "C" int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t
                  (!f8 || (is_aligned(k_scale_or_null, 4) && is_aligned(v_scale_or_null, 4))),
              SV_ERR_ALIGN);
   const bool whole = whole_tiles(D, page);
-  AttnPlan p = attention_plan(B, P, Hq, heads, D, dtype, whole, (int64_t)max_pages * page);
+  AttnPlan p = attention_plan(B, P, Hq, heads, D, dtype, (int64_t)max_pages * page);
   if (!ws_or_null) p.splits = 1;
   else if (p.splits > 1) SV_REQUIRE(is_aligned(ws_or_null, kWsAlign) && ws_bytes >= p.bytes, SV_ERR_WORKSPACE);
   SV_REQUIRE(p.items * p.splits <= 0xffffffffLL / (kAttnWaves * kWave), SV_ERR_TOO_LARGE);
@@ -182,7 +175,7 @@ extern "C" int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t
     w += ws_round((size_t)p.items * p.splits * p.tile_rows * 8);
     a.part_o = reinterpret_cast<float*>(w);
   }
-  const AttnLaunch t{p.nt, p.wr, whole, (unsigned)(p.items * p.splits), as_stream(stream)};
+  const AttnLaunch t{p.nt, whole, (unsigned)(p.items * p.splits), as_stream(stream)};
   if (dtype == SV_F32) {
     if (f8) launch_attention_f32_f8(a, t); else launch_attention_f32(a, t);
   } else {

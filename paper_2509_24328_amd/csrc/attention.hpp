@@ -12,8 +12,8 @@
 // then) and, in every lane, the sum of the weights of its keys.  Scores, weights, sums and outputs are float32; weights are rounded to
 // bfloat16 for the second product where the queries are bfloat16 (half a step, 2^-9 of a weight, at random).
 //
-// A workgroup has WR x WK wavefronts: WR blocks of 16 NT rows, WK interleaved parts of the keys, joined in LDS at the end.  Where there
-// are few rows, the keys of a row block are divided among up to `splits` workgroups, whose results a second kernel joins; each has
+// A workgroup has four wavefronts: one, two or four blocks of rows, and as many interleaved parts of the keys as that leaves, joined in
+// LDS at the end.  Where there are few rows, the keys of a row block are divided among up to `splits` workgroups, whose results a second kernel joins; each has
 // at least kMinSteps x 32 keys, and about as many as the average of kTargetGroups of them, from the lengths that the device knows.
 #pragma once
 
@@ -667,75 +667,63 @@ struct Wavefront {
   }
 };
 
-// One workgroup: a row block of a head of a sequence, a part of its keys.
-template <int ET, int CT, int DPAD, int NT, int WR, int WK, bool WHOLE>
-__global__ void __launch_bounds__(kAttnWaves* kWave, (DPAD == 256 || (ET == SV_F32 && DPAD == 128) ? 1 : 2)) attention_kernel(AttnArgs a) {
-  static_assert(WR * WK == kAttnWaves, "four wavefronts");
-  using Wf = Wavefront<ET, CT, DPAD, NT, WHOLE>;
+// What a workgroup works on: rows rho0 .. of head h of sequence b, steps [mine0, mine1) of the keys [lo, hi) from step step_lo on.
+struct Work {
+  Sequence s;
+  int b, h, item, split, parts, rho0, lo, hi, step0, step1;
+};
+
+// The rows of a workgroup with N blocks of sixteen to a wavefront: as many wavefronts share the keys among them as the rows leave.
+template <int ET, int CT, int DPAD, int N, bool WHOLE>
+__device__ __forceinline__ void attend(const AttnArgs& a, const Work& k, float* shared) {
+  using Wf = Wavefront<ET, CT, DPAD, N, WHOLE>;
   using Sh = Shape<ET, CT, DPAD>;
-  constexpr int kRows = 16 * NT;
-  // joined in LDS: the outputs of the wavefronts with another part of the keys, column by column
-  __shared__ float sh_o[WK > 1 ? WR * (WK / 2) : 1][WK > 1 ? NT * Wf::NO * 4 : 1][WK > 1 ? kWave : 1];
-  __shared__ float sh_ml[WK > 1 ? WR * (WK / 2) : 1][2][WK > 1 ? NT : 1][WK > 1 ? kWave : 1];
-  const int split = blockIdx.x % a.splits, item = blockIdx.x / a.splits;
-  const int tile = item % a.tiles, bh = item / a.tiles, h = bh % a.pages.heads, b = bh / a.pages.heads;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wr = wave % WR, wk = wave / WR;
-  const Sequence s = sequence_of(a, b);
-  const int rho0 = tile * a.tile_rows, rows = s.n * a.group - rho0;
-  if (rows <= 0) return;
-  const int i0 = divide(rho0, a.by_group), i1 = divide(min(rho0 + a.tile_rows, s.n * a.group) - 1, a.by_group);
-  int lo, hi;
-  keys_of(a, s, i0, i1, &lo, &hi);
-  const int step_lo = lo / kStep, steps = hi > lo ? (hi + kStep - 1) / kStep - step_lo : 0;
-  int mine0 = 0, mine1 = steps, parts = 1;
-  if (a.splits > 1) {
-    const int unit = steps_per_group(a);
-    parts = max(1, min((steps + unit - 1) / unit, a.splits));
-    if (split >= parts) return;
-    const int each = (steps + parts - 1) / parts;
-    mine0 = min(split * each, steps);
-    mine1 = min(mine0 + each, steps);
-    if (split == 0 && threadIdx.x == 0) a.n_split[item] = parts;
-  }
+  constexpr int kRows = 16 * N, NT = N;
+  const Sequence& s = k.s;
+  const int rows = min(s.n * a.group - k.rho0, a.tile_rows), blocks = (rows + kRows - 1) / kRows;
+  const int wr_all = blocks <= 1 ? 1 : (blocks <= 2 ? 2 : 4), wk_all = kAttnWaves / wr_all;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wr = wave & (wr_all - 1), wk = wave / wr_all;
+  const int h = k.h, item = k.item, split = k.split, parts = k.parts, rho0 = k.rho0;
   Wf w(a);
-  w.table = a.pages.table + (int64_t)b * a.pages.max_pages;
+  w.table = a.pages.table + (int64_t)k.b * a.pages.max_pages;
   w.head_off = (int64_t)h * (int)a.pages.page.d;
   w.start(s, rho0 + wr * kRows, h);
-  w.sweep(step_lo + mine0 + wk, step_lo + mine1, WK, lo, hi);
-  float l[NT];
+  w.sweep(k.step0 + wk, k.step1, wk_all, k.lo, k.hi);
+  float l[N];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) l[n] = across_sum(w.l[n]);
+  for (int n = 0; n < N; ++n) l[n] = across_sum(w.l[n]);
   const int lane = threadIdx.x & (kWave - 1);
-  if constexpr (WK > 1) {
-    // halves: the upper wavefronts hand over, the lower ones add
-#pragma unroll
-    for (int half = WK / 2; half >= 1; half /= 2) {
+  if (wk_all > 1) {
+    // joined in LDS, by halves: the upper wavefronts hand over, the lower ones add.  Two slots of [2 + 4 NO][N][64].
+    constexpr int kSlot = (2 + 4 * Wf::NO) * N * kWave;
+#pragma unroll 1
+    for (int half = wk_all / 2; half >= 1; half /= 2) {
       if (wk >= half && wk < 2 * half) {
-        const int slot = (wk - half) * WR + wr;
+        float* to = shared + ((wk - half) * wr_all + wr) * kSlot + lane;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          sh_ml[slot][0][n][lane] = w.mx[n];
-          sh_ml[slot][1][n][lane] = l[n];
+        for (int n = 0; n < N; ++n) {
+          to[(2 * n) * kWave] = w.mx[n];
+          to[(2 * n + 1) * kWave] = l[n];
 #pragma unroll
           for (int t = 0; t < Wf::NO; ++t) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sh_o[slot][(n * Wf::NO + t) * 4 + r][lane] = w.o[n][t][r];
+            for (int r = 0; r < 4; ++r) to[(2 * N + (n * Wf::NO + t) * 4 + r) * kWave] = w.o[n][t][r];
           }
         }
       }
       __syncthreads();
       if (wk < half) {
-        const int slot = wk * WR + wr;
+        const float* from = shared + (wk * wr_all + wr) * kSlot + lane;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const float m2 = sh_ml[slot][0][n][lane], top = fmaxf(w.mx[n], m2);
+        for (int n = 0; n < N; ++n) {
+          const float m2 = from[(2 * n) * kWave], top = fmaxf(w.mx[n], m2);
           const float f1 = w.mx[n] == top ? 1.f : exp2_fast(w.mx[n] - top), f2 = m2 == top ? 1.f : exp2_fast(m2 - top);
           w.mx[n] = top;
-          l[n] = l[n] * f1 + sh_ml[slot][1][n][lane] * f2;
+          l[n] = l[n] * f1 + from[(2 * n + 1) * kWave] * f2;
 #pragma unroll
           for (int t = 0; t < Wf::NO; ++t) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) w.o[n][t][r] = w.o[n][t][r] * f1 + sh_o[slot][(n * Wf::NO + t) * 4 + r][lane] * f2;
+            for (int r = 0; r < 4; ++r) w.o[n][t][r] = w.o[n][t][r] * f1 + from[(2 * N + (n * Wf::NO + t) * 4 + r) * kWave] * f2;
           }
         }
       }
@@ -799,9 +787,42 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, (DPAD == 256 || (ET == SV_F
   }
 }
 
+// One workgroup: a row block of a head of a sequence, a part of its keys.
+template <int ET, int CT, int DPAD, int NT, bool WHOLE>
+__global__ void __launch_bounds__(kAttnWaves* kWave, (DPAD == 256 || (ET == SV_F32 && DPAD == 128) ? 1 : 2)) attention_kernel(AttnArgs a) {
+  __shared__ float shared[2 * (2 + DPAD / 4) * NT * kWave];
+  Work k;
+  k.split = blockIdx.x % a.splits;
+  k.item = blockIdx.x / a.splits;
+  const int tile = k.item % a.tiles, bh = k.item / a.tiles;
+  k.h = bh % a.pages.heads;
+  k.b = bh / a.pages.heads;
+  k.s = sequence_of(a, k.b);
+  k.rho0 = tile * a.tile_rows;
+  const int rows = min(k.s.n * a.group - k.rho0, a.tile_rows);
+  if (rows <= 0) return;
+  const int i0 = divide(k.rho0, a.by_group), i1 = divide(k.rho0 + rows - 1, a.by_group);
+  keys_of(a, k.s, i0, i1, &k.lo, &k.hi);
+  const int step_lo = k.lo / kStep, steps = k.hi > k.lo ? (k.hi + kStep - 1) / kStep - step_lo : 0;
+  k.parts = 1;
+  k.step0 = step_lo;
+  k.step1 = step_lo + steps;
+  if (a.splits > 1) {
+    const int unit = steps_per_group(a);
+    k.parts = max(1, min((steps + unit - 1) / unit, a.splits));
+    if (k.split >= k.parts) return;
+    const int each = (steps + k.parts - 1) / k.parts;
+    k.step0 = step_lo + min(k.split * each, steps);
+    k.step1 = min(k.step0 + each, step_lo + steps);
+    if (k.split == 0 && threadIdx.x == 0) a.n_split[k.item] = k.parts;
+  }
+  if (NT > 1 && rows <= 16) attend<ET, CT, DPAD, 1, WHOLE>(a, k, shared);
+  else attend<ET, CT, DPAD, NT, WHOLE>(a, k, shared);
+}
+
 // Launches the kernel of a shape; what the rows decide is chosen in sv_chunk_attention.
 struct AttnLaunch {
-  int nt, wr;          // row blocks of a wavefront, row wavefronts of a workgroup
+  int nt;              // row blocks of a wavefront, at most
   bool whole;          // D is 64, 128 or 256 and no page ends inside a tile of sixteen keys
   unsigned grid;
   hipStream_t stream;
@@ -815,14 +836,10 @@ template <int ET, int CT, int DPAD>
 void launch_attention_of(const AttnArgs& a, const AttnLaunch& t) {
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(t.grid), dim3(kAttnWaves * kWave), 0, t.stream, a); };
   constexpr int NT = ET == SV_F32 || DPAD == 256 ? 1 : 2;
-  if (t.whole) {
-    if (t.wr == 4) go(attention_kernel<ET, CT, DPAD, NT, 4, 1, true>);
-    else if (t.wr == 2) go(attention_kernel<ET, CT, DPAD, NT, 2, 2, true>);
-    else if (t.nt == 2 && NT == 2) go(attention_kernel<ET, CT, DPAD, NT, 1, 4, true>);
-    else go(attention_kernel<ET, CT, DPAD, 1, 1, 4, true>);
+  if (t.nt == 1 || NT == 1) {
+    if (t.whole) go(attention_kernel<ET, CT, DPAD, 1, true>); else go(attention_kernel<ET, CT, DPAD, 1, false>);
   } else {
-    if (t.wr == 4) go(attention_kernel<ET, CT, DPAD, NT, 4, 1, false>);
-    else go(attention_kernel<ET, CT, DPAD, 1, 1, 4, false>);
+    if (t.whole) go(attention_kernel<ET, CT, DPAD, NT, true>); else go(attention_kernel<ET, CT, DPAD, NT, false>);
   }
 }
 template <int ET, int CT>

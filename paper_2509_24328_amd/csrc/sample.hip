@@ -333,10 +333,10 @@ struct Draw {
     return lo;
   }
 
-  // The largest key c of the row such that the entries >= c are at least K, or weigh at least `target` (which is `top_p * all`, `all`
-  // known in fp64); lo is such a key.
-  template <bool BY_COUNT>
-  __device__ __forceinline__ uint32_t narrow(int K, double target, double all, uint32_t lo, int n_lo) {
+  // The largest key c of the row such that the entries >= c are at least K, or weigh at least top_p of `all`; lo is such a key.  `all` is good
+  // to kMassError, and summed again by make_exact() where a decision needs it.
+  template <bool BY_COUNT, class Exact>
+  __device__ __forceinline__ uint32_t narrow(int K, double& all, bool& exact, Exact&& make_exact, uint32_t lo, int n_lo) {
     uint32_t hi = order_key((float)m) + 1;               // above every entry
     int n_hi = 0;
     for (int round = 0; hi - lo > kQuantum; ++round) {
@@ -354,7 +354,19 @@ struct Draw {
           vk[j] = i < n ? (uint32_t)(sh.key[i] >> 32) : 0u;
           w[j] = i < n && !BY_COUNT ? __builtin_rint(weight(key_float(vk[j])) / unit) * unit : 0.0;
         }
-        return search<BY_COUNT>(vk, w, lo, hi, n_hi, over, K, target);
+        const uint32_t cut = search<BY_COUNT>(vk, w, lo, hi, n_hi, over, K, a.top_p * all);
+        if (BY_COUNT || exact) return cut;
+        double at_cut = 0.0, past = 0.0;                 // masses of the list not below the cutoff, and above it
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) {
+          at_cut += vk[j] >= cut ? w[j] : 0.0;
+          past += vk[j] >= cut / kQuantum * kQuantum + kQuantum ? w[j] : 0.0;
+        }
+        at_cut = over + team.sum(at_cut) - a.top_p * all;
+        past = a.top_p * all - over - team.sum(past);
+        if (fmin(at_cut, past) > kMassError * all) return cut;
+        make_exact();
+        return search<BY_COUNT>(vk, w, lo, hi, n_hi, over, K, a.top_p * all);
       }
       uint32_t p[3];
       const uint32_t quarter = max((hi - lo) / 4, 1u);
@@ -379,8 +391,11 @@ struct Draw {
         if (BY_COUNT) {
           yes = c[k] >= K;
         } else {
-          if (fabs(s[k] - target) <= kMassError * all) s[k] = mass_above(p[k]);
-          yes = s[k] >= target;
+          if (fabs(s[k] - a.top_p * all) <= 2.0 * kMassError * all) {
+            make_exact();
+            s[k] = mass_above(p[k]);
+          }
+          yes = s[k] >= a.top_p * all;
         }
         if (yes) { lo = p[k]; n_lo = c[k]; break; }
         hi = p[k];
@@ -541,7 +556,7 @@ __device__ __forceinline__ void bad_row_out(const SampleArgs& a, int64_t r) {
 
 // No warps: a piece of the row for each wavefront in turn, weights relative to the piece's largest entry; one pass over the row.
 template <int DT>
-__global__ void __launch_bounds__(kDrawThreads, 4) sample_plain_kernel(SampleArgs a) {
+__global__ void __launch_bounds__(kDrawThreads, 2) sample_plain_kernel(SampleArgs a) {
   constexpr int EPV = Elem<DT>::per_vec;
   __shared__ DrawShared sh;
   __shared__ float piece_top[kList];
@@ -583,7 +598,6 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_plain_kernel(SampleArg
           nan |= v != v;
           top = fmaxf(top, v);
         }
-        __builtin_amdgcn_sched_barrier(0);
       }
       top = wave_max_f32(top);
       if (top == -INFINITY) continue;
@@ -600,10 +614,7 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_plain_kernel(SampleArg
         float x[EPV];
         unpack<DT>(q[j], x);
 #pragma unroll
-        for (int e = 0; e < EPV; ++e) {
-          s += d.weight(x[e]);
-          if (e % 2 == 1) __builtin_amdgcn_sched_barrier(0);   // (two weights side by side)
-        }
+        for (int e = 0; e < EPV; ++e) s += d.weight(x[e]);
       }
       if (base <= nvec && nvec < base + kPieceVecs * kWave && (nvec - base) % kWave == 0) {
 #pragma unroll
@@ -795,26 +806,35 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_kernel(SampleArgs a) {
     int want = use_k ? a.top_k : (use_p ? kNucleusRank : 0);
     if (attempt > 0) want = a.V <= kList ? 0 : min(kDeepRank, (n_keys * 2 + 2) / 3);
     uint32_t tau = none;
-    if (want > 0 && want <= kDrawThreads && attempt == 0) {
-      // every wavefront by itself, eight of the lanes' maxima in a lane
-      const u32x4 q = *reinterpret_cast<const u32x4*>(sh.lane_key + 8 * lane);
-      tau = select(low_key, top_key, want, [&](uint32_t probe) {
-        int c = 0;
+    // lanes whose maximum reaches a key: every wavefront by itself, eight of them in a lane
+    const u32x4 q = *reinterpret_cast<const u32x4*>(sh.lane_key + 8 * lane);
+    auto lanes = [&](uint32_t probe) {
+      int c = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) c += (int)__popcll(__ballot(((q[e / 2] >> (16 * (e % 2))) & 0xffffu) >= probe));
-        return c;
-      }) << 16;
+      for (int e = 0; e < 8; ++e) c += (int)__popcll(__ballot(((q[e / 2] >> (16 * (e % 2))) & 0xffffu) >= probe));
+      return c;
+    };
+    if (!use_k && use_min && lanes(min_key >> 16) <= kDrawThreads / 2) {
+      tau = none;                                        // few entries are above what min-p drops: all of them
+    } else if (want > 0 && want <= kDrawThreads && attempt == 0) {
+      tau = select(low_key, top_key, want, lanes) << 16;
       if (weigh && tau > min_key) {
         // a nucleus that the lanes' maxima above tau are far from filling is deeper than their list
         const double reached = team.sum((uint32_t)sh.lane_key[tid] >= (tau >> 16) ? (double)d.fast.weight(mine - top) : 0.0);
         if (reached < 0.7 * a.top_p * all) continue;
       }
     } else if (want > 0 && want <= n_keys) {
-      tau = select(0, top_key, want, [&](uint32_t probe) {
+      auto vectors = [&](uint32_t probe) {
         int c = 0;
-        each_key([&](uint32_t key, int) { c += key >= probe; });
+        for (int k = 8 * tid; k < n_keys; k += 8 * kDrawThreads) {
+          const u32x4 q = *reinterpret_cast<const u32x4*>(vec_key + k);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) c += ((q[e / 2] >> (16 * (e % 2))) & 0xffffu) >= probe;
+        }
         return team.count(wave_sum_i32(c));
-      }) << 16;
+      };
+      const uint32_t from = low_key > 0 && vectors(low_key) >= want ? low_key : 0;
+      tau = select(from, top_key, want, vectors) << 16;
     }
     tau = max(tau, none);
     if (!use_k) tau = max(tau, min_key);                 // (the K-th value may lie below what min-p keeps)
@@ -837,7 +857,7 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_kernel(SampleArgs a) {
       });
     __syncthreads();
     // their entries
-    u32x4 q[kOwn];
+    u32x4 held[kOwn];
     int v0[kOwn];
     const float least = key_float(tau);
     const int per = (n_vec + kDrawThreads - 1) / kDrawThreads;   // vectors of a thread
@@ -849,9 +869,9 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_kernel(SampleArgs a) {
     }
 #pragma unroll
     for (int j = 0; j < kOwn; ++j)
-      if (v0[j] >= 0 && v0[j] < nvec) q[j] = load_vec(d.row, v0[j]);
+      if (v0[j] >= 0 && v0[j] < nvec) held[j] = load_vec(d.row, v0[j]);
     auto entries = [&](int j, float (&x)[EPV]) {
-      if (v0[j] < nvec) unpack<DT>(q[j], x);
+      if (v0[j] < nvec) unpack<DT>(held[j], x);
       else vector_at(v0[j], x);
     };
 #pragma unroll
@@ -995,12 +1015,10 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_kernel(SampleArgs a) {
     __syncthreads();
     uint32_t least = none;                               // keys below it are dropped
     if (use_k) {
-      least = d.template narrow<true>(a.top_k, 0.0, 0.0, none, a.V);
+      least = d.template narrow<true>(a.top_k, all, exact, make_exact, none, a.V);
       if (use_p) all = d.mass_above(least);
-    } else if (use_p) {
-      make_exact();
     }
-    if (use_p) least = d.template narrow<false>(0, a.top_p * all, all, least, a.V);
+    if (use_p) least = d.template narrow<false>(0, all, exact, make_exact, least, a.V);
     z = d.draw_swept(key_float(least), u, &token, &W);
   }
   if (tid == 0) {
