@@ -792,9 +792,11 @@ template <int ET, int CT, int DPAD, int NT, bool WHOLE>
 __global__ void __launch_bounds__(kAttnWaves* kWave, (DPAD == 256 || (ET == SV_F32 && DPAD == 128) ? 1 : 2)) attention_kernel(AttnArgs a) {
   __shared__ float shared[2 * (2 + DPAD / 4) * NT * kWave];
   Work k;
-  k.split = blockIdx.x % a.splits;
-  k.item = blockIdx.x / a.splits;
-  const int tile = k.item % a.tiles, bh = k.item / a.tiles;
+  // workgroups go round the eight XCDs by their number: the row blocks of one head land on one (its keys and values are in that cache), and
+  // so do not the parts of a row block, most of which need not exist
+  const int heads = a.rows.B * a.pages.heads, bh = blockIdx.x % heads, rest = blockIdx.x / heads, tile = rest % a.tiles;
+  k.split = rest / a.tiles;
+  k.item = bh * a.tiles + tile;
   k.h = bh % a.pages.heads;
   k.b = bh / a.pages.heads;
   k.s = sequence_of(a, k.b);
