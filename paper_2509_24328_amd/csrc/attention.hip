@@ -175,7 +175,7 @@ extern "C" int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t
     w += ws_round((size_t)p.items * p.splits * p.tile_rows * 8);
     a.part_o = reinterpret_cast<float*>(w);
   }
-  const AttnLaunch t{p.nt, whole, (unsigned)(p.items * p.splits), as_stream(stream)};
+  const AttnLaunch t{p.nt, p.nt == 2 && p.tile_rows == 128, whole, (unsigned)(p.items * p.splits), as_stream(stream)};
   if (dtype == SV_F32) {
     if (f8) launch_attention_f32_f8(a, t); else launch_attention_f32(a, t);
   } else {

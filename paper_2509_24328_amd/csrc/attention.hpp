@@ -129,6 +129,15 @@ __device__ __forceinline__ void load_words(const char* p, uint32_t (&w)[N]) {
   }
 }
 
+// From LDS, aligned to its size.
+template <int N>
+__device__ __forceinline__ void load_lds(const char* p, uint32_t (&w)[N]) {
+  typedef uint32_t vec __attribute__((ext_vector_type(N)));
+  const vec v = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = v[i];
+}
+
 __device__ __forceinline__ uint32_t f8_pair_bf16(uint32_t w, bool high) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   const bf16x2 v = high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)
@@ -155,9 +164,12 @@ __device__ __forceinline__ float across_sum(float v) {
 }
 
 // The part of a row block's keys that a wavefront goes through, and its rows.
-template <int ET, int CT, int DPAD, int NT, bool WHOLE>
+template <int ET, int CT, int DPAD, int NT, bool WHOLE, bool STAGED = false>
 struct Wavefront {
-  using Sh = Shape<ET, CT, DPAD>;
+  // STAGED: keys and values come from LDS in the type of the queries, whatever the cache holds
+  using Sh = Shape<ET, STAGED ? ET : CT, DPAD>;
+  static constexpr bool kScaled = CT == SV_F8;          // rows have scales
+  static constexpr int kCacheBytes1 = CT == SV_F8 ? 1 : (CT == SV_F32 ? 4 : 2);
   static constexpr int NO = DPAD / 16;                  // output tiles of a block of sixteen rows
 
   const AttnArgs& a;
@@ -179,7 +191,7 @@ struct Wavefront {
     return (int64_t)at * a.pages.heads * (int)a.pages.page.d + head_off + (key - k * (int)a.pages.page.d);
   }
 
-  __device__ __forceinline__ int row_bytes() const { return (WHOLE ? DPAD : a.D) * Sh::cb; }
+  __device__ __forceinline__ int row_bytes() const { return (WHOLE ? DPAD : a.D) * kCacheBytes1; }
 
   __device__ __forceinline__ void start(const Sequence& s, int rho0, int h) {
 #pragma unroll
@@ -376,7 +388,7 @@ struct Wavefront {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) none[t][r] = found(w, t, 4 * g + r) < 0;
+        for (int r = 0; r < 4; ++r) none[t][r] = !STAGED && found(w, t, 4 * g + r) < 0;   // (staged keys in no page are NaN)
       }
     }
     bool raise = false;
@@ -388,7 +400,7 @@ struct Wavefront {
       for (int t = 0; t < 2; ++t) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float x = s[n][t][r] * (Sh::f8 ? ks[t][r] : a.scale2);
+          float x = s[n][t][r] * (kScaled ? ks[t][r] : a.scale2);
           if (PART) {
             const int key = key0 + 16 * t + 4 * g + r;
             x = none[t][r] ? NAN : x;
@@ -421,7 +433,7 @@ struct Wavefront {
         for (int r = 0; r < 4; ++r) {
           float p = exp2_fast(s[n][t][r] - base);
           l[n] += p;
-          if constexpr (Sh::f8) {
+          if constexpr (kScaled) {
             p *= vv.scale[4 * t + r];
             if (PART) {
               const int key = key0 + 16 * t + 4 * g + r;
@@ -539,12 +551,11 @@ struct Wavefront {
 
   // What clean_values took out, added to the rows that see it: weights are positive, so a sum with such a term is that of the values
   // themselves.  Read again from the cache, key by key.
-  __device__ __forceinline__ void add_odd_values(int key0, int lo, int hi, const Where& w) {
+  __device__ __forceinline__ void add_odd_values(int key0, int lo, int hi) {
 #pragma unroll 1
-    for (int j = 0; j < kStep; ++j) {
-      const int key = key0 + j;
-      const int64_t at = found(w, 0, j & 15), at1 = found(w, 1, j & 15), row = j < 16 ? at : at1;
-      if (key < lo || key >= hi || row < 0) continue;
+    for (int key = max(key0, lo); key < min(key0 + kStep, hi); ++key) {
+      const int64_t row = page_row(key);
+      if (row < 0) continue;
       const char* from = a.v_cache + row * row_bytes();
 #pragma unroll
       for (int t = 0; t < NO; ++t) {
@@ -553,10 +564,10 @@ struct Wavefront {
           const int col = (16 * (t / Sh::W) + 4 * g + r) * Sh::W + t % Sh::W;
           float v = 0.f;
           if (WHOLE || col < a.D) {
-            if constexpr (Sh::f8) {
+            if constexpr (CT == SV_F8) {
               const uint8_t c = static_cast<uint8_t>(from[col]);
               v = (c & 0x7f) == 0x7f ? NAN : 0.f;
-            } else if constexpr (Sh::f32) {
+            } else if constexpr (CT == SV_F32) {
               v = reinterpret_cast<const float*>(from)[col];
             } else {
               v = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(from)[col] << 16);
@@ -575,7 +586,7 @@ struct Wavefront {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) ks[t][r] = Sh::f8 ? kk.scale[t][r] * a.scale2 : 0.f;
+      for (int r = 0; r < 4; ++r) ks[t][r] = kScaled ? kk.scale[t][r] * a.scale2 : 0.f;
     }
   }
 
@@ -598,7 +609,7 @@ struct Wavefront {
       weigh<true>(key0, ks, vv, at, sc);
       const bool odd = clean_values(key0, lo, hi, vv);
       add_values(vv, sc);
-      if (odd) add_odd_values(key0, lo, hi, at);
+      if (odd) add_odd_values(key0, lo, hi);
     }
   }
 
@@ -629,24 +640,28 @@ struct Wavefront {
     }
   }
 
-  // Steps s0, s0 + stride, ... below s1 of the keys [lo, hi); step s begins at key 32 s.
-  __device__ __forceinline__ void sweep(int s0, int s1, int stride, int lo, int hi) {
-    if (s0 >= s1) return;
-    // keys that every row of the wavefront sees
-    int all_lo = 0, all_hi = 0x7fffffff;
+  // Keys of [lo, hi) that every row of the wavefront sees: all_lo .. all_hi.
+  __device__ __forceinline__ void seen_by_all(int lo, int hi, int* all_lo, int* all_hi) const {
+    int l0 = lo, h0 = hi - 1;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      all_lo = max(all_lo, low[n]);
-      all_hi = min(all_hi, pos[n]);
+      l0 = max(l0, low[n]);
+      h0 = min(h0, pos[n]);
     }
 #pragma unroll
     for (int d = 1; d < 16; d <<= 1) {
-      all_lo = max(all_lo, __shfl_xor(all_lo, d, kWave));
-      all_hi = min(all_hi, __shfl_xor(all_hi, d, kWave));
+      l0 = max(l0, __shfl_xor(l0, d, kWave));
+      h0 = min(h0, __shfl_xor(h0, d, kWave));
     }
-    all_lo = __builtin_amdgcn_readfirstlane(max(all_lo, lo));
-    all_hi = __builtin_amdgcn_readfirstlane(min(all_hi, hi - 1));
-    if (all_hi == 0x7fffffff) return;                    // no row is there
+    *all_lo = __builtin_amdgcn_readfirstlane(l0);
+    *all_hi = __builtin_amdgcn_readfirstlane(h0);
+  }
+
+  // Steps s0, s0 + stride, ... below s1 of the keys [lo, hi); step s begins at key 32 s.
+  __device__ __forceinline__ void sweep(int s0, int s1, int stride, int lo, int hi) {
+    if (s0 >= s1) return;
+    int all_lo, all_hi;
+    seen_by_all(lo, hi, &all_lo, &all_hi);
     // whether a page is missing
     bool gone = false;
     const int last = divide(min(kStep * s1, hi) - 1, a.pages.page);
@@ -673,68 +688,15 @@ struct Work {
   int b, h, item, split, parts, rho0, lo, hi, step0, step1;
 };
 
-// The rows of a workgroup with N blocks of sixteen to a wavefront: as many wavefronts share the keys among them as the rows leave.
-template <int ET, int CT, int DPAD, int N, bool WHOLE>
-__device__ __forceinline__ void attend(const AttnArgs& a, const Work& k, float* shared) {
-  using Wf = Wavefront<ET, CT, DPAD, N, WHOLE>;
-  using Sh = Shape<ET, CT, DPAD>;
-  constexpr int kRows = 16 * N, NT = N;
+// The wavefront's rows, from row rho on: outputs, or its part of them.
+template <class Wf, class Sh, int NT, bool WHOLE>
+__device__ __forceinline__ void write_out(const AttnArgs& a, const Work& k, const Wf& w, const float (&l)[NT], int rho_first) {
   const Sequence& s = k.s;
-  const int rows = min(s.n * a.group - k.rho0, a.tile_rows), blocks = (rows + kRows - 1) / kRows;
-  const int wr_all = blocks <= 1 ? 1 : (blocks <= 2 ? 2 : 4), wk_all = kAttnWaves / wr_all;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wr = wave & (wr_all - 1), wk = wave / wr_all;
-  const int h = k.h, item = k.item, split = k.split, parts = k.parts, rho0 = k.rho0;
-  Wf w(a);
-  w.table = a.pages.table + (int64_t)k.b * a.pages.max_pages;
-  w.head_off = (int64_t)h * (int)a.pages.page.d;
-  w.start(s, rho0 + wr * kRows, h);
-  w.sweep(k.step0 + wk, k.step1, wk_all, k.lo, k.hi);
-  float l[N];
-#pragma unroll
-  for (int n = 0; n < N; ++n) l[n] = across_sum(w.l[n]);
-  const int lane = threadIdx.x & (kWave - 1);
-  if (wk_all > 1) {
-    // joined in LDS, by halves: the upper wavefronts hand over, the lower ones add.  Two slots of [2 + 4 NO][N][64].
-    constexpr int kSlot = (2 + 4 * Wf::NO) * N * kWave;
-#pragma unroll 1
-    for (int half = wk_all / 2; half >= 1; half /= 2) {
-      if (wk >= half && wk < 2 * half) {
-        float* to = shared + ((wk - half) * wr_all + wr) * kSlot + lane;
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-          to[(2 * n) * kWave] = w.mx[n];
-          to[(2 * n + 1) * kWave] = l[n];
-#pragma unroll
-          for (int t = 0; t < Wf::NO; ++t) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) to[(2 * N + (n * Wf::NO + t) * 4 + r) * kWave] = w.o[n][t][r];
-          }
-        }
-      }
-      __syncthreads();
-      if (wk < half) {
-        const float* from = shared + (wk * wr_all + wr) * kSlot + lane;
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-          const float m2 = from[(2 * n) * kWave], top = fmaxf(w.mx[n], m2);
-          const float f1 = w.mx[n] == top ? 1.f : exp2_fast(w.mx[n] - top), f2 = m2 == top ? 1.f : exp2_fast(m2 - top);
-          w.mx[n] = top;
-          l[n] = l[n] * f1 + from[(2 * n + 1) * kWave] * f2;
-#pragma unroll
-          for (int t = 0; t < Wf::NO; ++t) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) w.o[n][t][r] = w.o[n][t][r] * f1 + from[(2 * N + (n * Wf::NO + t) * 4 + r) * kWave] * f2;
-          }
-        }
-      }
-      __syncthreads();
-    }
-    if (wk > 0) return;
-  }
+  const int h = k.h, rho0 = k.rho0, parts = k.parts, item = k.item, split = k.split;
   // lane (g, m): row m of the block, columns ((16 nb) + 4 g + r) W + c of output tile nb W + c
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int rho = rho0 + wr * kRows + 16 * n + w.m, i = divide(rho, a.by_group), hq = h * a.group + rho - i * a.group;
+    const int rho = rho_first + 16 * n + w.m, i = divide(rho, a.by_group), hq = h * a.group + rho - i * a.group;
     if (i >= s.n) continue;
     const bool out_of_pages = w.pos[n] >= s.cap;
     const bool any = w.mx[n] != -INFINITY || !(l[n] == 0.f);
@@ -787,11 +749,69 @@ __device__ __forceinline__ void attend(const AttnArgs& a, const Work& k, float* 
   }
 }
 
-// One workgroup: a row block of a head of a sequence, a part of its keys.
-template <int ET, int CT, int DPAD, int NT, bool WHOLE>
-__global__ void __launch_bounds__(kAttnWaves* kWave, (DPAD == 256 || (ET == SV_F32 && DPAD == 128) ? 1 : 2)) attention_kernel(AttnArgs a) {
-  __shared__ float shared[2 * (2 + DPAD / 4) * NT * kWave];
-  Work k;
+// The rows of a workgroup with N blocks of sixteen to a wavefront: as many wavefronts share the keys among them as the rows leave.
+template <int ET, int CT, int DPAD, int N, bool WHOLE>
+__device__ __forceinline__ void attend(const AttnArgs& a, const Work& k, float* shared) {
+  using Wf = Wavefront<ET, CT, DPAD, N, WHOLE>;
+  using Sh = Shape<ET, CT, DPAD>;
+  constexpr int kRows = 16 * N, NT = N;
+  const Sequence& s = k.s;
+  const int rows = min(s.n * a.group - k.rho0, a.tile_rows), blocks = (rows + kRows - 1) / kRows;
+  const int wr_all = blocks <= 1 ? 1 : (blocks <= 2 ? 2 : 4), wk_all = kAttnWaves / wr_all;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wr = wave & (wr_all - 1), wk = wave / wr_all;
+  const int h = k.h, rho0 = k.rho0;
+  Wf w(a);
+  w.table = a.pages.table + (int64_t)k.b * a.pages.max_pages;
+  w.head_off = (int64_t)h * (int)a.pages.page.d;
+  w.start(s, rho0 + wr * kRows, h);
+  w.sweep(k.step0 + wk, k.step1, wk_all, k.lo, k.hi);
+  float l[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) l[n] = across_sum(w.l[n]);
+  const int lane = threadIdx.x & (kWave - 1);
+  if (wk_all > 1) {
+    // joined in LDS, by halves: the upper wavefronts hand over, the lower ones add.  Two slots of [2 + 4 NO][N][64].
+    constexpr int kSlot = (2 + 4 * Wf::NO) * N * kWave;
+#pragma unroll 1
+    for (int half = wk_all / 2; half >= 1; half /= 2) {
+      if (wk >= half && wk < 2 * half) {
+        float* to = shared + ((wk - half) * wr_all + wr) * kSlot + lane;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          to[(2 * n) * kWave] = w.mx[n];
+          to[(2 * n + 1) * kWave] = l[n];
+#pragma unroll
+          for (int t = 0; t < Wf::NO; ++t) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) to[(2 * N + (n * Wf::NO + t) * 4 + r) * kWave] = w.o[n][t][r];
+          }
+        }
+      }
+      __syncthreads();
+      if (wk < half) {
+        const float* from = shared + (wk * wr_all + wr) * kSlot + lane;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          const float m2 = from[(2 * n) * kWave], top = fmaxf(w.mx[n], m2);
+          const float f1 = w.mx[n] == top ? 1.f : exp2_fast(w.mx[n] - top), f2 = m2 == top ? 1.f : exp2_fast(m2 - top);
+          w.mx[n] = top;
+          l[n] = l[n] * f1 + from[(2 * n + 1) * kWave] * f2;
+#pragma unroll
+          for (int t = 0; t < Wf::NO; ++t) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) w.o[n][t][r] = w.o[n][t][r] * f1 + from[(2 * N + (n * Wf::NO + t) * 4 + r) * kWave] * f2;
+          }
+        }
+      }
+      __syncthreads();
+    }
+    if (wk > 0) return;
+  }
+  write_out<Wf, Sh, N, WHOLE>(a, k, w, l, rho0 + wr * kRows);
+}
+
+// The part of the call that falls to this workgroup; the number of its rows, 0: nothing.
+__device__ __forceinline__ int work_of(const AttnArgs& a, Work& k) {
   // workgroups go round the eight XCDs by their number: the row blocks of one head land on one (its keys and values are in that cache), and
   // so do not the parts of a row block, most of which need not exist
   const int heads = a.rows.B * a.pages.heads, bh = blockIdx.x % heads, rest = blockIdx.x / heads, tile = rest % a.tiles;
@@ -802,7 +822,7 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, (DPAD == 256 || (ET == SV_F
   k.s = sequence_of(a, k.b);
   k.rho0 = tile * a.tile_rows;
   const int rows = min(k.s.n * a.group - k.rho0, a.tile_rows);
-  if (rows <= 0) return;
+  if (rows <= 0) return 0;
   const int i0 = divide(k.rho0, a.by_group), i1 = divide(k.rho0 + rows - 1, a.by_group);
   keys_of(a, k.s, i0, i1, &k.lo, &k.hi);
   const int step_lo = k.lo / kStep, steps = k.hi > k.lo ? (k.hi + kStep - 1) / kStep - step_lo : 0;
@@ -812,19 +832,189 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, (DPAD == 256 || (ET == SV_F
   if (a.splits > 1) {
     const int unit = steps_per_group(a);
     k.parts = max(1, min((steps + unit - 1) / unit, a.splits));
-    if (k.split >= k.parts) return;
+    if (k.split >= k.parts) return 0;
     const int each = (steps + k.parts - 1) / k.parts;
     k.step0 = step_lo + min(k.split * each, steps);
     k.step1 = min(k.step0 + each, step_lo + steps);
     if (k.split == 0 && threadIdx.x == 0) a.n_split[k.item] = k.parts;
   }
+  return rows;
+}
+
+// One workgroup: a row block of a head of a sequence, a part of its keys.
+template <int ET, int CT, int DPAD, int NT, bool WHOLE>
+__global__ void __launch_bounds__(kAttnWaves* kWave, (DPAD == 256 || (ET == SV_F32 && DPAD == 128) ? 1 : 2)) attention_kernel(AttnArgs a) {
+  __shared__ float shared[2 * (2 + DPAD / 4) * NT * kWave];
+  Work k;
+  const int rows = work_of(a, k);
+  if (rows <= 0) return;
   if (NT > 1 && rows <= 16) attend<ET, CT, DPAD, 1, WHOLE>(a, k, shared);
   else attend<ET, CT, DPAD, NT, WHOLE>(a, k, shared);
+}
+
+// Many rows: 128 to a workgroup, 32 to a wavefront, which all need the same keys and values.  A step of them at a time is staged in LDS as bfloat16
+// (8-bit ones are converted once, not by every wavefront), the next step under way in registers meanwhile.  The sixteen-byte chunks of a row are
+// permuted by its number, so that the rows of an operand (keys: sixteen rows, one chunk; values: one row, sixteen chunks) lie in different
+// banks.  What bounds it is the vector ALU beside the matrix cores: per 32 keys and 32 rows, 32 matrix instructions of 16 cycles
+// and 700 cycles of exponentials, maxima, sums and conversions.
+constexpr int kTileKeys = kStep;
+
+template <int CT, int DPAD, bool WHOLE>
+__global__ void __launch_bounds__(kAttnWaves* kWave, 2) attention_tile_kernel(AttnArgs a) {
+  constexpr int NT = 2, kChunks = DPAD / 8, kRowsAtOnce = kAttnWaves * kWave / kChunks, kLoads = kTileKeys / kRowsAtOnce;
+  constexpr bool kF8 = CT == SV_F8;
+  using Wf = Wavefront<SV_BF16, CT, DPAD, NT, WHOLE, true>;
+  using Sh = typename Wf::Sh;
+  __shared__ u32x4 tile[2][2][kTileKeys][kChunks];       // buffer, keys / values
+  __shared__ float scales[kF8 ? 2 : 1][2][kTileKeys];
+  auto place = [](int key, int chunk) { return chunk ^ (kChunks >= 16 ? key & 15 : (key >> 1) & (kChunks - 1)); };
+  Work k;
+  if (work_of(a, k) <= 0) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  Wf w(a);
+  w.table = a.pages.table + (int64_t)k.b * a.pages.max_pages;
+  w.head_off = (int64_t)k.h * (int)a.pages.page.d;
+  const int rho = k.rho0 + wave * 16 * NT;
+  w.start(k.s, rho, k.h);
+  int all_lo, all_hi;
+  w.seen_by_all(k.lo, k.hi, &all_lo, &all_hi);
+  // keys that some row of the wavefront sees
+  const int i0 = divide(rho, a.by_group), i1 = divide(rho + 16 * NT - 1, a.by_group);
+  int any_lo = k.hi, any_hi = k.hi;
+  if (i0 < k.s.n) keys_of(a, k.s, i0, min(i1, k.s.n - 1), &any_lo, &any_hi);
+
+  // a thread's chunk of rows row0, row0 + kRowsAtOnce, ... of a tile
+  const int chunk = threadIdx.x % kChunks, row0 = threadIdx.x / kChunks;
+  const bool there = WHOLE || 8 * chunk < a.D;
+  int64_t rows[kLoads];
+  Words<kF8 ? 2 : 4> kw[kLoads], vw[kLoads];
+  float sc[2];
+  auto find = [&](int key0) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) rows[j] = w.page_row(min(max(key0 + row0 + j * kRowsAtOnce, k.lo), k.hi - 1));
+  };
+  auto load = [&]() {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int64_t at = (rows[j] < 0 ? 0 : rows[j]) * w.row_bytes() + chunk * 8 * Wf::kCacheBytes1;
+      constexpr int n = kF8 ? 2 : 4;
+      if (there) {
+        load_words<n>(a.k_cache + at, kw[j].w);
+        load_words<n>(a.v_cache + at, vw[j].w);
+      } else {
+#pragma unroll
+        for (int e = 0; e < n; ++e) kw[j].w[e] = vw[j].w[e] = 0u;
+      }
+      if (rows[j] < 0) {                                 // in no page: scores are NaN
+#pragma unroll
+        for (int e = 0; e < n; ++e) { kw[j].w[e] = 0x7fff7fffu; vw[j].w[e] = 0u; }
+        if (kF8) { kw[j].w[0] = kw[j].w[1] = 0x7f7f7f7fu; }
+      }
+    }
+    if constexpr (kF8) {
+      // (the first kTileKeys threads' rows are every kRowsAtOnce-th: a thread's scales are those of one of its rows)
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+        if (chunk == j) {
+          sc[0] = rows[j] < 0 ? 1.f : a.k_scale[rows[j]];
+          sc[1] = rows[j] < 0 ? 1.f : a.v_scale[rows[j]];
+        }
+    }
+  };
+  auto store = [&](int buf) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int r = row0 + j * kRowsAtOnce, at = place(r, chunk);
+      if constexpr (kF8) {
+        tile[buf][0][r][at] = u32x4{f8_pair_bf16(kw[j].w[0], false), f8_pair_bf16(kw[j].w[0], true), f8_pair_bf16(kw[j].w[1], false),
+                                    f8_pair_bf16(kw[j].w[1], true)};
+        tile[buf][1][r][at] = u32x4{f8_pair_bf16(vw[j].w[0], false), f8_pair_bf16(vw[j].w[0], true), f8_pair_bf16(vw[j].w[1], false),
+                                    f8_pair_bf16(vw[j].w[1], true)};
+        if (chunk == j) { scales[buf][0][r] = sc[0]; scales[buf][1][r] = sc[1]; }
+      } else {
+        tile[buf][0][r][at] = u32x4{kw[j].w[0], kw[j].w[1], kw[j].w[2], kw[j].w[3]};
+        tile[buf][1][r][at] = u32x4{vw[j].w[0], vw[j].w[1], vw[j].w[2], vw[j].w[3]};
+      }
+    }
+  };
+  static_assert(kLoads <= kChunks, "a thread of a row for each of its scales");
+
+  typename Wf::Where nowhere;
+  if (k.step0 < k.step1) {
+    find(kStep * k.step0);
+    load();
+    store(0);
+    find(kStep * (k.step0 + 1));
+  }
+  int buf = 0;
+#pragma unroll 1
+  for (int s = k.step0; s < k.step1; ++s, buf ^= 1) {
+    __syncthreads();                                     // this step is written, and the one before it is done with
+    const bool more = s + 1 < k.step1;
+    if (more) {
+      load();
+      find(kStep * (s + 2));
+    }
+    const int key0 = kStep * s;
+    if (key0 < any_hi && key0 + kStep > any_lo) {
+      f32x4 sc2[NT][2];
+      typename Wf::Values vv;
+      float ks[2][4];
+      {
+        typename Wf::Keys kk;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+          for (int n = 0; n < Sh::NK; ++n) {
+            const int r = 16 * t + w.m;
+            const u32x4 x = tile[buf][0][r][place(r, 4 * n + w.g)];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) kk.k[t][n].w[e] = x[e];
+          }
+        }
+        w.scores(kk, sc2);
+        if constexpr (kF8) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = 16 * (i / 4) + 4 * w.g + i % 4;
+            kk.scale[i / 4][i % 4] = scales[buf][0][r];
+            vv.scale[i] = scales[buf][1][r];
+          }
+        }
+        w.scaled(kk, ks);
+      }
+      __builtin_amdgcn_sched_barrier(0);                 // (values read ahead of the weights would take registers that are not there)
+      const bool part = key0 < all_lo || key0 + kStep - 1 > all_hi;
+      if (part) w.template weigh<true>(key0, ks, vv, nowhere, sc2);
+      else w.template weigh<false>(key0, ks, vv, nowhere, sc2);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = 16 * (i / 4) + 4 * w.g + i % 4;
+#pragma unroll
+        for (int n = 0; n < Sh::NB; ++n) {
+          const int byte = (16 * n + w.m) * Sh::W * 2;
+          const char* from = reinterpret_cast<const char*>(&tile[buf][1][r][place(r, byte / 16)]) + byte % 16;
+          load_lds<Sh::WV>(from, vv.v[i][n].w);
+        }
+      }
+      bool odd = false;
+      if (part) odd = w.clean_values(key0, k.lo, k.hi, vv);
+      w.add_values(vv, sc2);
+      if (odd) w.add_odd_values(key0, k.lo, k.hi);
+    }
+    if (more) store(buf ^ 1);
+  }
+  float l[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) l[n] = across_sum(w.l[n]);
+  write_out<Wf, Sh, NT, WHOLE>(a, k, w, l, rho);
 }
 
 // Launches the kernel of a shape; what the rows decide is chosen in sv_chunk_attention.
 struct AttnLaunch {
   int nt;              // row blocks of a wavefront, at most
+  bool tile;           // more than 64 rows to a head and sequence
   bool whole;          // D is 64, 128 or 256 and no page ends inside a tile of sixteen keys
   unsigned grid;
   hipStream_t stream;
@@ -838,6 +1028,12 @@ template <int ET, int CT, int DPAD>
 void launch_attention_of(const AttnArgs& a, const AttnLaunch& t) {
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(t.grid), dim3(kAttnWaves * kWave), 0, t.stream, a); };
   constexpr int NT = ET == SV_F32 || DPAD == 256 ? 1 : 2;
+  if constexpr (NT == 2) {
+    if (t.tile) {
+      if (t.whole) go(attention_tile_kernel<CT, DPAD, true>); else go(attention_tile_kernel<CT, DPAD, false>);
+      return;
+    }
+  }
   if (t.nt == 1 || NT == 1) {
     if (t.whole) go(attention_kernel<ET, CT, DPAD, 1, true>); else go(attention_kernel<ET, CT, DPAD, 1, false>);
   } else {
