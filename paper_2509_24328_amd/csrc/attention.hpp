@@ -26,7 +26,9 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kStep = 32;              // keys of a step
 constexpr int kMinSteps = 8;           // steps of a workgroup that divides a row block's keys with others, at least
-constexpr int kTargetGroups = 1024;    // workgroups that the keys of a call are divided among
+// Workgroups that the keys of a call are divided among: two to a compute unit, which is what the registers hold.  64 x 1 over 16384 bf16: 512
+// 713 us, 1024 725, 2048 729; 64 x 9 over 8192 in 8 bits: 210, 216, 235; 2048 over 6144: 499, 537, 572.
+constexpr int kTargetGroups = 512;
 constexpr int kMaxSplits = 64;
 constexpr int kAttnWaves = 4;
 constexpr long long kMaxRows = 1 << 28;   // B * P * Hq: positions and rows stay within 32 bits
@@ -191,6 +193,7 @@ struct Wavefront {
     return (int64_t)at * a.pages.heads * (int)a.pages.page.d + head_off + (key - k * (int)a.pages.page.d);
   }
 
+  __device__ __forceinline__ float scale() const { return fabsf(a.scale2); }
   __device__ __forceinline__ int row_bytes() const { return (WHOLE ? DPAD : a.D) * kCacheBytes1; }
 
   __device__ __forceinline__ void start(const Sequence& s, int rho0, int h) {
@@ -214,6 +217,10 @@ struct Wavefront {
 #pragma unroll
           for (int j = 0; j < 4; ++j) qw[n][k * words + e * Sh::eb / 4 + j] = w[j];
         }
+      }
+      if (a.scale2 < 0.f) {                              // (the scale is taken positive)
+#pragma unroll
+        for (int j = 0; j < Sh::NK * Sh::EK * Sh::eb / 4; ++j) qw[n][j] ^= Sh::f32 ? 0x80000000u : 0x80008000u;
       }
       mx[n] = -INFINITY;
       l[n] = 0.f;
@@ -379,41 +386,52 @@ struct Wavefront {
     }
   }
 
-  // Scores to weights, in place (p: what multiplies the values), with the running maximum and sum.  PART: some key of the step is not
-  // seen by some row, or in no page.  ks: scales of the keys (8 bits).
+  // Scores to weights, in place (what multiplies the values), with the running maximum and sum, in three parts.  PART: some key of the step is
+  // not seen by some row, or in no page.  ks: scales of the keys (8 bits).
   template <bool PART>
-  __device__ __forceinline__ void weigh(int key0, const float (&ks)[2][4], const Values& vv, const Where& w, f32x4 (&s)[NT][2]) {
+  __device__ __forceinline__ void mask(int key0, const float (&ks)[2][4], const Where& w, f32x4 (&s)[NT][2]) const {
+    if constexpr (!PART && !kScaled) return;
     bool none[2][4];
     if (PART) {
+      asm volatile("");                                  // (a branch)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) none[t][r] = !STAGED && found(w, t, 4 * g + r) < 0;   // (staged keys in no page are NaN)
       }
     }
-    bool raise = false;
-    float top[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      float t8 = -INFINITY;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float x = s[n][t][r] * (kScaled ? ks[t][r] : a.scale2);
+          float x = kScaled ? s[n][t][r] * ks[t][r] : s[n][t][r];
           if (PART) {
             const int key = key0 + 16 * t + 4 * g + r;
             x = none[t][r] ? NAN : x;
             x = key >= low[n] && key <= pos[n] ? x : -INFINITY;
           }
           s[n][t][r] = x;
-          t8 = fmaxf(t8, x);
         }
       }
-      top[n] = across_max(t8);
-      raise |= top[n] > mx[n] + 8.f;
     }
-    if (__ballot(raise)) {
+  }
+
+  __device__ __forceinline__ void raise(const f32x4 (&s)[NT][2]) {
+    bool any = false;
+    float top[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float t8 = fmaxf(s[n][0][0], s[n][0][1]);
+      t8 = fmaxf(fmaxf(t8, s[n][0][2]), s[n][0][3]);
+      t8 = fmaxf(fmaxf(t8, s[n][1][0]), s[n][1][1]);
+      t8 = fmaxf(fmaxf(t8, s[n][1][2]), s[n][1][3]);
+      top[n] = across_max(kScaled ? t8 : t8 * scale());
+      any |= top[n] > mx[n] + 8.f;
+    }
+    if (__builtin_expect(__ballot(any) != 0, 0)) {
+      asm volatile("");                                  // (a branch: done without one and selected, this is a third of a step's operations)
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const bool up = top[n] > mx[n] + 8.f;
@@ -424,6 +442,10 @@ struct Wavefront {
         for (int t = 0; t < NO; ++t) o[n][t] *= f;
       }
     }
+  }
+
+  template <bool PART>
+  __device__ __forceinline__ void weigh(int key0, const Values& vv, f32x4 (&s)[NT][2]) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const float base = mx[n] == -INFINITY ? 0.f : mx[n];
@@ -431,7 +453,7 @@ struct Wavefront {
       for (int t = 0; t < 2; ++t) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float p = exp2_fast(s[n][t][r] - base);
+          float p = exp2_fast(kScaled ? s[n][t][r] - base : __builtin_fmaf(s[n][t][r], scale(), -base));
           l[n] += p;
           if constexpr (kScaled) {
             p *= vv.scale[4 * t + r];
@@ -586,7 +608,7 @@ struct Wavefront {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) ks[t][r] = kScaled ? kk.scale[t][r] * a.scale2 : 0.f;
+      for (int r = 0; r < 4; ++r) ks[t][r] = kScaled ? kk.scale[t][r] * scale() : 0.f;
     }
   }
 
@@ -606,7 +628,9 @@ struct Wavefront {
       scores(kk, sc);
       float ks[2][4];
       scaled(kk, ks);
-      weigh<true>(key0, ks, vv, at, sc);
+      mask<true>(key0, ks, at, sc);
+      raise(sc);
+      weigh<true>(key0, vv, sc);
       const bool odd = clean_values(key0, lo, hi, vv);
       add_values(vv, sc);
       if (odd) add_odd_values(key0, lo, hi);
@@ -634,7 +658,9 @@ struct Wavefront {
       scaled(kk, ks);
       settle(next);
       if (s + stride < s1) load_keys(next, kk);
-      weigh<false>(kStep * s, ks, vv, at, sc);
+      mask<false>(kStep * s, ks, at, sc);
+      raise(sc);
+      weigh<false>(kStep * s, vv, sc);
       add_values(vv, sc);
       at = next;
     }
@@ -883,7 +909,8 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, 2) attention_tile_kernel(At
   int any_lo = k.hi, any_hi = k.hi;
   if (i0 < k.s.n) keys_of(a, k.s, i0, min(i1, k.s.n - 1), &any_lo, &any_hi);
 
-  // a thread's chunk of rows row0, row0 + kRowsAtOnce, ... of a tile
+  // a thread's chunk of rows row0, row0 + kRowsAtOnce, ... of a step.  Its rows of the cache; WHOLE: that of the first of the sixteen keys that
+  // its wavefront's rows belong to, the same in all lanes.
   const int chunk = threadIdx.x % kChunks, row0 = threadIdx.x / kChunks;
   const bool there = WHOLE || 8 * chunk < a.D;
   int64_t rows[kLoads];
@@ -891,34 +918,40 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, 2) attention_tile_kernel(At
   float sc[2];
   auto find = [&](int key0) {
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) rows[j] = w.page_row(min(max(key0 + row0 + j * kRowsAtOnce, k.lo), k.hi - 1));
+    for (int j = 0; j < kLoads; ++j) {
+      const int r = row0 + j * kRowsAtOnce;
+      if constexpr (WHOLE) rows[j] = w.page_row(__builtin_amdgcn_readfirstlane(min(max(key0 + (r & ~15), k.lo & ~15), (k.hi - 1) & ~15)));
+      else rows[j] = w.page_row(min(max(key0 + r, k.lo), k.hi - 1));
+    }
   };
+  const uint32_t within = (WHOLE ? (uint32_t)((row0 & 15) * w.row_bytes()) : 0u) + (uint32_t)(chunk * 8 * Wf::kCacheBytes1);
   auto load = [&]() {
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
-      const int64_t at = (rows[j] < 0 ? 0 : rows[j]) * w.row_bytes() + chunk * 8 * Wf::kCacheBytes1;
+      int64_t row = rows[j];
+      if constexpr (WHOLE) {
+        const uint32_t r0 = __builtin_amdgcn_readfirstlane((uint32_t)row), r1 = __builtin_amdgcn_readfirstlane((uint32_t)(row >> 32));
+        row = (int64_t)(((uint64_t)r1 << 32) | r0);
+      }
+      const int64_t at = (row < 0 ? 0 : row) * w.row_bytes();
       constexpr int n = kF8 ? 2 : 4;
       if (there) {
-        load_words<n>(a.k_cache + at, kw[j].w);
-        load_words<n>(a.v_cache + at, vw[j].w);
+        load_words<n>(a.k_cache + at + within, kw[j].w);
+        load_words<n>(a.v_cache + at + within, vw[j].w);
       } else {
 #pragma unroll
         for (int e = 0; e < n; ++e) kw[j].w[e] = vw[j].w[e] = 0u;
       }
-      if (rows[j] < 0) {                                 // in no page: scores are NaN
+      if (row < 0) {                                     // in no page: scores are NaN
 #pragma unroll
-        for (int e = 0; e < n; ++e) { kw[j].w[e] = 0x7fff7fffu; vw[j].w[e] = 0u; }
-        if (kF8) { kw[j].w[0] = kw[j].w[1] = 0x7f7f7f7fu; }
+        for (int e = 0; e < n; ++e) { kw[j].w[e] = kF8 ? 0x7f7f7f7fu : 0x7fff7fffu; vw[j].w[e] = 0u; }
       }
-    }
-    if constexpr (kF8) {
-      // (the first kTileKeys threads' rows are every kRowsAtOnce-th: a thread's scales are those of one of its rows)
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j)
-        if (chunk == j) {
-          sc[0] = rows[j] < 0 ? 1.f : a.k_scale[rows[j]];
-          sc[1] = rows[j] < 0 ? 1.f : a.v_scale[rows[j]];
-        }
+      // (a thread of a row for the scales of each of its rows)
+      if (kF8 && chunk == j) {
+        const int64_t in = row < 0 ? 0 : row + (WHOLE ? row0 & 15 : 0);
+        sc[0] = row < 0 ? 1.f : a.k_scale[in];
+        sc[1] = row < 0 ? 1.f : a.v_scale[in];
+      }
     }
   };
   auto store = [&](int buf) {
@@ -938,6 +971,7 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, 2) attention_tile_kernel(At
     }
   };
   static_assert(kLoads <= kChunks, "a thread of a row for each of its scales");
+  static_assert(kWave / kChunks <= 16, "the rows of a wavefront belong to sixteen keys that begin at a multiple of 16");
 
   typename Wf::Where nowhere;
   if (k.step0 < k.step1) {
@@ -985,8 +1019,11 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, 2) attention_tile_kernel(At
       }
       __builtin_amdgcn_sched_barrier(0);                 // (values read ahead of the weights would take registers that are not there)
       const bool part = key0 < all_lo || key0 + kStep - 1 > all_hi;
-      if (part) w.template weigh<true>(key0, ks, vv, nowhere, sc2);
-      else w.template weigh<false>(key0, ks, vv, nowhere, sc2);
+      if (part) w.template mask<true>(key0, ks, nowhere, sc2);
+      else w.template mask<false>(key0, ks, nowhere, sc2);
+      w.raise(sc2);
+      if (kF8 && part) w.template weigh<true>(key0, vv, sc2);
+      else w.template weigh<false>(key0, vv, sc2);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
