@@ -839,12 +839,18 @@ int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t* t_offsets
  *   u  [rows] double in [0, 1)      in   (outside: the nearest number inside; sv_uniforms makes such numbers)
  *   token [rows] int32, logprob_or_null [rows] float         out
  *   flags_or_null [rows] uint32     out  SV_FLAG_BAD_ROW (also where u is NaN): token -1, logprob NaN
+ *   ws_or_null                      256-byte aligned, of sv_sample_workspace_bytes.  Without it one workgroup reads each row: the same
+ *                                   results, but for the order of the sums, in more time
  * Weights and sums are float64, in an order that the sizes fix: the same call gives the same tokens.
  * 0 < top_p, 0 <= min_p <= 1, temperature in [1e-3, 1e3], V <= 16777216.
  */
 int sv_sample(const void* z, int64_t z_stride, int rows, int V, int dtype, float temperature, int top_k, float top_p,
               float min_p, const double* u, int32_t* token, float* logprob_or_null, uint32_t* flags_or_null,
-              sv_stream_t stream);
+              void* ws_or_null, size_t ws_bytes, sv_stream_t stream);
+
+/* Bytes of device scratch with which sv_sample divides its rows among more workgroups where there are few (0: it never does, or the shape is
+ * invalid). */
+size_t sv_sample_workspace_bytes(int rows, int V, int dtype);
 
 /*
  * The uniforms sv_verify_sample draws (for tests and for callers that want to

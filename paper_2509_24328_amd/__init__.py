@@ -13,6 +13,6 @@ from .binding import (sv_warp_cutoffs_multi, sv_warp_compact_multi, sv_accept_ra
                       sv_embedding_grad_workspace_bytes, sv_grad_norm, sv_clip_grad_norm,
                       sv_grad_norm_workspace_bytes, SV_TOP_MAX,
                       sv_rope_frequencies, sv_rope, sv_cache_write, sv_cache_read, sv_chunk_attention,
-                      sv_chunk_attention_workspace_bytes, sv_sample, Cache, SV_F8, SV_ROPE_HALVES, SV_ROPE_PAIRS,
+                      sv_chunk_attention_workspace_bytes, sv_sample, sv_sample_workspace_bytes, Cache, SV_F8, SV_ROPE_HALVES, SV_ROPE_PAIRS,
                       SV_ROPE_PLAIN, SV_ROPE_LINEAR, SV_ROPE_NTK, SV_ROPE_PARTS,
                       sv_workspace_bytes)

@@ -41,7 +41,7 @@ EXPORTS = ("sv_strerror", "sv_workspace_bytes", "sv_row_stats", "sv_accept_estim
            "sv_token_logprobs_workspace_bytes", "sv_embedding",
            "sv_embedding_grad_workspace_bytes", "sv_embedding_grad", "sv_grad_norm_workspace_bytes", "sv_grad_norm",
            "sv_clip_grad_norm", "sv_rope_frequencies", "sv_rope", "sv_cache_write", "sv_cache_read",
-           "sv_chunk_attention", "sv_chunk_attention_workspace_bytes", "sv_sample")
+           "sv_chunk_attention", "sv_chunk_attention_workspace_bytes", "sv_sample", "sv_sample_workspace_bytes")
 SV_WARP_MAX_TENSORS = 8
 SV_STATIC_SCRATCH_BYTES = 1 << 20
 SV_TOP_MAX = 32
@@ -157,7 +157,9 @@ lib.sv_chunk_attention.restype = _i
 lib.sv_chunk_attention.argtypes = [_vp, _ll, _vp, _i, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _vp, _vp, _i, _vp, _vp, _i, _i, _f, _i,
                                    _vp, _ll, _vp, _vp, _vp, _sz, _vp]
 lib.sv_sample.restype = _i
-lib.sv_sample.argtypes = [_vp, _ll, _i, _i, _i, _f, _i, _f, _f, _vp, _vp, _vp, _vp, _vp]
+lib.sv_sample.argtypes = [_vp, _ll, _i, _i, _i, _f, _i, _f, _f, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+lib.sv_sample_workspace_bytes.restype = _sz
+lib.sv_sample_workspace_bytes.argtypes = [_i, _i, _i]
 lib.sv_set_timing_events.restype = _i
 lib.sv_set_timing_events.argtypes = [_i, _vp, _vp]
 
@@ -683,30 +685,35 @@ def sv_clip_grad_norm(grads, max_norm, norm, out=None, flag=None, ws=None, strea
 # ---------------------------------------------------------------------------
 # the model side of a step
 # ---------------------------------------------------------------------------
-def _here(*tensors):
-    """Refuses tensors that do not lie on the current device, whose stream the calls run on.  (Numbers of devices, from torch's C layer:
-    torch.device objects take longer to make than a small call runs.)"""
+def _device():
+    """Number of the current device, whose stream the calls run on.  (From torch's C layer: torch.device objects take longer to make
+    than a small call runs.)"""
     try:
-        device = torch._C._cuda_getDevice()
+        return torch._C._cuda_getDevice()
     except (AttributeError, RuntimeError):
-        device = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError(f"sv: tensors must lie on the current device (cuda:{device}, got {t.device})")
+        return torch.cuda.current_device()
 
 
-def _dense(t):
-    """Address of a contiguous tensor whose device has been looked at (None -> NULL)."""
+def _refuse(t, device):
+    if t.get_device() != device:
+        raise ValueError(f"sv: tensors must lie on the current device (cuda:{device}, got {t.device})")
+    raise ValueError(f"sv: tensors must be contiguous device tensors (got device={t.device}, contiguous={t.is_contiguous()})")
+
+
+def _at(t, device):
+    """Address of a contiguous tensor on the current device (None -> NULL)."""
     if t is None:
         return None
-    if not t.is_contiguous():
-        raise ValueError(f"sv: tensors must be contiguous device tensors (got device={t.device}, contiguous=False)")
+    if t.get_device() != device or not t.is_contiguous():
+        _refuse(t, device)
     return t.data_ptr()
 
 
-def _heads(t):
-    """(address, elements from row to row) of [..., H, D] whose heads follow each other and whose rows lie at one distance, as
-    columns of a wider projection do."""
+def _heads(t, device):
+    """(address, elements from row to row) of [..., H, D] on the current device whose heads follow each other and whose rows lie at one
+    distance, as columns of a wider projection do."""
+    if t.get_device() != device:
+        _refuse(t, device)
     shape, strides = t.shape, t.stride()
     if len(shape) == 3 and strides[2] == 1 and strides[1] == shape[2] and strides[0] >= shape[1] * shape[2]:
         return t.data_ptr(), strides[0]
@@ -739,7 +746,7 @@ def _tag(t):
 
 class Cache:
     """Keys and values of a model's layer in pages: k, v [n_pages, heads, page, D] in float32, bfloat16 or float8_e4m3fn, the last
-    one with float32 scales [n_pages, heads, page].  Takes tensors, or makes them (Cache.empty)."""
+    one with float32 scales k_scale, v_scale [n_pages, heads, page].  Made from tensors, which stay its own, or by Cache.empty."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         f8 = k.dtype == torch.float8_e4m3fn
@@ -755,9 +762,18 @@ class Cache:
             _f32(k_scale, v_scale)
             if k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3]:
                 raise SvError(SV_ERR_INVALID_ARG)
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.heads, self.page, self.D = k.shape
         self.dtype = SV_F8 if f8 else _TAGS[k.dtype]
+        self.device = k.get_device()
+        self._tensors = (k, v, k_scale, v_scale)
+        at = [_at(t, self.device) if k.is_cuda else _ptr(t) for t in self._tensors]
+        # (one validation for all calls: a layer's cache takes part in every one of its steps)
+        self._args = (at[0], at[1], self.dtype, at[2], at[3], self.n_pages, self.page)
+
+    k = property(lambda self: self._tensors[0])
+    v = property(lambda self: self._tensors[1])
+    k_scale = property(lambda self: self._tensors[2])
+    v_scale = property(lambda self: self._tensors[3])
 
     @classmethod
     def empty(cls, n_pages, heads, page, D, dtype=torch.bfloat16, device="cuda"):
@@ -766,57 +782,57 @@ class Cache:
             return cls(k, v)
         return cls(k, v, *(torch.empty((n_pages, heads, page), dtype=torch.float32, device=device) for _ in range(2)))
 
-    def _ptrs(self):
-        return (_dense(self.k), _dense(self.v), self.dtype, _dense(self.k_scale), _dense(self.v_scale), self.n_pages, self.page)
 
-
-def _new_rows(rows, t_offsets, start, pages, P):
-    """(n_rows, B, P) of new tokens whose rows have the leading shape `rows`: [B, P], or [n_rows] with t_offsets [B+1] and P."""
-    if pages.dim() != 2:
+def _new_rows(shape, t_offsets, start, pages, P, cache, device):
+    """(n_rows, B, P, max_pages, addresses of t_offsets, start and pages) of new tokens in rows of `shape`: [B, P, heads, D], or
+    [n_rows, heads, D] with t_offsets [B+1] and P."""
+    table = pages.shape
+    if len(table) != 2 or start.numel() != table[0]:
         raise SvError(SV_ERR_INVALID_ARG)
-    B = pages.shape[0]
-    if start.numel() != B:
-        raise SvError(SV_ERR_INVALID_ARG)
-    if t_offsets is None:
-        _i32(start, pages)
-        if len(rows) != 2 or rows[0] != B or (P is not None and P != rows[1]):
-            raise SvError(SV_ERR_INVALID_ARG)
-        return rows[0] * rows[1], B, rows[1]
-    _i32(t_offsets, start, pages)
-    if len(rows) != 1 or P is None or t_offsets.numel() != B + 1:
-        raise SvError(SV_ERR_INVALID_ARG)
-    return rows[0], B, P
-
-
-def sv_rope_frequencies(freq, base=10000.0, scaling=SV_ROPE_PLAIN, factor=1.0, low=1.0, high=32.0, length=0, stream=None):
-    """freq: [rot / 2] float64."""
-    if freq.dtype != torch.float64:
+    if start.dtype not in _INT32 or pages.dtype not in _INT32:
         raise SvError(SV_ERR_DTYPE)
-    _here(freq)
-    _check(lib.sv_rope_frequencies(2 * freq.numel(), base, scaling, factor, low, high, length, _dense(freq), _stream(stream)))
+    if cache.device != device:
+        _refuse(cache.k, device)
+    B, max_pages = table
+    if t_offsets is None:
+        if len(shape) != 4 or shape[0] != B or (P is not None and P != shape[1]):
+            raise SvError(SV_ERR_INVALID_ARG)
+        return B * shape[1], B, shape[1], max_pages, None, _at(start, device), _at(pages, device)
+    if len(shape) != 3 or P is None or t_offsets.numel() != B + 1:
+        raise SvError(SV_ERR_INVALID_ARG)
+    if t_offsets.dtype not in _INT32:
+        raise SvError(SV_ERR_DTYPE)
+    return shape[0], B, P, max_pages, _at(t_offsets, device), _at(start, device), _at(pages, device)
 
 
-def _freq(freq):
+def _freq(freq, device):
     if freq is None:
         return None, 0
     if freq.dtype != torch.float64:
         raise SvError(SV_ERR_DTYPE)
-    return _dense(freq), 2 * freq.numel()
+    return _at(freq, device), 2 * freq.numel()
+
+
+def sv_rope_frequencies(freq, base=10000.0, scaling=SV_ROPE_PLAIN, factor=1.0, low=1.0, high=32.0, length=0, stream=None):
+    """freq: [rot / 2] float64."""
+    addr, rot = _freq(freq, _device())
+    _check(lib.sv_rope_frequencies(rot, base, scaling, factor, low, high, length, addr, _stream(stream)))
 
 
 def sv_rope(x, positions, freq, out, layout=SV_ROPE_HALVES, amplitude=1.0, inverse=False, stream=None):
     """x, out: [..., H, D], out may be x; positions: one int32 per row; freq: [rot / 2] float64."""
-    addr, stride = _heads(x)
-    o_addr, o_stride = _heads(out)
+    device = _device()
+    addr, stride = _heads(x, device)
+    o_addr, o_stride = _heads(out, device)
     shape = x.shape
     H, D = shape[-2:]
     n = positions.numel()
     if out.shape != shape or out.dtype != x.dtype or x.numel() != n * H * D:
         raise SvError(SV_ERR_INVALID_ARG)
-    _i32(positions)
-    _here(x, positions, freq, out)
-    f, rot = _freq(freq)
-    _check(lib.sv_rope(addr, stride, _dense(positions), n, H, D, _tag(x), f, rot, layout, amplitude, inverse, o_addr, o_stride,
+    if positions.dtype not in _INT32:
+        raise SvError(SV_ERR_DTYPE)
+    f, rot = _freq(freq, device)
+    _check(lib.sv_rope(addr, stride, _at(positions, device), n, H, D, _tag(x), f, rot, layout, amplitude, inverse, o_addr, o_stride,
                        _stream(stream)))
 
 
@@ -824,12 +840,12 @@ def sv_cache_write(cache, k, v, lengths, pages, t_offsets=None, P=None, q=None, 
                    layout=SV_ROPE_HALVES, amplitude=1.0, flags=None, stream=None):
     """k, v: [B, P, heads, D]; or [n_rows, heads, D] with t_offsets [B+1] and P.  q, q_out: the same with the queries' heads.
     pages: [B, max_pages].  freq None: nothing is turned."""
-    shape = k.shape
-    n_rows, B, P = _new_rows(shape[:-2], t_offsets, lengths, pages, P)
+    device, shape = _device(), k.shape
+    n_rows, B, P, max_pages, offs, start, table = _new_rows(shape, t_offsets, lengths, pages, P, cache, device)
     if v.shape != shape or v.dtype != k.dtype or shape[-2] != cache.heads or shape[-1] != cache.D:
         raise SvError(SV_ERR_INVALID_ARG)
-    k_addr, k_stride = _heads(k)
-    v_addr, v_stride = _heads(v)
+    k_addr, k_stride = _heads(k, device)
+    v_addr, v_stride = _heads(v, device)
     q_addr, q_stride, o_addr, o_stride, Hq = None, 0, None, 0, 0
     if (q is None) != (q_out is None):
         raise SvError(SV_ERR_NULL)
@@ -839,52 +855,59 @@ def sv_cache_write(cache, k, v, lengths, pages, t_offsets=None, P=None, q=None, 
             raise SvError(SV_ERR_INVALID_ARG)
         if q.dtype != k.dtype or q_out.dtype != k.dtype:
             raise SvError(SV_ERR_DTYPE)
-        q_addr, q_stride = _heads(q)
-        o_addr, o_stride = _heads(q_out)
+        q_addr, q_stride = _heads(q, device)
+        o_addr, o_stride = _heads(q_out, device)
         Hq = q_shape[-2]
     if flags is not None:
         _i32(flags)
         _outputs((n_rows,), flags)
-    _here(k, v, cache.k, cache.v, cache.k_scale, cache.v_scale, q, q_out, lengths, pages, t_offsets, freq, flags)
-    f, rot = _freq(freq)
-    kc, vc, tag, ks, vs, n_pages, page = cache._ptrs()
-    _check(lib.sv_cache_write(k_addr, k_stride, v_addr, v_stride, q_addr, q_stride, Hq, o_addr, o_stride, _dense(t_offsets), n_rows,
-                              _dense(lengths), _dense(pages), pages.shape[1], B, P, cache.heads, cache.D, _tag(k), f, rot, layout,
-                              amplitude, kc, vc, tag, ks, vs, n_pages, page, _dense(flags), _stream(stream)))
+    f, rot = _freq(freq, device)
+    kc, vc, tag, ks, vs, n_pages, page = cache._args
+    _check(lib.sv_cache_write(k_addr, k_stride, v_addr, v_stride, q_addr, q_stride, Hq, o_addr, o_stride, offs, n_rows, start, table,
+                              max_pages, B, P, cache.heads, cache.D, _tag(k), f, rot, layout, amplitude, kc, vc, tag, ks, vs, n_pages,
+                              page, _at(flags, device), _stream(stream)))
 
 
 def sv_cache_read(cache, k, v, start, pages, t_offsets=None, P=None, flags=None, stream=None):
     """k, v (out): [B, P, heads, D]; or [n_rows, heads, D] with t_offsets [B+1] and P: positions start[b] + i."""
-    shape = k.shape
-    n_rows, B, P = _new_rows(shape[:-2], t_offsets, start, pages, P)
+    device, shape = _device(), k.shape
+    n_rows, B, P, max_pages, offs, first, table = _new_rows(shape, t_offsets, start, pages, P, cache, device)
     if v.shape != shape or v.dtype != k.dtype or shape[-2] != cache.heads or shape[-1] != cache.D:
         raise SvError(SV_ERR_INVALID_ARG)
-    k_addr, k_stride = _heads(k)
-    v_addr, v_stride = _heads(v)
+    k_addr, k_stride = _heads(k, device)
+    v_addr, v_stride = _heads(v, device)
     if flags is not None:
         _i32(flags)
         _outputs((n_rows,), flags)
-    _here(k, v, cache.k, cache.v, cache.k_scale, cache.v_scale, start, pages, t_offsets, flags)
-    kc, vc, tag, ks, vs, n_pages, page = cache._ptrs()
-    _check(lib.sv_cache_read(kc, vc, tag, ks, vs, n_pages, page, _dense(t_offsets), n_rows, _dense(start), _dense(pages),
-                             pages.shape[1], B, P, cache.heads, cache.D, _tag(k), k_addr, k_stride, v_addr, v_stride, _dense(flags),
-                             _stream(stream)))
+    kc, vc, tag, ks, vs, n_pages, page = cache._args
+    _check(lib.sv_cache_read(kc, vc, tag, ks, vs, n_pages, page, offs, n_rows, first, table, max_pages, B, P, cache.heads, cache.D,
+                             _tag(k), k_addr, k_stride, v_addr, v_stride, _at(flags, device), _stream(stream)))
 
 
 def sv_chunk_attention_workspace_bytes(B, P, Hq, heads, D, dtype, max_pages, page):
     return int(lib.sv_chunk_attention_workspace_bytes(B, P, Hq, heads, D, dtype, max_pages, page))
 
 
+def _scratch(n, stream):
+    """n bytes of torch's memory on the stream of the call, which may hand it to a later call of that stream."""
+    if n == 0:
+        return None
+    if stream is None:
+        return torch.empty(n, dtype=torch.uint8, device="cuda")
+    with torch.cuda.stream(stream):
+        return torch.empty(n, dtype=torch.uint8, device="cuda")
+
+
 def sv_chunk_attention(cache, q, out, lengths, pages, t_offsets=None, P=None, scale=None, window=0, first=None, lse=None,
                        flags=None, ws=None, stream=None):
     """q, out: [B, P, Hq, D]; or [n_rows, Hq, D] with t_offsets [B+1] and P.  scale None: 1 / sqrt(D).  ws None: scratch is torch's."""
-    shape = q.shape
-    n_rows, B, P = _new_rows(shape[:-2], t_offsets, lengths, pages, P)
+    device, shape = _device(), q.shape
+    n_rows, B, P, max_pages, offs, start, table = _new_rows(shape, t_offsets, lengths, pages, P, cache, device)
     Hq, D = shape[-2:]
     if out.shape != shape or out.dtype != q.dtype or D != cache.D:
         raise SvError(SV_ERR_INVALID_ARG)
-    q_addr, q_stride = _heads(q)
-    o_addr, o_stride = _heads(out)
+    q_addr, q_stride = _heads(q, device)
+    o_addr, o_stride = _heads(out, device)
     if first is not None:
         _i32(first)
         _outputs((B,), first)
@@ -894,38 +917,38 @@ def sv_chunk_attention(cache, q, out, lengths, pages, t_offsets=None, P=None, sc
     if flags is not None:
         _i32(flags)
         _outputs((n_rows,), flags)
-    _here(q, out, cache.k, cache.v, cache.k_scale, cache.v_scale, lengths, pages, t_offsets, first, lse, flags, ws)
-    tag, max_pages = _tag(q), pages.shape[1]
+    dtype = _tag(q)
     if ws is None:
-        n = lib.sv_chunk_attention_workspace_bytes(B, P, Hq, cache.heads, D, tag, max_pages, cache.page)
-        if n > 0 and stream is None:
-            ws = torch.empty(n, dtype=torch.uint8, device="cuda")
-        elif n > 0:
-            with torch.cuda.stream(stream):
-                ws = torch.empty(n, dtype=torch.uint8, device="cuda")
-    kc, vc, c_tag, ks, vs, n_pages, page = cache._ptrs()
-    _check(lib.sv_chunk_attention(q_addr, q_stride, _dense(t_offsets), n_rows, _dense(lengths), _dense(first), _dense(pages),
-                                  max_pages, B, P, Hq, cache.heads, D, tag, kc, vc, c_tag, ks, vs, n_pages, page,
-                                  D ** -0.5 if scale is None else scale, window, o_addr, o_stride, _dense(lse), _dense(flags),
-                                  _dense(ws), 0 if ws is None else ws.numel(), _stream(stream)))
+        ws = _scratch(lib.sv_chunk_attention_workspace_bytes(B, P, Hq, cache.heads, D, dtype, max_pages, cache.page), stream)
+    kc, vc, tag, ks, vs, n_pages, page = cache._args
+    _check(lib.sv_chunk_attention(q_addr, q_stride, offs, n_rows, start, _at(first, device), table, max_pages, B, P, Hq, cache.heads, D,
+                                  dtype, kc, vc, tag, ks, vs, n_pages, page, D ** -0.5 if scale is None else scale, window, o_addr,
+                                  o_stride, _at(lse, device), _at(flags, device), _at(ws, device), 0 if ws is None else ws.numel(),
+                                  _stream(stream)))
 
 
-def sv_sample(z, u, token, logprob=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, flags=None, stream=None):
-    """z: [..., V]; u (float64), token (int32), logprob, flags: one entry per row."""
-    V = z.shape[-1]
-    rows = u.numel()
-    if u.dtype != torch.float64:
+def sv_sample_workspace_bytes(rows, V, dtype):
+    return int(lib.sv_sample_workspace_bytes(rows, V, dtype))
+
+
+def sv_sample(z, u, token, logprob=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, flags=None, ws=None, stream=None):
+    """z: [..., V]; u (float64), token (int32), logprob, flags: one entry per row.  ws None: scratch is torch's."""
+    device, V, rows = _device(), z.shape[-1], u.numel()
+    if u.dtype != torch.float64 or token.dtype not in _INT32:
         raise SvError(SV_ERR_DTYPE)
     if z.numel() != rows * V or token.numel() != rows:
         raise SvError(SV_ERR_INVALID_ARG)
-    _i32(token)
     if logprob is not None:
         _f32(logprob)
         _outputs((rows,), logprob)
     if flags is not None:
         _i32(flags)
         _outputs((rows,), flags)
-    _here(z, u, token, logprob, flags)
+    if z.get_device() != device:
+        _refuse(z, device)
     addr, stride = _strided(z)
-    _check(lib.sv_sample(addr, stride, rows, V, _tag(z), temperature, top_k, top_p, min_p, _dense(u), _dense(token), _dense(logprob),
-                         _dense(flags), _stream(stream)))
+    tag = _tag(z)
+    if ws is None:
+        ws = _scratch(lib.sv_sample_workspace_bytes(rows, V, tag), stream)
+    _check(lib.sv_sample(addr, stride, rows, V, tag, temperature, top_k, top_p, min_p, _at(u, device), _at(token, device),
+                         _at(logprob, device), _at(flags, device), _at(ws, device), 0 if ws is None else ws.numel(), _stream(stream)))

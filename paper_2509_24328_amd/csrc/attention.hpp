@@ -25,7 +25,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kStep = 32;              // keys of a step
-constexpr int kMinSteps = 8;           // steps of a workgroup that divides a row block's keys with others, at least
+constexpr int kMinSteps = 4;           // steps of a workgroup that divides a row block's keys with others, at least
 // Workgroups that the keys of a call are divided among: two to a compute unit, which is what the registers hold.  64 x 1 over 16384 bf16: 512
 // 713 us, 1024 725, 2048 729; 64 x 9 over 8192 in 8 bits: 210, 216, 235; 2048 over 6144: 499, 537, 572.
 constexpr int kTargetGroups = 512;

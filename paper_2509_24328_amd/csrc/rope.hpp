@@ -28,11 +28,36 @@ struct CosSin {
   double c, s;
 };
 
+// cos and sin of an angle, times the amplitude: n quarters of a turn and a rest within an eighth of one, formed with the product's own
+// rounding added back; the series of sine and cosine up to x^15 / 15! and x^16 / 16! (0.786^17 / 17! = 5e-17).  Good to 1e-15 and
+// the angle's own rounding, in 30 operations: the library's sincos, made for any angle, takes several hundred.
 __device__ __forceinline__ CosSin cos_sin(double angle, double amplitude) {
+  constexpr double kTurns = 0.15915494309189533576888376337251, kTurnsLo = -9.8393383375591e-18;   // 1 / (2 pi), and what that leaves
+  const double t = angle * kTurns, lo = __builtin_fma(angle, kTurns, -t) + angle * kTurnsLo;
+  const double n = __builtin_rint(4.0 * t);
+  const double x = (__builtin_fma(-0.25, n, t) + lo) * 6.283185307179586476925286766559, x2 = x * x;
+  double s = -1.0 / 1307674368000.0;
+  s = __builtin_fma(s, x2, 1.0 / 6227020800.0);
+  s = __builtin_fma(s, x2, -1.0 / 39916800.0);
+  s = __builtin_fma(s, x2, 1.0 / 362880.0);
+  s = __builtin_fma(s, x2, -1.0 / 5040.0);
+  s = __builtin_fma(s, x2, 1.0 / 120.0);
+  s = __builtin_fma(s, x2, -1.0 / 6.0);
+  s = __builtin_fma(s * x2, x, x);
+  double c = 1.0 / 20922789888000.0;
+  c = __builtin_fma(c, x2, -1.0 / 87178291200.0);
+  c = __builtin_fma(c, x2, 1.0 / 479001600.0);
+  c = __builtin_fma(c, x2, -1.0 / 3628800.0);
+  c = __builtin_fma(c, x2, 1.0 / 40320.0);
+  c = __builtin_fma(c, x2, -1.0 / 720.0);
+  c = __builtin_fma(c, x2, 1.0 / 24.0);
+  c = __builtin_fma(c, x2, -0.5);
+  c = __builtin_fma(c, x2, 1.0);
+  const int q = (int)((long long)n & 3);
+  const double a = q & 1 ? s : c, b = q & 1 ? c : s;     // magnitudes of cos and sin in the quarter
   CosSin r;
-  sincos(angle, &r.s, &r.c);
-  r.c *= amplitude;
-  r.s *= amplitude;
+  r.c = (q == 1 || q == 2 ? -a : a) * amplitude;
+  r.s = (q >= 2 ? -b : b) * amplitude;
   return r;
 }
 

@@ -42,6 +42,9 @@ struct SampleArgs {
   int32_t* token;
   float* logprob;
   uint32_t* flags;
+  // of rows that are read by more than one workgroup (null otherwise): every piece's mass and largest entry (+inf: a NaN)
+  double* piece_mass;                    // [rows, pieces]
+  float* piece_top;                      // [rows, pieces]
 };
 
 __device__ __forceinline__ uint32_t order_key(float f) {           // ascending
@@ -493,19 +496,18 @@ struct Draw {
 #pragma unroll
     for (int j = 0; j < kOwn; ++j) w[j] = (int)threadIdx.x * kOwn + j < groups ? sh.piece[threadIdx.x * kOwn + j] : 0.0;
     const int g = place_of(w, u, &W, &begin);
-    *token = in_pieces(g * group, min((g + 1) * group, pieces), begin, u * W, least);
+    *token = in_blocks(g * group * kPieceVecs, min((g + 1) * group, pieces) * kPieceVecs, begin, u * W, least);
     *total = W;
     return load_elem<DT>(row, *token);
   }
 
-  // The token at which the running mass, `before` ahead of piece p0, passes `at`, among pieces p0 .. p1 - 1; if it does not, the last kept one.
-  // A wavefront for each of a piece's eight vectors of 64 lanes.
-  __device__ __forceinline__ int in_pieces(int p0, int p1, double before, double at, float least) {
-    static_assert(kPieceVecs == kDrawWaves, "a wavefront for each vector of a piece");
+  // The token at which the running mass, `before` ahead of block b0, passes `at`, among blocks b0 .. b1 - 1 of 64 vectors; if it does not, the
+  // last kept one.  A wavefront for each block.
+  __device__ __forceinline__ int in_blocks(int b0, int b1, double before, double at, float least) {
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, nvec = a.V / EPV;
     int last_seen = -1;
-    for (int p = p0; p < p1; ++p) {
-      const int64_t i = ((int64_t)p * kPieceVecs + wave) * kWave + lane;
+    for (int b = b0; b < b1; b += kDrawWaves) {
+      const int64_t i = b + wave < b1 ? (int64_t)(b + wave) * kWave + lane : (int64_t)nvec + 1;
       double w[EPV], s = 0.0;
       float x[EPV];
 #pragma unroll
@@ -554,8 +556,75 @@ __device__ __forceinline__ void bad_row_out(const SampleArgs& a, int64_t r) {
   if (a.flags) a.flags[r] = SV_FLAG_BAD_ROW;
 }
 
-// No warps: a piece of the row for each wavefront in turn, weights relative to the piece's largest entry; one pass over the row.
+// A wavefront's piece of a row, vectors (PV piece + j) 64 + lane: its largest entry (+inf where a NaN is), and its mass relative to that.
+template <int DT, int PV>
+__device__ __forceinline__ float piece_of(const SampleArgs& a, const char* row, int piece, double* mass) {
+  constexpr int EPV = Elem<DT>::per_vec;
+  const int lane = threadIdx.x & (kWave - 1), nvec = a.V / EPV;
+  const int64_t base = (int64_t)piece * PV * kWave + lane;
+  u32x4 q[PV];
+#pragma unroll
+  for (int j = 0; j < PV; ++j)
+    if (base + j * kWave < nvec) q[j] = load_vec(row, (int)(base + j * kWave));
+  // (the entries past the last vector)
+  const int past = base <= nvec && nvec < base + PV * kWave && (nvec - base) % kWave == 0 ? a.V - nvec * EPV : 0;
+  float top = -INFINITY;
+  bool nan = false;
+#pragma unroll
+  for (int j = 0; j < PV; ++j) {
+    if (base + j * kWave >= nvec) continue;
+    float x[EPV];
+    unpack<DT>(q[j], x);
+#pragma unroll
+    for (int e = 0; e < EPV; ++e) {
+      top = fmaxf(top, x[e]);
+      nan |= x[e] != x[e];
+    }
+  }
+  for (int e = 0; e < past; ++e) {
+    const float x = load_elem<DT>(row, nvec * EPV + e);
+    top = fmaxf(top, x);
+    nan |= x != x;
+  }
+  top = wave_max_f32(top);
+  // (unpacked again below: kept as floats they take 64 registers)
+#pragma unroll
+  for (int j = 0; j < PV; ++j) asm volatile("" : "+v"(q[j]));
+  double s = 0.0;
+  if (top > -INFINITY) {
+#pragma unroll
+    for (int j = 0; j < PV; ++j) {
+      if (base + j * kWave >= nvec) continue;
+      float x[EPV];
+      unpack<DT>(q[j], x);
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) s += exp2_series(((double)x[e] - (double)top) * a.scale);
+      if constexpr (EPV == 8) __builtin_amdgcn_sched_barrier(0);   // (eight weights side by side are enough; four are not)
+    }
+    for (int e = 0; e < past; ++e) s += exp2_series(((double)load_elem<DT>(row, nvec * EPV + e) - (double)top) * a.scale);
+    s = wave_sum_f64(s);
+  }
+  *mass = s;
+  return __ballot(nan) ? INFINITY : top;
+}
+
+// Few long rows without warps: a wavefront for each of their pieces, ahead of sample_plain_kernel.
 template <int DT>
+__global__ void __launch_bounds__(256) sample_pieces_kernel(SampleArgs a, int rows, int pieces) {
+  const int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+  const int r = (int)(at / pieces), piece = (int)(at - (int64_t)r * pieces);
+  if (r >= rows) return;
+  double mass;
+  const float top = piece_of<DT, kPieceVecs>(a, a.z + r * a.z_stride, piece, &mass);
+  if ((threadIdx.x & (kWave - 1)) == 0) {
+    a.piece_mass[at] = mass;
+    a.piece_top[at] = top;
+  }
+}
+
+// No warps: masses of the pieces, from the sweep before or by the wavefronts in turn, one pass over the row; then the piece that holds u W.
+// PV: vectors of a lane in a piece; two where the row is so short that pieces of eight leave wavefronts without one.
+template <int DT, int PV>
 __global__ void __launch_bounds__(kDrawThreads, 2) sample_plain_kernel(SampleArgs a) {
   constexpr int EPV = Elem<DT>::per_vec;
   __shared__ DrawShared sh;
@@ -565,67 +634,37 @@ __global__ void __launch_bounds__(kDrawThreads, 2) sample_plain_kernel(SampleArg
   Team team{sh};
   Draw<DT> d{a, a.z + r * a.z_stride, sh, team, 0.0, {0.f, 0.f}};
   double u = a.u[r];
-  const int nvec = a.V / EPV, pieces = nvec / (kPieceVecs * kWave) + 1;
+  const int pieces = a.V / EPV / (PV * kWave) + 1;
   const int group = (pieces + kList - 1) / kList, groups = (pieces + group - 1) / group;
-  bool nan = false;
   float row_top = -INFINITY;
-  for (int g = wave; g < groups; g += kDrawWaves) {
-    float ref = -INFINITY;
-    double sum = 0.0;
-    for (int p = g * group; p < min((g + 1) * group, pieces); ++p) {
-      const int64_t base = (int64_t)p * kPieceVecs * kWave + lane;
-      u32x4 q[kPieceVecs];
-#pragma unroll
-      for (int j = 0; j < kPieceVecs; ++j)
-        if (base + j * kWave < nvec) q[j] = load_vec(d.row, (int)(base + j * kWave));
-      float tail[EPV], top = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < EPV; ++e) tail[e] = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < kPieceVecs; ++j) {
-        const int64_t i = base + j * kWave;
-        float x[EPV];
-        if (i < nvec) {
-          unpack<DT>(q[j], x);
-        } else if (i == nvec) {                          // the entries past the last vector
-#pragma unroll
-          for (int e = 0; e < EPV; ++e)
-            if (i * EPV + e < a.V) tail[e] = load_elem<DT>(d.row, (int)(i * EPV + e));
-        }
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) {
-          const float v = i < nvec ? x[e] : tail[e];
-          nan |= v != v;
-          top = fmaxf(top, v);
-        }
-      }
-      top = wave_max_f32(top);
-      if (top == -INFINITY) continue;
-      if (top > ref) {
-        sum = ref == -INFINITY ? 0.0 : sum * exp2_series(((double)ref - (double)top) * a.scale);
-        ref = top;
-      }
-      d.m = (double)ref;
-      double s = 0.0;
-#pragma unroll
-      for (int j = 0; j < kPieceVecs; ++j) {
-        const int64_t i = base + j * kWave;
-        if (i >= nvec) continue;
-        float x[EPV];
-        unpack<DT>(q[j], x);
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) s += d.weight(x[e]);
-      }
-      if (base <= nvec && nvec < base + kPieceVecs * kWave && (nvec - base) % kWave == 0) {
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) s += d.weight(tail[e]);
-      }
-      sum += wave_sum_f64(s);
+  if (a.piece_mass) {
+    for (int g = tid; g < groups; g += kDrawThreads) {
+      sh.piece[g] = a.piece_mass[r * pieces + g];
+      const float t = a.piece_top[r * pieces + g];
+      piece_top[g] = t;
+      row_top = fmaxf(row_top, t);
     }
-    if (lane == 0) { sh.piece[g] = sum; piece_top[g] = ref; }
-    row_top = fmaxf(row_top, ref);
+    row_top = wave_max_f32(row_top);
+  } else {
+    for (int g = wave; g < groups; g += kDrawWaves) {
+      float ref = -INFINITY;
+      double sum = 0.0;
+      for (int p = g * group; p < min((g + 1) * group, pieces); ++p) {
+        double s;
+        const float top = piece_of<DT, PV>(a, d.row, p, &s);
+        if (top == -INFINITY) continue;
+        if (top > ref) {
+          sum = ref == -INFINITY ? 0.0 : sum * exp2_series(((double)ref - (double)top) * a.scale);
+          ref = top;
+        } else {
+          s *= exp2_series(((double)top - (double)ref) * a.scale);
+        }
+        sum += s;
+      }
+      if (lane == 0) { sh.piece[g] = sum; piece_top[g] = ref; }
+      row_top = fmaxf(row_top, ref);
+    }
   }
-  if (__ballot(nan)) row_top = INFINITY;
   if (lane == 0) sh.wave_top[wave] = row_top;
   __syncthreads();
   float top = -INFINITY;
@@ -642,7 +681,7 @@ __global__ void __launch_bounds__(kDrawThreads, 2) sample_plain_kernel(SampleArg
     w[j] = i < groups && sh.piece[i] > 0.0 ? sh.piece[i] * d.weight(piece_top[i]) : 0.0;
   }
   const int g = d.place_of(w, u, &W, &begin);
-  const int token = d.in_pieces(g * group, min((g + 1) * group, pieces), begin, u * W, -INFINITY);
+  const int token = d.in_blocks(g * group * PV, min((g + 1) * group, pieces) * PV, begin, u * W, -INFINITY);
   if (tid == 0) {
     a.token[r] = token;
     if (a.logprob) a.logprob[r] = (float)(((double)load_elem<DT>(d.row, token) - d.m) * a.inv_t - log(W));
@@ -735,12 +774,13 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_kernel(SampleArgs a) {
     }
   }
   for (int k = n_keys + tid; k < ((n_keys + 7) & ~7); k += kDrawThreads) vec_key[k] = 0;
-  sh.lane_key[tid] = (uint16_t)(order_key(mine) >> 16);
+  const uint32_t lane_key = order_key(mine) >> 16;
+  sh.lane_key[tid] = (uint16_t)lane_key;
   {
-    const float hi = wave_max_f32(nan ? INFINITY : mine), lo = -wave_max_f32(-mine);
+    const float hi = wave_max_f32(nan ? INFINITY : mine), lo = -wave_max_f32(-(float)lane_key);
     if (lane == 0) {
       sh.wave_top[wave] = __ballot(nan) ? INFINITY : hi;
-      sh.wave_low[wave] = order_key(lo) >> 16;
+      sh.wave_low[wave] = (uint32_t)lo;
     }
   }
   __syncthreads();
@@ -778,7 +818,7 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_kernel(SampleArgs a) {
       const uint32_t probe = t | (1u << bit);
       const int c = count(probe);
       if (c >= want) t = probe;
-      if (c >= want && c <= want + want / 4) break;
+      if (c >= want && c <= want + (want < 40 ? 16 : want / 8)) break;
     }
     return t;
   };
@@ -820,21 +860,45 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_kernel(SampleArgs a) {
       tau = select(low_key, top_key, want, lanes) << 16;
       if (weigh && tau > min_key) {
         // a nucleus that the lanes' maxima above tau are far from filling is deeper than their list
-        const double reached = team.sum((uint32_t)sh.lane_key[tid] >= (tau >> 16) ? (double)d.fast.weight(mine - top) : 0.0);
-        if (reached < 0.7 * a.top_p * all) continue;
+        const double reached = team.sum(lane_key >= (tau >> 16) ? (double)d.fast.weight(mine - top) : 0.0);
+        if (reached < 0.85 * a.top_p * all) continue;
       }
     } else if (want > 0 && want <= n_keys) {
-      auto vectors = [&](uint32_t probe) {
-        int c = 0;
-        for (int k = 8 * tid; k < n_keys; k += 8 * kDrawThreads) {
-          const u32x4 q = *reinterpret_cast<const u32x4*>(vec_key + k);
+      // three probes a step
+      uint32_t lo = low_key, hi = top_key + 1;           // `want` vectors reach lo, fewer reach hi
+      for (bool first = true; hi - lo > 1; first = false) {
+        const uint32_t step = max((hi - lo) / 4, 1u);
+        uint32_t p[3];
+        int c[3] = {0, 0, 0};
+        double unused[3];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) c += ((q[e / 2] >> (16 * (e % 2))) & 0xffffu) >= probe;
+        for (int k = 0; k < 3; ++k) p[k] = first ? (k == 0 ? lo : lo + (hi - lo) * k / 3) : min(lo + (k + 1) * step, hi);
+        for (int k = 8 * tid; k < n_keys; k += 8 * kDrawThreads) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(vec_key + k);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t key = (x[e / 2] >> (16 * (e % 2))) & 0xffffu;
+#pragma unroll
+            for (int n = 0; n < 3; ++n) c[n] += key >= p[n];
+          }
         }
-        return team.count(wave_sum_i32(c));
-      };
-      const uint32_t from = low_key > 0 && vectors(low_key) >= want ? low_key : 0;
-      tau = select(from, top_key, want, vectors) << 16;
+        // (two counts in a word: of 64 lanes with at most 80 keys each)
+        const int both = wave_sum_i32(c[0] | (c[1] << 16));
+        c[0] = both & 0xffff;
+        c[1] = both >> 16;
+        c[2] = wave_sum_i32(c[2]);
+        team.template sums<3, false>(unused, c);
+        if (first && c[0] < want) { hi = lo; lo = 0; continue; }   // (not even the lowest of the lanes' maxima is reached by as many)
+        int reached = n_keys;
+#pragma unroll
+        for (int k = 2; k >= 0; --k) {
+          if (p[k] >= hi) continue;
+          if (c[k] >= want) { lo = p[k]; reached = c[k]; break; }
+          hi = p[k];
+        }
+        if (reached <= want + want / 8) break;
+      }
+      tau = lo << 16;
     }
     tau = max(tau, none);
     if (!use_k) tau = max(tau, min_key);                 // (the K-th value may lie below what min-p keeps)
@@ -1028,11 +1092,25 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_kernel(SampleArgs a) {
   }
 }
 
+// Whether rows without warps are read by more than one workgroup each: a compute unit forms 30 weights in a nanosecond, so a second launch
+// (4 us) pays for long rows that leave most of the card idle.  One launch / two, us: bf16 64 x 16384 15.4 / 17.4, 64 x 32000 17.6 / 17.3, 64 x 152064
+// 58 / 26, 192 x 152064 67 / 52, 256 x 152064 69 / 68.
+inline bool sample_splits(int rows, int V) { return rows <= 192 && V >= 32000 && V <= (1 << 21); }
+inline int sample_pieces(int V, int e) { return V / (16 / e) / (kPieceVecs * kWave) + 1; }
+inline size_t sample_top_at(int rows, int V, int e) { return ws_round((size_t)rows * sample_pieces(V, e) * 8); }
+
 }  // namespace sv
+
+extern "C" size_t sv_sample_workspace_bytes(int rows, int V, int dtype) {
+  const int e = sv::elem_bytes(dtype);
+  if (rows < 1 || V < 1 || V > (1 << 24) || e == 0) return 0;
+  if (!sv::sample_splits(rows, V)) return 0;
+  return sv::sample_top_at(rows, V, e) + sv::ws_round((size_t)rows * sv::sample_pieces(V, e) * 4);
+}
 
 extern "C" int sv_sample(const void* z, int64_t z_stride, int rows, int V, int dtype, float temperature, int top_k, float top_p,
                          float min_p, const double* u, int32_t* token, float* logprob_or_null, uint32_t* flags_or_null,
-                         sv_stream_t stream) {
+                         void* ws_or_null, size_t ws_bytes, sv_stream_t stream) {
   using namespace sv;
   const int e = elem_bytes(dtype);
   SV_REQUIRE(e != 0, SV_ERR_DTYPE);
@@ -1048,8 +1126,21 @@ extern "C" int sv_sample(const void* z, int64_t z_stride, int rows, int V, int d
   const int vectors = (V + 16 / e - 1) / (16 / e), share = (vectors + kMaxKeys - 1) / kMaxKeys;
   SampleArgs a{static_cast<const char*>(z), z_stride * e, V, top_k > 0 && top_k < V ? top_k : 0, share, kLog2e / (double)temperature,
                sc.inv_t, top_p < 1.f ? (double)top_p : 1.0, min_p > 0.f ? __builtin_log2((double)min_p) : -INFINITY, u, token,
-               logprob_or_null, flags_or_null};
+               logprob_or_null, flags_or_null, nullptr, nullptr};
   const bool plain = a.top_k == 0 && a.top_p >= 1.0 && min_p == 0.f;
+  const int pieces = sample_pieces(V, e);
+  bool shorter = pieces < 2 * kDrawWaves;
+  if (ws_or_null && sample_splits(rows, V)) {
+    SV_REQUIRE(is_aligned(ws_or_null, kWsAlign) && ws_bytes >= sv_sample_workspace_bytes(rows, V, dtype), SV_ERR_WORKSPACE);
+    if (plain) {
+      a.piece_mass = static_cast<double*>(ws_or_null);
+      a.piece_top = reinterpret_cast<float*>(static_cast<char*>(ws_or_null) + sample_top_at(rows, V, e));
+      shorter = false;
+      const dim3 grid((unsigned)(((long long)rows * pieces + 3) / 4));
+      if (dtype == SV_F32) hipLaunchKernelGGL(sample_pieces_kernel<DT_F32>, grid, dim3(256), 0, as_stream(stream), a, rows, pieces);
+      else hipLaunchKernelGGL(sample_pieces_kernel<DT_BF16>, grid, dim3(256), 0, as_stream(stream), a, rows, pieces);
+    }
+  }
   const size_t lds = plain ? 0 : ((size_t)(vectors + share - 1) / share + 7) / 8 * 16;
   in_launches(rows, kDrawThreads, [&](long long first, dim3 grid) {
     SampleArgs b = a;
@@ -1059,8 +1150,13 @@ extern "C" int sv_sample(const void* z, int64_t z_stride, int rows, int V, int d
     if (b.logprob) b.logprob += first;
     if (b.flags) b.flags += first;
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kDrawThreads), lds, as_stream(stream), b); };
-    if (dtype == SV_F32) { if (plain) go(sample_plain_kernel<DT_F32>); else go(sample_kernel<DT_F32>); }
-    else { if (plain) go(sample_plain_kernel<DT_BF16>); else go(sample_kernel<DT_BF16>); }
+    if (!plain) {
+      if (dtype == SV_F32) go(sample_kernel<DT_F32>); else go(sample_kernel<DT_BF16>);
+    } else if (shorter) {
+      if (dtype == SV_F32) go(sample_plain_kernel<DT_F32, 2>); else go(sample_plain_kernel<DT_BF16, 2>);
+    } else {
+      if (dtype == SV_F32) go(sample_plain_kernel<DT_F32, kPieceVecs>); else go(sample_plain_kernel<DT_BF16, kPieceVecs>);
+    }
   });
   return launch_status();
 }

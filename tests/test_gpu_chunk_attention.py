@@ -192,7 +192,7 @@ def test_long_sequences_are_divided(dtype, kind):
     i32 = lambda v: torch.as_tensor(v, dtype=torch.int32).cuda()
     out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
     le, pg, of = i32(lengths), i32(pages), i32(offs)
-    c = cache._ptrs()
+    c = cache._args
     assert L.sv_chunk_attention(q.data_ptr(), 8 * 128, of.data_ptr(), q.shape[0], le.data_ptr(), None, pg.data_ptr(), pages.shape[1], 5, 3, 8, 2,
                                 128, int(dtype == BF16), c[0], c[1], c[2], c[3], c[4], c[5], c[6], 128 ** -0.5, 0, out.data_ptr(), 8 * 128,
                                 lse.data_ptr(), None, None, 0, torch.cuda.current_stream().cuda_stream) == 0
