@@ -12,19 +12,17 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttnArgs a) {
   const int64_t bi = at / a.Hq;
   const int i = (int)(bi % a.rows.P), b = (int)(bi / a.rows.P);
   if (b >= a.rows.B) return;
-  const Sequence s = sequence_of(a, b);
-  if (i >= s.n) return;
   const int h = hq / a.group, rho = i * a.group + hq - h * a.group, tile = rho / a.tile_rows;
   const int item = (b * a.pages.heads + h) * a.tiles + tile;
-  const int parts = a.n_split[item];
-  if (parts <= 1) return;
   const int64_t part0 = (int64_t)item * a.splits * a.tile_rows + (rho - tile * a.tile_rows);
-  float m = -INFINITY, l = 0.f;
-  if (lane < parts) {
-    const int64_t p = part0 + (int64_t)lane * a.tile_rows;
-    m = a.part_ml[2 * p];
-    l = a.part_ml[2 * p + 1];
-  }
+  // all asked for together: how many parts there are, whether the row is there, and maxima and sums of as many parts as there may be
+  const int64_t p = part0 + (int64_t)min(lane, a.splits - 1) * a.tile_rows;
+  float m = a.part_ml[2 * p], l = a.part_ml[2 * p + 1];
+  const int parts = a.n_split[item];
+  const Sequence s = sequence_of(a, b);
+  if (i >= s.n || parts <= 1) return;
+  m = lane < parts ? m : -INFINITY;
+  l = lane < parts ? l : 0.f;
   const float top = wave_max_f32(m);
   const float f = m == top ? 1.f : exp2_fast(m - top);
   const double total = wave_sum_f64(lane < parts ? (double)l * f : 0.0);
@@ -36,9 +34,16 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttnArgs a) {
   char* to = a.out + (int64_t)(s.row0 + i) * a.out_stride;
   for (int col = 4 * lane; col < a.D; col += 4 * kWave) {
     f32x4 o{0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < parts; ++k) {
-      typedef f32x4 vec __attribute__((aligned(4)));
-      o += *reinterpret_cast<const vec*>(a.part_o + (part0 + (int64_t)k * a.tile_rows) * a.D + col) * lane_f32(f, k);
+    typedef f32x4 vec __attribute__((aligned(4)));
+    const float* from = a.part_o + part0 * a.D + col;
+    for (int k0 = 0; k0 < parts; k0 += 8) {              // (eight parts under way together)
+      f32x4 p[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k0 + k < parts) p[k] = *reinterpret_cast<const vec*>(from + (int64_t)(k0 + k) * a.tile_rows * a.D);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k0 + k < parts) o += p[k] * lane_f32(f, k0 + k);
     }
     o *= inv;
     if constexpr (ET == SV_F32) {

@@ -80,6 +80,7 @@ __global__ void __launch_bounds__(kRopeThreads) cache_write_kernel(CacheArgs a) 
   __shared__ int64_t sh_row[4];
   const int r0 = blockIdx.x * a.tokens, half = a.sh.half, D = a.sh.D;
   const int nt = min(a.tokens, a.rows.n_rows - r0);
+  const double freq0 = half && (int)threadIdx.x < nt * half ? a.freq[threadIdx.x % half] : 0.0;   // (asked for ahead of the places)
   if (threadIdx.x < kWave)
     for (int t = 0; t < nt; ++t) {
       const Place p = place_of_row(a.rows, r0 + t);
@@ -95,7 +96,7 @@ __global__ void __launch_bounds__(kRopeThreads) cache_write_kernel(CacheArgs a) 
   if (half) {
     for (int k = threadIdx.x; k < nt * half; k += kRopeThreads) {
       const int t = k / half;
-      if (sh_b[t] >= 0) cs[k] = cos_sin((double)sh_pos[t] * a.freq[k - t * half], a.amplitude);
+      if (sh_b[t] >= 0) cs[k] = cos_sin((double)sh_pos[t] * (k < kRopeThreads ? freq0 : a.freq[k - t * half]), a.amplitude);
     }
     __syncthreads();
   }

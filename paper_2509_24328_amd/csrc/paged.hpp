@@ -33,23 +33,31 @@ struct Place {
 };
 
 // The sequence and position of row r (the same in all lanes of the wavefront, all of them active): the sequences that end at or before
-// r are counted, a lane for each, so that a long batch takes one load and not a chain of them.
+// r are counted, a lane for each, and its beginning and start come from the lane that holds them: one load's time, not a chain of
+// them.
 __device__ __forceinline__ Place place_of_row(const Rows& rows, int r) {
-  int b, i;
+  int b, i, s;
   if (rows.offsets) {
-    b = 0;
-    for (int k = threadIdx.x & (kWave - 1); k - (int)(threadIdx.x & (kWave - 1)) < rows.B; k += kWave) {
-      const bool ends = k < rows.B && rows.offsets[k + 1] <= r;
-      b += __popcll(__ballot(ends));
+    const int lane = threadIdx.x & (kWave - 1);
+    int k0 = 0, begin = 0, start = 0, n = 0;
+    for (; k0 < rows.B; k0 += kWave) {
+      const int k = k0 + lane;
+      const bool in = k < rows.B;
+      begin = in ? rows.offsets[k] : 0;
+      start = in ? rows.start[k] : 0;
+      n = __popcll(__ballot(in && rows.offsets[k + 1] <= r));
+      if (n < kWave) break;
     }
+    b = k0 + n;
     if (b >= rows.B) return {-1, 0};
-    i = r - rows.offsets[b];
+    i = r - __builtin_amdgcn_readlane(begin, n);
+    s = __builtin_amdgcn_readlane(start, n);
   } else {
     b = r / rows.P;
     i = r - b * rows.P;
+    s = rows.start[b];
   }
   if (i < 0 || i >= rows.P) return {-1, 0};
-  const int s = rows.start[b];
   // (a start below 0, or one so large that the position leaves 32 bits, is in no page)
   return {b, s < 0 || s > 0x7fffffff - i ? -1 : s + i};
 }

@@ -587,9 +587,10 @@ __device__ __forceinline__ float piece_of(const SampleArgs& a, const char* row, 
     nan |= x != x;
   }
   top = wave_max_f32(top);
-  // (unpacked again below: kept as floats they take 64 registers)
+  // (bfloat16 unpacked again below: kept as floats they take 64 registers)
 #pragma unroll
-  for (int j = 0; j < PV; ++j) asm volatile("" : "+v"(q[j]));
+  for (int j = 0; j < PV; ++j)
+    if constexpr (EPV == 8) asm volatile("" : "+v"(q[j]));
   double s = 0.0;
   if (top > -INFINITY) {
 #pragma unroll
@@ -818,7 +819,7 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_kernel(SampleArgs a) {
       const uint32_t probe = t | (1u << bit);
       const int c = count(probe);
       if (c >= want) t = probe;
-      if (c >= want && c <= want + (want < 40 ? 16 : want / 8)) break;
+      if (c >= want && c <= want + (want < 40 ? 8 : want / 8)) break;
     }
     return t;
   };
