@@ -81,12 +81,15 @@ struct AttnPlan {
   size_t bytes;
 };
 
-// How the rows of a call are laid out over workgroups: one block of up to 16 or 32 rows to a wavefront, up to four of them.
-inline AttnPlan attention_plan(int B, int P, int Hq, int heads, int D, int dtype, int64_t max_tokens) {
+// How the rows of a call are laid out over workgroups: one block of up to 16, 32 or 48 rows to a wavefront, up to four of them.
+inline AttnPlan attention_plan(int B, int P, int Hq, int heads, int D, int dtype, bool f8, int64_t max_tokens) {
   AttnPlan p{};
   const int64_t rows = (int64_t)P * (Hq / heads);
   const bool wide = dtype == SV_F32 || D > 128;             // (outputs of one block of rows fill a wavefront's registers)
   p.nt = wide || rows <= 16 ? 1 : 2;
+  // (8-bit keys, converted once by one wavefront of 48 rows and not by two of 32: 64 x 9 with 4 heads to one over 8192 tokens, all nine
+  // there, 320 us and 414; one to nine there 214 and 219.  Keys of 16 bits do not leave the registers.)
+  if (f8 && p.nt == 2 && rows > 32 && rows <= 48) p.nt = 3;
   p.tile_rows = 16 * p.nt * (rows <= 16 * p.nt ? 1 : (rows <= 32 * p.nt ? 2 : 4));
   const int64_t tiles = (rows + p.tile_rows - 1) / p.tile_rows;
   p.items = (int64_t)B * heads * tiles;
@@ -114,7 +117,9 @@ extern "C" size_t sv_chunk_attention_workspace_bytes(int B, int P, int Hq, int h
   if (B < 1 || P < 1 || heads < 1 || Hq < heads || Hq % heads != 0 || Hq > SV_HEADS_MAX || D < 8 || D > SV_ATTENTION_HEAD_MAX || D % 8 != 0 ||
       elem_bytes(dtype) == 0 || max_pages < 1 || page < 1 || page > SV_PAGE_MAX || (long long)B * P > kMaxRows / Hq)
     return 0;
-  return attention_plan(B, P, Hq, heads, D, dtype, (int64_t)max_pages * page).bytes;
+  const size_t own = attention_plan(B, P, Hq, heads, D, dtype, false, (int64_t)max_pages * page).bytes;
+  const size_t f8 = attention_plan(B, P, Hq, heads, D, dtype, true, (int64_t)max_pages * page).bytes;
+  return own > f8 ? own : f8;
 }
 
 extern "C" int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t* t_offsets_or_null, int n_rows,
@@ -146,7 +151,7 @@ extern "C" int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t
                  (!f8 || (is_aligned(k_scale_or_null, 4) && is_aligned(v_scale_or_null, 4))),
              SV_ERR_ALIGN);
   const bool whole = whole_tiles(D, page);
-  AttnPlan p = attention_plan(B, P, Hq, heads, D, dtype, (int64_t)max_pages * page);
+  AttnPlan p = attention_plan(B, P, Hq, heads, D, dtype, f8, (int64_t)max_pages * page);
   if (!ws_or_null) p.splits = 1;
   else if (p.splits > 1) SV_REQUIRE(is_aligned(ws_or_null, kWsAlign) && ws_bytes >= p.bytes, SV_ERR_WORKSPACE);
   SV_REQUIRE(p.items * p.splits <= 0xffffffffLL / (kAttnWaves * kWave), SV_ERR_TOO_LARGE);

@@ -875,6 +875,7 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, (DPAD == 256 || (ET == SV_F
   const int rows = work_of(a, k);
   if (rows <= 0) return;
   if (NT > 1 && rows <= 16) attend<ET, CT, DPAD, 1, WHOLE>(a, k, shared);
+  else if (NT > 2 && rows <= 32) attend<ET, CT, DPAD, 2, WHOLE>(a, k, shared);
   else attend<ET, CT, DPAD, NT, WHOLE>(a, k, shared);
 }
 
@@ -1068,6 +1069,12 @@ void launch_attention_of(const AttnArgs& a, const AttnLaunch& t) {
   if constexpr (NT == 2) {
     if (t.tile) {
       if (t.whole) go(attention_tile_kernel<CT, DPAD, true>); else go(attention_tile_kernel<CT, DPAD, false>);
+      return;
+    }
+  }
+  if constexpr (NT == 2 && CT == SV_F8) {
+    if (t.nt == 3) {
+      if (t.whole) go(attention_kernel<ET, CT, DPAD, 3, true>); else go(attention_kernel<ET, CT, DPAD, 3, false>);
       return;
     }
   }

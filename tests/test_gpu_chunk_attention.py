@@ -178,6 +178,18 @@ def test_pages_that_are_not_there(dtype, kind, page):
     check(cache, q, run(cache, q, lengths, pages, offs, T), lengths, pages, offs, T)
 
 
+@pytest.mark.parametrize("T, group", [(9, 4), (12, 4), (6, 8), (33, 1), (7, 7)])
+@pytest.mark.parametrize("D, page", [(128, 16), (112, 24), (64, 16)])
+@pytest.mark.parametrize("kind", [F8, BF16])
+def test_rows_between_two_blocks_and_four(kind, D, page, T, group):
+    """33 to 49 rows to a head, and fewer in the sequences that have fewer tokens; lengths that are divided and lengths that are not."""
+    lengths, counts = [1500, 3, 0, 700, 260], [T, max(1, T // 2), T, 1, T - 1]
+    cache, pages = make(lengths, [T] * 5, 2, D, page, kind, seed=T)
+    offs = np.concatenate([[0], np.cumsum(counts)]).tolist()
+    q = queries(offs[-1], 2 * group, D, BF16)
+    check(cache, q, run(cache, q, lengths, pages, offs, T), lengths, pages, offs, T)
+
+
 @pytest.mark.parametrize("dtype, kind", TYPES)
 def test_long_sequences_are_divided(dtype, kind):
     """Lengths from 1 to 4000 in one call, with and without scratch: the parts of a long one are joined."""
