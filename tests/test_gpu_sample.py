@@ -150,6 +150,14 @@ def test_rows_beyond_32_bits():
     assert np.array_equal(token[-3:].cpu().numpy(), want.numpy())
 
 
+@pytest.mark.parametrize("V, dtype", [(170001, F32), (330001, BF16), (500009, F32)])
+def test_vocabularies_that_share_maxima(V, dtype):
+    """More vectors than there are maxima kept of them."""
+    z, u = logits(3, V, dtype, 12)
+    for warp in WARPS[:4] + WARPS[5:10]:
+        check(z, u, **warp)
+
+
 def test_no_rows():
     P.sv_sample(torch.empty((0, 8), device="cuda"), torch.empty(0, dtype=torch.float64, device="cuda"),
                 torch.empty(0, dtype=torch.int32, device="cuda"))
