@@ -190,6 +190,31 @@ def test_rows_between_two_blocks_and_four(kind, D, page, T, group):
     check(cache, q, run(cache, q, lengths, pages, offs, T), lengths, pages, offs, T)
 
 
+@pytest.mark.parametrize("T", [1, 3, 7, 12])
+@pytest.mark.parametrize("D, page", [(128, 16), (112, 24), (64, 16), (40, 8)])
+@pytest.mark.parametrize("kind", [F8, BF16])
+def test_many_sequences(kind, D, page, T):
+    """270 heads of sequences that differ in length, some with no new tokens, some behind their pages, some with a window or a first position
+    that leaves nothing; more sequences than a wavefront has lanes."""
+    B, g = 135, torch.Generator().manual_seed(T)
+    lengths = (torch.rand(B, generator=g) ** 6 * 1500).to(torch.int32).tolist()
+    counts = torch.randint(0, T + 1, (B,), generator=g).tolist()
+    lengths[:4], counts[:4] = [0, 1400, 5, 31], [T, T, 0, 1]
+    cache, pages = make(lengths, [T] * B, 2, D, page, kind, seed=T)
+    offs = np.concatenate([[0], np.cumsum(counts)]).tolist()
+    q = queries(offs[-1], 8, D, BF16)
+    got = run(cache, q, lengths, pages, offs, T)
+    check(cache, q, got, lengths, pages, offs, T)
+    again = run(cache, q, lengths, pages, offs, T)
+    assert all(torch.equal(x.nan_to_num(3.0), y.nan_to_num(3.0)) for x, y in zip(got, again))
+    lengths[7], lengths[90] = -1, 100000
+    pages[1, 3] = -2
+    first = [0] * B
+    first[1], first[9], first[134] = 900, 5000, lengths[134]
+    for window in (0, 50):
+        check(cache, q, run(cache, q, lengths, pages, offs, T, window, first), lengths, pages, offs, T, window, first)
+
+
 @pytest.mark.parametrize("dtype, kind", TYPES)
 def test_long_sequences_are_divided(dtype, kind):
     """Lengths from 1 to 4000 in one call, with and without scratch: the parts of a long one are joined."""
