@@ -75,7 +75,7 @@ __device__ __forceinline__ void write_f8(const void* row, const RopeShape& sh, c
 template <int DT, bool PAIRS, bool F8>
 __global__ void __launch_bounds__(kRopeThreads) cache_write_kernel(CacheArgs a) {
   constexpr int EPV = Elem<DT>::per_vec;
-  extern __shared__ CosSin cs[];                       // [tokens][half]
+  extern __shared__ CosSin cs[];                       // [tokens][pitch]
   __shared__ int sh_b[4], sh_pos[4];
   __shared__ int64_t sh_row[4];
   const int r0 = blockIdx.x * a.tokens, half = a.sh.half, D = a.sh.D;
@@ -96,7 +96,9 @@ __global__ void __launch_bounds__(kRopeThreads) cache_write_kernel(CacheArgs a) 
   if (half) {
     for (int k = threadIdx.x; k < nt * half; k += kRopeThreads) {
       const int t = k / half;
-      if (sh_b[t] >= 0) cs[k] = cos_sin((double)sh_pos[t] * (k < kRopeThreads ? freq0 : a.freq[k - t * half]), a.amplitude);
+      if (sh_b[t] >= 0)
+        cs[t * a.sh.pitch + angle_at<EPV>(k - t * half)] =
+            cos_sin((double)sh_pos[t] * (k < kRopeThreads ? freq0 : a.freq[k - t * half]), a.amplitude);
     }
     __syncthreads();
   }
@@ -106,7 +108,7 @@ __global__ void __launch_bounds__(kRopeThreads) cache_write_kernel(CacheArgs a) 
     const int t = k / H, h = k - t * H;
     if (sh_b[t] < 0) continue;
     const int64_t r = r0 + t;
-    const CosSin* c = cs + t * half;
+    const CosSin* c = cs + t * a.sh.pitch;
     if (h < a.Hq) {
       const char* from = a.q + r * a.q_stride + (int64_t)h * D * e_in;
       char* to = a.q_out + r * a.q_out_stride + (int64_t)h * D * e_in;
@@ -263,7 +265,7 @@ extern "C" int sv_cache_write(const void* k, int64_t k_stride, const void* v, in
                     rope_shape(D, 0, dtype), (double)amplitude, static_cast<char*>(k_cache), static_cast<char*>(v_cache),
                     k_scale_or_null, v_scale_or_null, flags_or_null};
   const dim3 grid((n_rows + a.tokens - 1) / a.tokens);
-  const size_t lds = (size_t)a.tokens * (rot / 2) * sizeof(CosSin);
+  const size_t lds = (size_t)a.tokens * a.sh.pitch * sizeof(CosSin);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kRopeThreads), lds, as_stream(stream), a); };
   const bool pairs = rot > 0 && layout == SV_ROPE_PAIRS, f8 = cache_dtype == SV_F8;
   if (dtype == SV_F32) {

@@ -19,11 +19,11 @@ struct RopeArgs {
 // memory: each column is read once and written once.
 template <int DT, bool PAIRS>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeArgs a) {
-  extern __shared__ CosSin cs[];                       // [tokens][half]
+  extern __shared__ CosSin cs[];                       // [tokens][pitch]
   const int t0 = blockIdx.x * a.tokens, nt = min(a.tokens, a.n - t0), half = a.sh.half;
   for (int k = threadIdx.x; k < nt * half; k += kRopeThreads) {
     const int t = k / half;
-    cs[k] = cos_sin((double)a.positions[t0 + t] * a.freq[k - t * half] * a.sign, a.amplitude);
+    cs[t * a.sh.pitch + angle_at<Elem<DT>::per_vec>(k - t * half)] = cos_sin((double)a.positions[t0 + t] * a.freq[k - t * half] * a.sign, a.amplitude);
   }
   __syncthreads();
   const int lane = threadIdx.x % kRopeLanes;
@@ -32,7 +32,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeArgs a) {
     if (a.positions[t0 + t] < 0) continue;
     const char* row = a.x + (t0 + t) * a.x_stride + (int64_t)h * a.head_bytes;
     char* to = a.out + (t0 + t) * a.out_stride + (int64_t)h * a.head_bytes;
-    turn_head<DT, PAIRS>(row, a.sh, cs + t * half, lane, a.in_place,
+    turn_head<DT, PAIRS>(row, a.sh, cs + t * a.sh.pitch, lane, a.in_place,
                          [&](int at, int n, const float (&f)[Elem<DT>::per_vec]) { store_some<DT>(to, at, n, f); });
   }
 }
@@ -90,7 +90,7 @@ extern "C" int sv_rope(const void* x, int64_t x_stride, const int32_t* positions
              // four tokens share a workgroup's start where every compute unit has several workgroups anyway
              n >= 4096 ? 4 : 1, rope_shape(D, rot, dtype), (double)amplitude, inverse ? -1.0 : 1.0, x == out};
   const dim3 grid((n + a.tokens - 1) / a.tokens);
-  const size_t lds = (size_t)a.tokens * (rot / 2) * sizeof(CosSin);
+  const size_t lds = (size_t)a.tokens * a.sh.pitch * sizeof(CosSin);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kRopeThreads), lds, as_stream(stream), a); };
   if (dtype == SV_F32) {
     if (layout == SV_ROPE_PAIRS) go(rope_kernel<DT_F32, true>); else go(rope_kernel<DT_F32, false>);

@@ -18,10 +18,13 @@ constexpr int kRopeGroups = kRopeThreads / kRopeLanes;
 // What of a head is turned, by vectors of EPV elements: `turns` chunks of EPV pairs, `copies` chunks of EPV columns.
 struct RopeShape {
   int D, half, turns, copies;
-};
+  int pitch;                         // angles of a token in LDS, with a gap after every vector's: lanes read vectors' angles side by side,
+};                                   // and without gaps all from the same banks (64 x 9 tokens of 48 heads into 8 bits 9.5 us and 8.1; 16384 x 32 60 and 58)
+template <int EPV>
+__device__ __forceinline__ int angle_at(int j) { return j + j / EPV; }
 inline RopeShape rope_shape(int D, int rot, int dtype) {
   const int epv = 16 / elem_bytes(dtype), half = rot / 2;
-  return RopeShape{D, half, (half + epv - 1) / epv, (D - rot + epv - 1) / epv};
+  return RopeShape{D, half, (half + epv - 1) / epv, (D - rot + epv - 1) / epv, half + (half - 1) / epv};
 }
 
 struct CosSin {
@@ -102,7 +105,7 @@ __device__ __forceinline__ void store_some(void* row, int at, int n, const float
   }
 }
 
-// One head, by the lanes of a group (lane: 0 .. kRopeLanes - 1).  cs: the token's angles, `half` of them.  put(column, count, values)
+// One head, by the lanes of a group (lane: 0 .. kRopeLanes - 1).  cs: the token's angles, at angle_at.  put(column, count, values)
 // is called for every chunk, with float32 values; columns that stay are passed on unchanged, unless skip_copies.
 template <int DT, bool PAIRS, class Put>
 __device__ __forceinline__ void turn_head(const void* row, const RopeShape& sh, const CosSin* cs, int lane, bool skip_copies,
@@ -110,6 +113,7 @@ __device__ __forceinline__ void turn_head(const void* row, const RopeShape& sh, 
   constexpr int EPV = Elem<DT>::per_vec;
   for (int c = lane; c < sh.turns; c += kRopeLanes) {
     const int j = c * EPV, n = min(EPV, sh.half - j);          // pairs j .. j + n - 1
+    const CosSin* at_j = cs + angle_at<EPV>(j);
     const int first = PAIRS ? 2 * j : j, second = PAIRS ? 2 * j + EPV : sh.half + j;
     const int n1 = PAIRS ? min(EPV, 2 * n) : n, n2 = PAIRS ? 2 * n - n1 : n;
     float u[EPV], w[EPV];
@@ -121,7 +125,7 @@ __device__ __forceinline__ void turn_head(const void* row, const RopeShape& sh, 
     }
 #pragma unroll
     for (int e = 0; e < EPV; ++e) {
-      const CosSin t = cs[min(j + e, sh.half - 1)];
+      const CosSin t = at_j[min(e, n - 1)];
       float& fa = PAIRS ? (e < EPV / 2 ? u[2 * e] : w[2 * e - EPV]) : u[e];
       float& fb = PAIRS ? (e < EPV / 2 ? u[2 * e + 1] : w[2 * e + 1 - EPV]) : w[e];
       const double a = (double)fa, b = (double)fb;
