@@ -116,6 +116,7 @@ enum {
 #define SV_ATTENTION_HEAD_MAX 256
 /* Largest number of heads, and of tokens a page. */
 #define SV_HEADS_MAX 1024
+#define SV_TOKENS_MAX 33554432
 #define SV_PAGE_MAX 65536
 
 /* What of a head's columns turns together (sv_rope), and how frequencies are stretched (sv_rope_frequencies). */
@@ -747,7 +748,7 @@ int sv_clip_grad_norm(int n, const void* const* grads, const int64_t* numel, con
  * A position whose entry is outside [0, n_pages), or that lies behind the last entry, is in no page
  * (SV_FLAG_BAD_PAGE): it is not written, and what is read from or computed with it is NaN.  A length below 0 counts
  * as one behind the last entry.  Two new tokens must not share a place of the cache.
- * Limits: D <= SV_HEAD_MAX, heads <= SV_HEADS_MAX, page <= SV_PAGE_MAX.
+ * Limits: D <= SV_HEAD_MAX, heads <= SV_HEADS_MAX, page <= SV_PAGE_MAX, n_rows (B * P without t_offsets) <= SV_TOKENS_MAX.
  * ------------------------------------------------------------------------ */
 
 /*
@@ -770,7 +771,7 @@ int sv_rope_frequencies(int rot, double base, int scaling, double factor, double
  *   x, out [n, H, D] dtype     out may be x itself (same address and stride), and must not overlap it otherwise
  *   positions [n] int32        rows of a negative one are left as they are
  *   freq [rot / 2] double      of sv_rope_frequencies, or any
- * amplitude > 0; rot even, 2 <= rot <= D.
+ * amplitude > 0; rot even, 2 <= rot <= D; n <= SV_TOKENS_MAX.
  */
 int sv_rope(const void* x, int64_t x_stride, const int32_t* positions, int n, int H, int D, int dtype,
             const double* freq, int rot, int layout, float amplitude, int inverse, void* out,
@@ -819,7 +820,7 @@ size_t sv_chunk_attention_workspace_bytes(int B, int P, int Hq, int heads, int D
  * A row that sees no position, or only scores of -inf: out 0, lse -inf.  What the cache holds at positions that a row does not see
  * does not matter to it, NaN and infinities included.  Scores, weights and sums are float32, weights rounded to bfloat16 before they
  * multiply bfloat16 (or 8-bit) values for bfloat16 queries; out is rounded once.
- * Hq a multiple of heads, D a multiple of 8 and <= SV_ATTENTION_HEAD_MAX, B * P * Hq <= 2^28, window >= 0.
+ * Hq a multiple of heads, D a multiple of 8 and <= SV_ATTENTION_HEAD_MAX, B * P <= SV_TOKENS_MAX, B * P * Hq <= 2^28, window >= 0.
  */
 int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t* t_offsets_or_null, int n_rows,
                        const int32_t* lengths, const int32_t* first_or_null, const int32_t* pages, int max_pages, int B,

@@ -46,7 +46,7 @@ SV_WARP_MAX_TENSORS = 8
 SV_STATIC_SCRATCH_BYTES = 1 << 20
 SV_TOP_MAX = 32
 SV_EMBEDDING_MAX_TOKENS = 1 << 24
-SV_HEAD_MAX, SV_ATTENTION_HEAD_MAX, SV_HEADS_MAX, SV_PAGE_MAX = 1024, 256, 1024, 65536
+SV_HEAD_MAX, SV_ATTENTION_HEAD_MAX, SV_HEADS_MAX, SV_PAGE_MAX, SV_TOKENS_MAX = 1024, 256, 1024, 65536, 33554432
 SV_ROPE_HALVES, SV_ROPE_PAIRS = 0, 1
 SV_ROPE_PLAIN, SV_ROPE_LINEAR, SV_ROPE_NTK, SV_ROPE_PARTS = 0, 1, 2, 3
 (SV_KERNEL_ROW_STATS, SV_KERNEL_ACCEPT_ESTIMATE, SV_KERNEL_SELECT_LENGTH, SV_KERNEL_VERIFY_ROWS,

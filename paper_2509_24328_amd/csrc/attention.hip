@@ -115,7 +115,7 @@ inline bool whole_tiles(int D, int page) { return (D == 64 || D == 128 || D == 2
 extern "C" size_t sv_chunk_attention_workspace_bytes(int B, int P, int Hq, int heads, int D, int dtype, int max_pages, int page) {
   using namespace sv;
   if (B < 1 || P < 1 || heads < 1 || Hq < heads || Hq % heads != 0 || Hq > SV_HEADS_MAX || D < 8 || D > SV_ATTENTION_HEAD_MAX || D % 8 != 0 ||
-      elem_bytes(dtype) == 0 || max_pages < 1 || page < 1 || page > SV_PAGE_MAX || (long long)B * P > kMaxRows / Hq)
+      elem_bytes(dtype) == 0 || max_pages < 1 || page < 1 || page > SV_PAGE_MAX || (long long)B * P > SV_TOKENS_MAX || (long long)B * P > kMaxRows / Hq)
     return 0;
   const size_t own = attention_plan(B, P, Hq, heads, D, dtype, false, (int64_t)max_pages * page).bytes;
   const size_t f8 = attention_plan(B, P, Hq, heads, D, dtype, true, (int64_t)max_pages * page).bytes;
@@ -136,7 +136,7 @@ extern "C" int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t
   SV_REQUIRE(status == SV_OK, status);
   SV_REQUIRE(Hq >= heads && Hq % heads == 0 && D % 8 == 0 && window >= 0, SV_ERR_INVALID_ARG);
   SV_REQUIRE(scale > -INFINITY && scale < INFINITY, SV_ERR_INVALID_ARG);
-  SV_REQUIRE(D <= SV_ATTENTION_HEAD_MAX && Hq <= SV_HEADS_MAX && (long long)B * P <= kMaxRows / Hq, SV_ERR_TOO_LARGE);
+  SV_REQUIRE(D <= SV_ATTENTION_HEAD_MAX && Hq <= SV_HEADS_MAX && (long long)B * P <= SV_TOKENS_MAX && (long long)B * P <= kMaxRows / Hq, SV_ERR_TOO_LARGE);
   if (!t_offsets_or_null) n_rows = B * P;
   if (B == 0 || n_rows == 0) return SV_OK;
   SV_REQUIRE(q_stride >= (int64_t)Hq * D && out_stride >= (int64_t)Hq * D, SV_ERR_INVALID_ARG);

@@ -81,7 +81,7 @@ __device__ __forceinline__ int64_t cache_row(const Pages& pg, int b, int positio
 inline int check_rows(const int32_t* t_offsets, int n_rows, int B, int P, int max_pages, int n_pages, int heads, int page, int D) {
   SV_REQUIRE(B >= 0 && P >= 1 && n_rows >= 0 && max_pages >= 1 && n_pages >= 0 && heads >= 1 && page >= 1 && D >= 1,
              SV_ERR_INVALID_ARG);
-  SV_REQUIRE(t_offsets || (long long)B * P <= 0x7fffffffLL, SV_ERR_TOO_LARGE);
+  SV_REQUIRE((t_offsets ? (long long)n_rows : (long long)B * P) <= SV_TOKENS_MAX, SV_ERR_TOO_LARGE);   // (64 threads to a row, 2^32 to a launch)
   SV_REQUIRE(D <= SV_HEAD_MAX && heads <= SV_HEADS_MAX && page <= SV_PAGE_MAX, SV_ERR_TOO_LARGE);
   return SV_OK;
 }

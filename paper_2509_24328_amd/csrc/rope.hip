@@ -79,7 +79,7 @@ extern "C" int sv_rope(const void* x, int64_t x_stride, const int32_t* positions
   SV_REQUIRE(n >= 0 && H >= 1 && D >= 1 && rot >= 2 && rot % 2 == 0 && rot <= D, SV_ERR_INVALID_ARG);
   SV_REQUIRE(layout == SV_ROPE_HALVES || layout == SV_ROPE_PAIRS, SV_ERR_INVALID_ARG);
   SV_REQUIRE(amplitude > 0.f && amplitude < INFINITY, SV_ERR_INVALID_ARG);
-  SV_REQUIRE(D <= SV_HEAD_MAX && H <= SV_HEADS_MAX, SV_ERR_TOO_LARGE);
+  SV_REQUIRE(D <= SV_HEAD_MAX && H <= SV_HEADS_MAX && n <= SV_TOKENS_MAX, SV_ERR_TOO_LARGE);   // (64 threads to a row, 2^32 to a launch)
   SV_REQUIRE(x_stride >= (int64_t)H * D && out_stride >= (int64_t)H * D, SV_ERR_INVALID_ARG);
   SV_REQUIRE(x_stride < (1ll << 40) && out_stride < (1ll << 40), SV_ERR_TOO_LARGE);
   SV_REQUIRE(x != out || x_stride == out_stride, SV_ERR_INVALID_ARG);

@@ -47,7 +47,7 @@ def test_rope():
     for bad in (dict(n=-1), dict(H=0), dict(D=0), dict(rot=0), dict(rot=3), dict(rot=10), dict(layout=2), dict(amp=0.0), dict(amp=nan),
                 dict(amp=inf), dict(xs=15), dict(os=15), dict(out=p, os=17)):
         assert call(**bad) == Bd.SV_ERR_INVALID_ARG, bad
-    for bad in (dict(D=1025, xs=4096, os=4096), dict(H=1025, xs=1 << 20, os=1 << 20), dict(xs=1 << 40)):
+    for bad in (dict(D=1025, xs=4096, os=4096), dict(H=1025, xs=1 << 20, os=1 << 20), dict(xs=1 << 40), dict(n=(1 << 25) + 1)):
         assert call(**bad) == Bd.SV_ERR_TOO_LARGE, bad
     for bad in ("x", "pos", "freq", "out"):
         assert call(**{bad: None}) == Bd.SV_ERR_NULL, bad
@@ -60,7 +60,7 @@ def rows(k):
 
 
 ROWS_INVALID = (dict(B=-1), dict(P=0), dict(n_rows=-1), dict(mp=0), dict(np=-1), dict(np=0), dict(heads=0), dict(page=0), dict(D=0))
-ROWS_LARGE = (dict(page=65537), dict(B=1 << 16, P=1 << 16))
+ROWS_LARGE = (dict(page=65537), dict(B=1 << 16, P=1 << 16), dict(B=1 << 13, P=(1 << 12) + 1), dict(offs=p, n_rows=(1 << 25) + 1))
 
 
 def write(**k):
@@ -118,7 +118,7 @@ def test_chunk_attention():
                                dict(qs=31), dict(os=31), dict(out=p)):
         assert attend(**bad) == Bd.SV_ERR_INVALID_ARG, bad
     for bad in ROWS_LARGE + (dict(D=264, qs=4096, os=4096), dict(Hq=2048, qs=1 << 20, os=1 << 20), dict(qs=1 << 40), dict(os=1 << 40),
-                             dict(B=1 << 13, P=1 << 14)):
+                             dict(B=1 << 13, P=1 << 14), dict(offs=p, B=1 << 13, P=1 << 13, Hq=2), dict(B=1 << 24, P=1 << 1, Hq=16, qs=128, os=128)):
         assert attend(**bad) == Bd.SV_ERR_TOO_LARGE, bad
     for bad in ("q", "len", "pages", "kc", "vc", "out"):
         assert attend(**{bad: None}) == Bd.SV_ERR_NULL, bad

@@ -290,6 +290,28 @@ def test_another_stream_and_graph_replays():
         assert torch.equal(out, ref[0]) and torch.equal(lse, ref[1])
 
 
+@pytest.mark.parametrize("T", [1, 12, 40])
+@pytest.mark.parametrize("kind, n_pages, D, page", [(BF16, 140000, 128, 16), (BF16, 140000, 120, 17), (F8, 280000, 128, 16)])
+def test_a_cache_beyond_32_bits(kind, n_pages, D, page, T):
+    """Pages more than 2^32 bytes apart: the same numbers as from a small cache with the same pages, to the last bit."""
+    lengths, used = [200, 37], [[n_pages - 1 - 3 * j for j in range(16)], [n_pages - 2 - 3 * j for j in range(15)] + [0]]
+    used[0][5], used[1][1] = 3, n_pages // 2
+    small, pages = make(lengths, [T] * 2, 8, D, page, kind, seed=T)
+    pages = pages[:, :16]
+    big = P.Cache.empty(n_pages, 8, page, D, kind)
+    far = torch.full_like(pages, -1)
+    for b in range(2):
+        for j in range(pages.shape[1]):
+            if pages[b, j] >= 0:
+                far[b, j] = used[b][j]
+                for to, of in zip(big._tensors, small._tensors):
+                    if to is not None:
+                        to[used[b][j]].view(torch.uint8).copy_(of[pages[b, j]].view(torch.uint8))
+    q = queries(2 * T, 32, D, BF16).view(2, T, 32, D)
+    for got, want in zip(run(big, q, lengths, far, None, None), run(small, q, lengths, pages, None, None)):
+        assert torch.equal(got, want)
+
+
 def test_nothing_to_do():
     cache, pages = make([3], [1], 1, 64, 16, BF16)
     q = torch.empty((0, 2, 64), dtype=BF16, device="cuda")

@@ -158,6 +158,14 @@ def test_vocabularies_that_share_maxima(V, dtype):
         check(z, u, **warp)
 
 
+@pytest.mark.parametrize("K", [2048, 2049, 5000, 19999, 20000, 20001])
+def test_many_entries_left(K):
+    for dtype in (F32, BF16):
+        z, u = logits(3, 20000, dtype, K)
+        for warp in (dict(), dict(top_p=0.9), dict(top_p=0.7, min_p=1e-5, temperature=3.0)):
+            check(z, u, top_k=K, **warp)
+
+
 def test_no_rows():
     P.sv_sample(torch.empty((0, 8), device="cuda"), torch.empty(0, dtype=torch.float64, device="cuda"),
                 torch.empty(0, dtype=torch.int32, device="cuda"))
