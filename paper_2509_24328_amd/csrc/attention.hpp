@@ -7,14 +7,17 @@
 // The result of the first product has, in lane (g, m), keys 4 g .. 4 g + 3 of row m, which is operand B of the second one if its sum
 // over 32 keys takes them in the order (tile, key 4 g + r): the order of a sum is free as long as both operands follow it.
 // Likewise the columns of the first product: a lane's sixteen bytes are at 64 s + 16 g of the row, for keys and queries alike.
-// So keys and values go from the cache's pages into registers and from there into the matrix cores, without LDS.
+// So keys and values go from the cache's pages into registers and from there into the matrix cores, without LDS (up to 64 rows).
 // The softmax is one pass: a running maximum (in units of log2, raised only when it is exceeded by more than 8: a weight is at most 2^8
 // then) and, in every lane, the sum of the weights of its keys.  Scores, weights, sums and outputs are float32; weights are rounded to
-// bfloat16 for the second product where the queries are bfloat16 (half a step, 2^-9 of a weight, at random).
+// bfloat16 for the second product where the queries are bfloat16 (half a step: at most 2^-8 of a weight).
 //
 // A workgroup has four wavefronts: one, two or four blocks of rows, and as many interleaved parts of the keys as that leaves, joined in
 // LDS at the end.  Where there are few rows, the keys of a row block are divided among up to `splits` workgroups, whose results a second kernel joins; each has
 // at least kMinSteps x 32 keys, and about as many as the average of kTargetGroups of them, from the lengths that the device knows.
+// What bounds it: reading the cache once (64 x 1 over 16384 tokens, 8 heads of 128 bf16 columns: 711 us, 6.0 TB/s); 8-bit keys and values are also
+// converted, four instructions to eight columns, and sequences of 2048 to 8192 tokens do not divide evenly (64 x 9: 206 us, 3.4 TB/s).  In one sequence of
+// 1500 tokens nothing but a chain of loads is left: 7 us and 5 for the join.
 #pragma once
 
 #include "paged.hpp"
@@ -27,7 +30,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr int kStep = 32;              // keys of a step
 constexpr int kMinSteps = 4;           // steps of a workgroup that divides a row block's keys with others, at least
 // Workgroups that the keys of a call are divided among: two to a compute unit, which is what the registers hold.  64 x 1 over 16384 bf16: 512
-// 713 us, 1024 725, 2048 729; 64 x 9 over 8192 in 8 bits: 210, 216, 235; 2048 over 6144: 499, 537, 572.
+// 711 us, 1024 718, 2048 722; 64 x 9 over 2048 to 8192 in 8 bits, with the join: 219, 225, 240; 2048 over 6144: 452, 508, 536 (on one card).
 constexpr int kTargetGroups = 512;
 constexpr int kMaxSplits = 64;
 constexpr int kAttnWaves = 4;
@@ -856,8 +859,10 @@ __device__ __forceinline__ int work_of(const AttnArgs& a, Work& k) {
   k.step0 = step_lo;
   k.step1 = step_lo + steps;
   if (a.splits > 1) {
-    const int unit = steps_per_group(a);
-    k.parts = max(1, min((steps + unit - 1) / unit, a.splits));
+    // (up to a quarter more than the average stays whole, where a part is long: 64 x 1 over 2048 to 8192 tokens 280 us so 267, in 8 bits 181
+    // and 165.  Parts of a few steps do not: 5 x 7 float32 rows over 900 tokens 17.4 us, so 20.5)
+    const int unit = steps_per_group(a), more = unit >= 16 ? unit / 4 : 0;
+    k.parts = max(1, min((steps - more + unit - 1) / unit, a.splits));
     if (k.split >= k.parts) return 0;
     const int each = (steps + k.parts - 1) / k.parts;
     k.step0 = step_lo + min(k.split * each, steps);
