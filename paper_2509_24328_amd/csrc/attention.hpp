@@ -888,7 +888,7 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, (DPAD == 256 || (ET == SV_F
 // (8-bit ones are converted once, not by every wavefront), the next step under way in registers meanwhile.  The sixteen-byte chunks of a row are
 // permuted by its number, so that the rows of an operand (keys: sixteen rows, one chunk; values: one row, sixteen chunks) lie in different
 // banks.  What bounds it is the vector ALU beside the matrix cores: per 32 keys and 32 rows, 32 matrix instructions of 16 cycles
-// and 700 cycles of exponentials, maxima, sums and conversions.  A wavefront at its products goes before the one that shares its SIMD and is at
+// and about 900 cycles of exponentials (16, four slots each), maxima, sums and conversions (160).  A wavefront at its products goes before the one that shares its SIMD and is at
 // its exponentials: 2048 over 6144 with 32 heads on 8, 450 us without that and 418 with it, on one card.  (The scores of the next step formed
 // beside the weights of this one, in one wavefront: 485.)
 constexpr int kTileKeys = kStep;

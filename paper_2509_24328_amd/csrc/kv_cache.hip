@@ -2,6 +2,10 @@
 // A cache in 8 bits holds e4m3 numbers and a float32 scale for every token and head, amax / 448 (not below 2^-126; 1 where all
 // columns are 0): the largest column of a head is then as well resolved as e4m3 resolves anything, whatever the layer's range, and a
 // row costs 4 bytes more.  A head that holds a NaN or an infinity has the scale NaN and reads back as NaN.
+// A workgroup has one token, four from 4096 tokens on: its place and angles once, then a head for every eight lanes, so that queries, keys
+// and values share one launch and one lookup.  What bounds it: one user's or one step's tokens, a chain of loads (offsets and lengths, the page,
+// the head) and the store (64 x 9 tokens, 48 heads of 128 bf16 columns into 8 bits: 8.2 us); a prompt, the memory (4096 tokens, 24 heads of 80
+// float32 columns: 16 us, 3.9 TB/s; 5096 tokens back: 12.5 us, 4.2 TB/s).
 #include "paged.hpp"
 #include "rope.hpp"
 
