@@ -88,7 +88,7 @@ inline AttnPlan attention_plan(int B, int P, int Hq, int heads, int D, int dtype
   const bool wide = dtype == SV_F32 || D > 128;             // (outputs of one block of rows fill a wavefront's registers)
   p.nt = wide || rows <= 16 ? 1 : 2;
   // (8-bit keys, converted once by one wavefront of 48 rows and not by two of 32: 64 x 9 with 4 heads to one over 8192 tokens, all nine
-  // there, 320 us and 414; one to nine there 214 and 219.  Keys of 16 bits do not leave the registers.)
+  // there, 320 us and 414 (302 since its products have priority); one to nine there 214 and 219.  Keys of 16 bits do not leave the registers.)
   if (f8 && p.nt == 2 && rows > 32 && rows <= 48) p.nt = 3;
   p.tile_rows = 16 * p.nt * (rows <= 16 * p.nt ? 1 : (rows <= 32 * p.nt ? 2 : 4));
   const int64_t tiles = (rows + p.tile_rows - 1) / p.tile_rows;
