@@ -13,8 +13,9 @@
 // bfloat16 for the second product where the queries are bfloat16 (half a step: at most 2^-8 of a weight).
 //
 // A workgroup has four wavefronts: one, two or four blocks of rows, and as many interleaved parts of the keys as that leaves, joined in
-// LDS at the end.  Where there are few rows, the keys of a row block are divided among up to `splits` workgroups, whose results a second kernel joins; each has
-// at least kMinSteps x 32 keys, and about as many as the average of kTargetGroups of them, from the lengths that the device knows.
+// LDS at the end.  Where there are few rows, the keys of a row block are divided among up to `splits` workgroups, whose results a second kernel
+// joins; each has at least kMinSteps x 32 keys, and about as many as the average of kTargetGroups of them, from the lengths that the device
+// knows.
 // What bounds it: reading the cache once (64 x 1 over 16384 tokens, 8 heads of 128 bf16 columns: 711 us, 6.0 TB/s); 8-bit keys and values are also
 // converted, four instructions to eight columns, and sequences of 2048 to 8192 tokens do not divide evenly (64 x 9: 206 us, 3.4 TB/s).  In one sequence of
 // 1500 tokens nothing but a chain of loads is left: 7 us and 5 for the join.
@@ -893,10 +894,10 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, (DPAD == 256 || (ET == SV_F
 // Many rows: 128 to a workgroup, 32 to a wavefront, which all need the same keys and values.  A step of them at a time is staged in LDS as bfloat16
 // (8-bit ones are converted once, not by every wavefront), the next step under way in registers meanwhile.  The sixteen-byte chunks of a row are
 // permuted by its number, so that the rows of an operand (keys: sixteen rows, one chunk; values: one row, sixteen chunks) lie in different
-// banks.  What bounds it is the vector ALU beside the matrix cores: per 32 keys and 32 rows, 32 matrix instructions of 16 cycles
-// and about 900 cycles of exponentials (16, four slots each), maxima, sums and conversions (160).  A wavefront at its products goes before the one that shares its SIMD and is at
-// its exponentials: 2048 over 6144 with 32 heads on 8, 450 us without that and 418 with it, on one card.  (The scores of the next step formed
-// beside the weights of this one, in one wavefront: 485.)
+// banks.  What bounds it is the vector ALU beside the matrix cores: per 32 keys and 32 rows, 32 matrix instructions of 16 cycles and about 900
+// cycles of exponentials (16, four slots each), maxima, sums and conversions (160).  A wavefront at its products goes before the one
+// that shares its SIMD and is at its exponentials: 2048 over 6144 with 32 heads on 8, 450 us without that and 418 with it, on one card.  (The
+// scores of the next step formed beside the weights of this one, in one wavefront: 485.)
 constexpr int kTileKeys = kStep;
 
 template <int CT, int DPAD, bool WHOLE>

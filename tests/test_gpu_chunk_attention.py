@@ -312,6 +312,35 @@ def test_a_cache_beyond_32_bits(kind, n_pages, D, page, T):
         assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("dtype, kind", TYPES)
+def test_shared_pages(dtype, kind):
+    """Sequences that share their first pages, and a table that names one page twice."""
+    lengths, T = [600, 600, 90], 5
+    cache, pages = make(lengths, [T] * 3, 2, 64, 16, kind)
+    pages[1, :30] = pages[0, :30]
+    pages[2, 3] = pages[2, 1]
+    q = queries(3 * T, 8, 64, dtype)
+    check(cache, q, run(cache, q.view(3, T, 8, 64), lengths, pages, None, None), lengths, pages, None, T)
+
+
+def test_two_calls_at_once():
+    """Two batches over one cache on two streams, each with scratch of its own."""
+    lengths, T = [3000, 20, 1500, 2500], 3
+    cache, pages = make(lengths, [T] * 4, 2, 128, 16, BF16)
+    q = queries(4 * T, 8, 128, BF16).view(4, T, 8, 128)
+    i32 = lambda v: torch.as_tensor(v, dtype=torch.int32).cuda()
+    n, table = i32(lengths), pages.cuda()
+    calls = [(q, n, table), (q.flip(0).contiguous(), n.flip(0).contiguous(), table.flip(0).contiguous())]
+    outs, streams = [torch.empty_like(q) for _ in calls], [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for (x, le, pg), out, s in zip(calls, outs, streams):
+            P.sv_chunk_attention(cache, x, out, le, pg, stream=s)
+    torch.cuda.synchronize()
+    want = run(cache, q, lengths, pages, None, None)[0]
+    assert torch.equal(outs[0], want) and torch.equal(outs[1], want.flip(0))
+
+
 def test_nothing_to_do():
     cache, pages = make([3], [1], 1, 64, 16, BF16)
     q = torch.empty((0, 2, 64), dtype=BF16, device="cuda")
