@@ -169,7 +169,8 @@ extern "C" int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t
   a.D = D;
   a.window = window;
   a.by_group = fast_div(a.group);
-  a.scale2 = (float)((double)scale * kLog2e);
+  a.zero = scale == 0.f && !f8;
+  a.scale2 = a.zero ? 1.f : (float)((double)scale * kLog2e);
   a.k_cache = static_cast<const char*>(k_cache);
   a.v_cache = static_cast<const char*>(v_cache);
   a.k_scale = k_scale_or_null;

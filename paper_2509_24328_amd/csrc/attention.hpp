@@ -48,6 +48,8 @@ struct AttnArgs {
   int Hq, group, D, window;
   FastDiv by_group;
   float scale2;                        // scale * log2 e
+  bool zero;                           // the scale is 0, scale2 1: queries are multiplied by 0 instead, since 0 times the -inf of an unseen key is
+                                       // a NaN (not over 8-bit caches, where keys are masked behind the product with the scale)
   const char *k_cache, *v_cache;
   const float *k_scale, *v_scale;
   int tiles, splits, tile_rows;        // row blocks of a head of a sequence; most workgroups to one; rows of one
@@ -155,6 +157,10 @@ __device__ __forceinline__ bf16x8 as_bf16x8(uint32_t a, uint32_t b, uint32_t c, 
   return __builtin_bit_cast(bf16x8, u32x4{a, b, c, d});
 }
 
+// 0 times the number whose exponent has the bits E: 0, or a NaN (in those bits and the one below) for what is not finite.
+template <uint32_t E>
+__device__ __forceinline__ uint32_t zero_or_nan(uint32_t w) { return (w & E) == E ? E | (E >> 1) : 0u; }
+
 // max / sum over the four lanes that hold the same row (lanes m, m + 16, m + 32, m + 48)
 __device__ __forceinline__ float across_max(float v) {
   Halves h = swap32(__float_as_uint(v), __float_as_uint(v));
@@ -221,6 +227,11 @@ struct Wavefront {
 #pragma unroll
           for (int j = 0; j < 4; ++j) qw[n][k * words + e * Sh::eb / 4 + j] = w[j];
         }
+      }
+      if (!kScaled && a.zero) {
+#pragma unroll
+        for (int j = 0; j < Sh::NK * Sh::EK * Sh::eb / 4; ++j) qw[n][j] = Sh::f32 ? zero_or_nan<0x7f800000u>(qw[n][j])
+                                                                                 : zero_or_nan<0x7f800000u>(qw[n][j]) | zero_or_nan<0x00007f80u>(qw[n][j]);
       }
       if (a.scale2 < 0.f) {                              // (the scale is taken positive)
 #pragma unroll
