@@ -35,6 +35,7 @@ constexpr int kMinSteps = 4;           // steps of a workgroup that divides a ro
 constexpr int kTargetGroups = 512;
 constexpr int kMaxSplits = 64;
 constexpr int kAttnWaves = 4;
+constexpr float kFar = 16777216.f;     // 2^24
 constexpr long long kMaxRows = 1 << 28;   // B * P * Hq: positions and rows stay within 32 bits
 
 struct AttnArgs {
@@ -192,6 +193,7 @@ struct Wavefront {
   uint32_t qw[NT][Sh::NK * Sh::EK * Sh::eb / 4];        // queries, by the columns of the keys' loads
   f32x4 o[NT][NO];
   float mx[NT], l[NT];
+  bool far;                                             // some row's maximum is beyond 2^24 (the same in all lanes; not with kScaled)
 
   __device__ __forceinline__ Wavefront(const AttnArgs& args) : a(args), g((threadIdx.x & 63) >> 4), m(threadIdx.x & 15) {}
 
@@ -207,6 +209,7 @@ struct Wavefront {
   __device__ __forceinline__ int row_bytes() const { return (WHOLE ? DPAD : a.D) * kCacheBytes1; }
 
   __device__ __forceinline__ void start(const Sequence& s, int rho0, int h) {
+    far = false;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const int rho = rho0 + 16 * n + m, i = divide(rho, a.by_group), hq = h * a.group + rho - i * a.group;
@@ -456,11 +459,32 @@ struct Wavefront {
 #pragma unroll
         for (int t = 0; t < NO; ++t) o[n][t] *= f;
       }
+      if constexpr (!kScaled) {
+        bool beyond = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) beyond |= fabsf(mx[n]) >= kFar && mx[n] > -INFINITY;
+        far = __ballot(beyond) != 0;
+      }
     }
   }
 
+  // The maximum is that of rounded products with the scale, and an exponent an exact product less the maximum: at the largest key it is the
+  // maximum's rounding, up to half a unit of it.  Below 2^24 that is 1/2 at most; from there on products are rounded first (2^-24 of a score, as
+  // a score's own sum is), so that it is 0.
   template <bool PART>
   __device__ __forceinline__ void weigh(int key0, const Values& vv, f32x4 (&s)[NT][2]) {
+    float by = scale();
+    if constexpr (!kScaled) {
+      if (__builtin_expect(far, 0)) {
+        asm volatile("");                                  // (a branch)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) s[n][t] *= by;
+        }
+        by = 1.f;
+      }
+    }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const float base = mx[n] == -INFINITY ? 0.f : mx[n];
@@ -468,7 +492,7 @@ struct Wavefront {
       for (int t = 0; t < 2; ++t) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float p = exp2_fast(kScaled ? s[n][t][r] - base : __builtin_fmaf(s[n][t][r], scale(), -base));
+          float p = exp2_fast(kScaled ? s[n][t][r] - base : __builtin_fmaf(s[n][t][r], by, -base));
           l[n] += p;
           if constexpr (kScaled) {
             p *= vv.scale[4 * t + r];
