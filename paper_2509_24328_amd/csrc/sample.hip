@@ -29,9 +29,10 @@ constexpr int kOwn = kList / kDrawThreads;   // entries of the list that a threa
 constexpr int kNucleusRank = 40;         // first guess of a nucleus: the entries above this many lane maxima
 constexpr int kDeepRank = 1200;          // second guess: above this many vectors' maxima
 constexpr int kMaxKeys = 40960;          // vectors' maxima in LDS (80 KB); longer rows share one among several vectors
-// Error of a float32 mass, relative: the exponent k of a weight is off by 2^-23 |k| (difference and product), which is 8.3e-8 |k| of the
-// weight; an average over the mass has |k| <= 24 (2^24 entries that far down weigh as much as the first).  Up to six factors of v_exp_f32
-// (a lane's maximum is raised a few times), 2^-23 each, and 2^-21 for sums of eight terms: 3.3e-6.
+// Error of a float32 mass, relative: the exponent k of a weight is off by 2^-23 |k| (two roundings), which is 8.3e-8 |k| of the weight; an
+// average over the mass has |k| <= 24 (2^24 entries that far down weigh as much as the first), and 25.3 where the weights refer to
+// a whole number up to 1.3 above the largest entry.  v_exp_f32 adds 2^-23, and sums of eight terms 2^-21: 2.7e-6.  Nothing else adds to it: lanes'
+// sums are fp64, and their references whole numbers, so that raising one scales its sum by a power of two.
 constexpr double kMassError = 4e-6;
 
 struct SampleArgs {
@@ -56,7 +57,7 @@ __device__ __forceinline__ uint32_t order_key(float f) {           // ascending
 }
 __device__ __forceinline__ float key_float(uint32_t k) { return __uint_as_float((k >> 31) ? (k & 0x7fffffffu) : ~k); }
 
-// 2^k, k <= 0, to 1e-15: k = n + f with |f| <= 1/2, and the series of e^(f ln 2) up to the eleventh power (0.347^12 / 12! = 6e-15).
+// 2^k, k <= 1, to 1e-15: k = n + f with |f| <= 1/2, and the series of e^(f ln 2) up to the eleventh power (0.347^12 / 12! = 6e-15).
 __device__ __forceinline__ double exp2_series(double k) {
   const double n = __builtin_rint(k), r = (k - n) * kLn2;
   double p = 1.0 / 39916800.0;
@@ -80,6 +81,12 @@ struct FastScale {
   __device__ __forceinline__ float weight(float below) const {
     const float b = fmaxf(below, -1e30f);                // (-inf times lo is no -inf)
     return exp2_fast(__builtin_fmaf(b, hi, b * lo));
+  }
+  // The same relative to 2^ref, ref a whole number next to the exponent of the largest entry.
+  __device__ __forceinline__ float whole(float top) const { return fminf(fmaxf(__builtin_ceilf(top * hi), kRefFloor), kRefCeil); }
+  __device__ __forceinline__ float weight_to(float x, float ref) const {
+    const float b = fmaxf(x, -1e30f);
+    return exp2_fast(__builtin_fmaf(b, lo, __builtin_fmaf(b, hi, -ref)));
   }
 };
 
@@ -707,8 +714,8 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_kernel(SampleArgs a) {
   const int n_keys = (n_all + a.share - 1) / a.share;
   double u = a.u[r];
 
-  // sweep: maxima of vectors, of the lane and the row; the row's mass relative to the lane's maximum
-  float mine = -INFINITY;
+  // sweep: maxima of vectors, of the lane and the row; the row's mass relative to 2^ref of the lane
+  float mine = -INFINITY, ref = kRefFloor;
   bool nan = false;
   double mass = 0.0;
   const bool weigh = use_p && !use_k;
@@ -728,10 +735,14 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_kernel(SampleArgs a) {
     for (int e = 0; e < EPV; ++e) nan |= x[e] != x[e];
     const float m = fmaxf(mine, t);
     if (weigh && m > -INFINITY) {
+      if (m > mine) {
+        const float r = d.fast.whole(m);
+        mass = __builtin_ldexp(mass, (int)(ref - r));
+        ref = r;
+      }
       float s = 0.f;
 #pragma unroll
-      for (int e = 0; e < EPV; e += 2) s += d.fast.weight(x[e] - m) + d.fast.weight(x[e + 1] - m);
-      if (m > mine) mass *= mine == -INFINITY ? 0.0 : (double)d.fast.weight(mine - m);
+      for (int e = 0; e < EPV; e += 2) s += d.fast.weight_to(x[e], ref) + d.fast.weight_to(x[e + 1], ref);
       mass += (double)s;
     }
     mine = m;
@@ -803,13 +814,16 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_kernel(SampleArgs a) {
   double all = 0.0;                                      // the row's mass
   bool exact = true;
   if (weigh) {
-    all = team.sum(mine == -INFINITY ? 0.0 : mass * (double)d.fast.weight(mine - top));
+    const float top_ref = d.fast.whole(top);
+    all = team.sum(mine == -INFINITY ? 0.0 : __builtin_ldexp(mass, (int)(ref - top_ref)));
+    all *= exp2_series((double)top_ref - ((double)top * (double)d.fast.hi + (double)top * (double)d.fast.lo));
     exact = false;
   }
   auto make_exact = [&]() {
     if (!exact) all = d.mass_above(none);
     exact = true;
   };
+  if (weigh && fabs(y) >= 0x1p22) make_exact();          // (the whole numbers of float32 next to it may be farther off)
 
   // A sixteen-bit key that at least `want` of the keys counted by count(probe) reach, and few more than that if there is such a one; the keys
   // lie between `from`, which `want` of them reach, and `to`.
