@@ -821,6 +821,7 @@ size_t sv_chunk_attention_workspace_bytes(int B, int P, int Hq, int heads, int D
  * does not matter to it, NaN and infinities included.  Scores, weights and sums are float32, weights rounded to bfloat16 before they
  * multiply bfloat16 (or 8-bit) values for bfloat16 queries; out is rounded once.  A score, its log2 e times and <q, k> itself are to be less than
  * 2^127 in magnitude, as float32 numbers are; beyond that the row may be NaN.
+ * Positions from 2^31 - 256 - P on count as behind the last entry of pages.
  * Hq a multiple of heads, D a multiple of 8 and <= SV_ATTENTION_HEAD_MAX, B * P <= SV_TOKENS_MAX, B * P * Hq <= 2^28, window >= 0.
  */
 int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t* t_offsets_or_null, int n_rows,

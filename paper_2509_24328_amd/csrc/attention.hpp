@@ -47,6 +47,7 @@ struct AttnArgs {
   Pages pages;
   const int32_t* first;                // [B], or null
   int Hq, group, D, window;
+  int cap;                             // positions from here on are in no page
   FastDiv by_group;
   float scale2;                        // scale * log2 e
   bool zero;                           // the scale is 0, scale2 1: queries are multiplied by 0 instead, since 0 times the -inf of an unseen key is
@@ -77,8 +78,7 @@ __device__ __forceinline__ Sequence sequence_of(const AttnArgs& a, int b) {
   }
   s.start = a.rows.start[b];
   s.first = a.first ? max(a.first[b], 0) : 0;
-  const int64_t cap = (int64_t)a.pages.max_pages * (int)a.pages.page.d;
-  s.cap = (int)(cap < 0x40000000 ? cap : 0x40000000);
+  s.cap = a.cap;
   if (s.start < 0 || s.start > s.cap) s.start = s.cap;              // every row is behind the last page
   return s;
 }
