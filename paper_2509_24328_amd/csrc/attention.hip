@@ -168,9 +168,6 @@ extern "C" int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t
   a.group = Hq / heads;
   a.D = D;
   a.window = window;
-  // (positions of the last new tokens, and of the steps around them, stay within 32 bits)
-  const int64_t tokens = (int64_t)max_pages * page, most = 0x7fffff00ll - P;
-  a.cap = (int)(tokens < most ? tokens : most);
   a.by_group = fast_div(a.group);
   a.zero = scale == 0.f && !f8;
   a.scale2 = a.zero ? 1.f : (float)((double)scale * kLog2e);

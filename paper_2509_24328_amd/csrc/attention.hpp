@@ -47,7 +47,6 @@ struct AttnArgs {
   Pages pages;
   const int32_t* first;                // [B], or null
   int Hq, group, D, window;
-  int cap;                             // positions from here on are in no page
   FastDiv by_group;
   float scale2;                        // scale * log2 e
   bool zero;                           // the scale is 0, scale2 1: queries are multiplied by 0 instead, since 0 times the -inf of an unseen key is
@@ -78,7 +77,9 @@ __device__ __forceinline__ Sequence sequence_of(const AttnArgs& a, int b) {
   }
   s.start = a.rows.start[b];
   s.first = a.first ? max(a.first[b], 0) : 0;
-  s.cap = a.cap;
+  const int64_t cap = (int64_t)a.pages.max_pages * (int)a.pages.page.d;
+  const int most = 0x7fffff00 - a.rows.P;      // (positions of the last new tokens, and of the steps around them, stay within 32 bits)
+  s.cap = (int)(cap < most ? cap : most);
   if (s.start < 0 || s.start > s.cap) s.start = s.cap;              // every row is behind the last page
   return s;
 }
