@@ -154,7 +154,6 @@ extern "C" int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t
   AttnPlan p = attention_plan(B, P, Hq, heads, D, dtype, f8, (int64_t)max_pages * page);
   if (!ws_or_null) p.splits = 1;
   else if (p.splits > 1) SV_REQUIRE(is_aligned(ws_or_null, kWsAlign) && ws_bytes >= p.bytes, SV_ERR_WORKSPACE);
-  SV_REQUIRE(p.items * p.splits <= 0xffffffffLL / (kAttnWaves * kWave), SV_ERR_TOO_LARGE);
   AttnArgs a{};
   a.q = static_cast<const char*>(q);
   a.out = static_cast<char*>(out);
@@ -186,20 +185,38 @@ extern "C" int sv_chunk_attention(const void* q, int64_t q_stride, const int32_t
     w += ws_round((size_t)p.items * p.splits * p.tile_rows * 8);
     a.part_o = reinterpret_cast<float*>(w);
   }
-  const AttnLaunch t{p.nt, p.nt == 2 && p.tile_rows == 128, whole, (unsigned)(p.items * p.splits), as_stream(stream)};
-  if (dtype == SV_F32) {
-    if (f8) launch_attention_f32_f8(a, t); else launch_attention_f32(a, t);
-  } else {
-    if (f8) launch_attention_bf16_f8(a, t); else launch_attention_bf16(a, t);
+  // A launch holds 2^32 lanes: of more row blocks (which are not divided, so that no call needs scratch for them), as many sequences as one takes.
+  // Those of one sequence fit, at most P Hq / 64 + heads.
+  const int64_t each = (int64_t)heads * p.tiles * p.splits, most = 0xffffffffLL / (kAttnWaves * kWave) / each;
+  for (int b = 0, n; b < B; b += n) {
+    n = (int)(B - b < most ? B - b : most);
+    AttnArgs s = a;
+    s.rows.B = n;
+    s.rows.start += b;
+    s.pages.table += (int64_t)b * max_pages;
+    if (s.first) s.first += b;
+    if (s.rows.offsets) {
+      s.rows.offsets += b;
+    } else {
+      s.q += (int64_t)b * P * s.q_stride;
+      s.out += (int64_t)b * P * s.out_stride;
+      if (s.lse) s.lse += (int64_t)b * P * Hq;
+    }
+    const AttnLaunch t{p.nt, p.nt == 2 && p.tile_rows == 128, whole, (unsigned)(n * each), as_stream(stream)};
+    if (dtype == SV_F32) {
+      if (f8) launch_attention_f32_f8(s, t); else launch_attention_f32(s, t);
+    } else {
+      if (f8) launch_attention_bf16_f8(s, t); else launch_attention_bf16(s, t);
+    }
   }
   if (p.splits > 1) {
     const int64_t all = (int64_t)B * P * Hq;
     if (dtype == SV_F32)
-      hipLaunchKernelGGL((attention_join_kernel<SV_F32>), dim3((unsigned)((all + 3) / 4)), dim3(256), 0, t.stream, a);
+      hipLaunchKernelGGL((attention_join_kernel<SV_F32>), dim3((unsigned)((all + 3) / 4)), dim3(256), 0, as_stream(stream), a);
     else
-      hipLaunchKernelGGL((attention_join_kernel<SV_BF16>), dim3((unsigned)((all + 3) / 4)), dim3(256), 0, t.stream, a);
+      hipLaunchKernelGGL((attention_join_kernel<SV_BF16>), dim3((unsigned)((all + 3) / 4)), dim3(256), 0, as_stream(stream), a);
   }
   if (flags_or_null)
-    hipLaunchKernelGGL(attention_flags_kernel, dim3((unsigned)(((int64_t)B * P + 3) / 4)), dim3(256), 0, t.stream, a, flags_or_null);
+    hipLaunchKernelGGL(attention_flags_kernel, dim3((unsigned)(((int64_t)B * P + 3) / 4)), dim3(256), 0, as_stream(stream), a, flags_or_null);
   return launch_status();
 }
