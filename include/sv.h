@@ -817,6 +817,7 @@ size_t sv_chunk_attention_workspace_bytes(int B, int P, int Hq, int heads, int D
  *   flags_or_null [n_rows] uint32     out  SV_FLAG_BAD_PAGE: a position that the row sees is in no page; out and lse are NaN
  *   ws_or_null                        256-byte aligned, of sv_chunk_attention_workspace_bytes.  Without it one workgroup goes through
  *                                     all keys of its rows: the same results, but for the order of the sums, in more time
+ * Rows are laid out for P new tokens of every sequence: a batch of long chunks and of single tokens takes less time in two calls.
  * A row that sees no position, or only scores of -inf: out 0, lse -inf.  What the cache holds at positions that a row does not see
  * does not matter to it, NaN and infinities included.  Scores, weights and sums are float32, weights rounded to bfloat16 before they
  * multiply bfloat16 (or 8-bit) values for bfloat16 queries; out is rounded once.  A score, its log2 e times and <q, k> itself are to be less than

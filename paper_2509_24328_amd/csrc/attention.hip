@@ -87,8 +87,11 @@ inline AttnPlan attention_plan(int B, int P, int Hq, int heads, int D, int dtype
   const int64_t rows = (int64_t)P * (Hq / heads);
   const bool wide = dtype == SV_F32 || D > 128;             // (outputs of one block of rows fill a wavefront's registers)
   p.nt = wide || rows <= 16 ? 1 : 2;
-  // (8-bit keys, converted once by one wavefront of 48 rows and not by two of 32: 64 x 9 with 4 heads to one over 8192 tokens, all nine
-  // there, 320 us and 414 (302 since its products have priority); one to nine there 214 and 219.  Keys of 16 bits do not leave the registers.)
+  // (8-bit keys, converted once by one wavefront of 48 rows and not by two of 32, though 70 registers of it go to memory.  64 sequences of 8192 tokens, 4
+  // heads to one, 48 rows and 32, us: 9 tokens of each, 128 columns, pages of 64 304 and 367, of 20 330 and 402; 64 columns 175 and 267, pages of 20 200 and
+  // 318; 12 tokens, 128 columns 307 and 366, 64 columns 183 and 268.  Of 1 to 9 tokens over 2048 to 8192, where most sequences have
+  // no more than 32 rows anyway: 128 columns 210 and 204, pages of 20 236 and 227, 64 columns 155 and 153; of 1 to 12 254 and 286, 163 and 206.
+  // The worst found: 64 columns, 1 or 6 of 10 tokens, 152 and 128.  Keys of 16 bits do not leave the registers.)
   if (f8 && p.nt == 2 && rows > 32 && rows <= 48) p.nt = 3;
   p.tile_rows = 16 * p.nt * (rows <= 16 * p.nt ? 1 : (rows <= 32 * p.nt ? 2 : 4));
   const int64_t tiles = (rows + p.tile_rows - 1) / p.tile_rows;

@@ -16,9 +16,11 @@
 // LDS at the end.  Where there are few rows, the keys of a row block are divided among up to `splits` workgroups, whose results a second kernel
 // joins; each has at least kMinSteps x 32 keys, and about as many as the average of kTargetGroups of them, from the lengths that the device
 // knows.
-// What bounds it: reading the cache once (64 x 1 over 16384 tokens, 8 heads of 128 bf16 columns: 711 us, 6.0 TB/s); 8-bit keys and values are also
-// converted, four instructions to eight columns, and sequences of 2048 to 8192 tokens do not divide evenly (64 x 9: 206 us, 3.4 TB/s).  In one sequence of
+// What bounds it: reading the cache once (64 x 1 over 16384 tokens, 8 heads of 128 bf16 columns: 708 us, 6.1 TB/s); 8-bit keys and values are also
+// converted, four instructions to eight columns, and sequences of 2048 to 8192 tokens do not divide evenly (64 x 9: 199 us, 3.5 TB/s).  In one sequence of
 // 1500 tokens nothing but a chain of loads is left: 7 us and 5 for the join.
+// Rows are laid out over wavefronts, and keys over workgroups, by the largest number of new tokens that a sequence may have: one chunk of 512 tokens and
+// 63 single ones of other sequences, all over 8192, take 973 us in one call, and 376 and 150 in two.
 #pragma once
 
 #include "paged.hpp"
@@ -30,8 +32,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kStep = 32;              // keys of a step
 constexpr int kMinSteps = 4;           // steps of a workgroup that divides a row block's keys with others, at least
-// Workgroups that the keys of a call are divided among: two to a compute unit, which is what the registers hold.  64 x 1 over 16384 bf16: 512
-// 711 us, 1024 718, 2048 722; 64 x 9 over 2048 to 8192 in 8 bits, with the join: 219, 225, 240; 2048 over 6144: 452, 508, 536 (on one card).
+// Workgroups that the keys of a call are divided among: two to a compute unit, which is what the registers hold.  Calls with 512, 1024 and 2048 of
+// them, on one card: 64 x 1 over 16384 bf16 714, 722 and 726 us; 64 x 9 over 2048 to 8192 in 8 bits 217, 225 and 230; 2048 over 6144 389, 474 and 504.
 constexpr int kTargetGroups = 512;
 constexpr int kMaxSplits = 64;
 constexpr int kAttnWaves = 4;
@@ -929,11 +931,13 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, (DPAD == 256 || (ET == SV_F
 
 // Many rows: 128 to a workgroup, 32 to a wavefront, which all need the same keys and values.  A step of them at a time is staged in LDS as bfloat16
 // (8-bit ones are converted once, not by every wavefront), the next step under way in registers meanwhile.  The sixteen-byte chunks of a row are
-// permuted by its number, so that the rows of an operand (keys: sixteen rows, one chunk; values: one row, sixteen chunks) lie in different
-// banks.  What bounds it is the vector ALU beside the matrix cores: per 32 keys and 32 rows, 32 matrix instructions of 16 cycles and about 900
-// cycles of exponentials (16, four slots each), maxima, sums and conversions (160).  A wavefront at its products goes before the one
-// that shares its SIMD and is at its exponentials: 2048 over 6144 with 32 heads on 8, 450 us without that and 418 with it, on one card.  (The
-// scores of the next step formed beside the weights of this one, in one wavefront: 485.)
+// permuted by its number, so that the sixteen rows of a key operand lie in different banks.  Of a wavefront's step 32 cycles of bank conflicts are
+// counted, as many as its eight value reads have passes of sixteen lanes, whose groups read four rows, each permuted its own way.
+// What bounds it is the vector ALU beside the matrix cores: per 32 keys and 32 rows, 32 matrix instructions of 16 cycles and about 206 of the vector
+// ALU, some 900 cycles: exponentials (16, four slots each), maxima, sums, conversions, and 32 permutations that transpose the values.  A wavefront at its
+// products goes before the one that shares its SIMD and is at its exponentials: 2048 over 6144 with 32 heads on 8, 450 us without that and 418
+// with it, on one card, the median of the first twelve launches (of a hundred it is 375 us, of their first twelve 421).  (The scores of the next step
+// formed beside the weights of this one, in one wavefront: 485 and not 418.)
 constexpr int kTileKeys = kStep;
 
 template <int CT, int DPAD, bool WHOLE>

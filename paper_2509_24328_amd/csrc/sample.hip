@@ -26,8 +26,17 @@ constexpr int kDrawWaves = kDrawThreads / kWave;
 constexpr int kList = 2048;              // entries of the list
 constexpr int kPieceVecs = 8;            // vectors of a lane in a piece: 4096 bfloat16 or 2048 float32 entries
 constexpr int kOwn = kList / kDrawThreads;   // entries of the list that a thread owns
-constexpr int kNucleusRank = 40;         // first guess of a nucleus: the entries above this many lane maxima
-constexpr int kDeepRank = 1200;          // second guess: above this many vectors' maxima
+// Where a nucleus is guessed to end: above this many of the lanes' maxima, then above this many of the vectors'.  The first list is what one
+// wavefront settles, the second what kList holds.  us, bf16, a generator's logits (one entry in a hundred 8 above the rest).  512 x 128256: T 0.7, top-p
+// 0.8, 20, 40 and 80 lanes 69, 66 and 52; T 1, top-p 0.95, min-p 0.02 47.7, 47.5 and 47.3; 16 x 32000, T 0.7, top-p 0.8, 14.3, 15.4 and 19.0.  600, 1200
+// and 1800 vectors, 512 x 128256, T 1, top-p 0.95 201, 110 and 202; T 1.3, top-p 0.8 250, 201 and 233; deeper ones do not fit (T 1.3, top-p
+// 0.95 450 with each).
+constexpr int kNucleusRank = 40;
+constexpr int kDeepRank = 1200;
+// The first list is passed over where the lanes' maxima above it hold less than this of the nucleus.  0.6, 0.85 and 1, us: 512 x 128256, T 1, top-p 0.95
+// 117, 110 and 109, T 0.7, top-p 0.8 63, 66 and 59; 16 x 32000, T 1, top-p 0.95 32, 31 and 26.  (The maxima are not all that the list holds: it may
+// do where they do not.)
+constexpr double kReachedEnough = 0.85;
 constexpr int kMaxKeys = 40960;          // vectors' maxima in LDS (80 KB); longer rows share one among several vectors
 // Error of a float32 mass, relative: the exponent k of a weight is off by 2^-23 |k| (two roundings), which is 8.3e-8 |k| of the weight; an
 // average over the mass has |k| <= 24 (2^24 entries that far down weigh as much as the first), and 25.3 where the weights refer to
@@ -879,7 +888,7 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_kernel(SampleArgs a) {
       if (weigh && tau > min_key) {
         // a nucleus that the lanes' maxima above tau are far from filling is deeper than their list
         const double reached = team.sum(lane_key >= (tau >> 16) ? (double)d.fast.weight(mine - top) : 0.0);
-        if (reached < 0.85 * a.top_p * all) continue;
+        if (reached < kReachedEnough * a.top_p * all) continue;
       }
     } else if (want > 0 && want <= n_keys) {
       // three probes a step
@@ -1110,7 +1119,7 @@ __global__ void __launch_bounds__(kDrawThreads, 4) sample_kernel(SampleArgs a) {
   }
 }
 
-// Whether rows without warps are read by more than one workgroup each: a compute unit forms 30 weights in a nanosecond, so a second launch
+// Whether rows without warps are read by more than one workgroup each: a compute unit forms 2.2 to 2.6 weights in a nanosecond, so a second launch
 // (4 us) pays for long rows that leave most of the card idle.  One launch / two, us: bf16 64 x 16384 15.4 / 17.4, 64 x 32000 17.6 / 17.3, 64 x 152064
 // 58 / 26, 192 x 152064 67 / 52, 256 x 152064 69 / 68.
 inline bool sample_splits(int rows, int V) { return rows <= 192 && V >= 32000 && V <= (1 << 21); }
